@@ -389,6 +389,138 @@ int odb_generate(odb_model *m, odb_cache *c, int32_t *tokens_dev, int prompt_len
                  odb_generate_event *events, int32_t *event_tokens_dev, int max_events,
                  void *stream);
 
+/* ---- Paged K/V: requests of different lengths share a pool of pages ------------------------------------------
+ * The cache above holds sequences of one length.  Where requests of different lengths come, grow by blocks and are
+ * cut behind a predicted end (odb_predict_length), K/V live in pages: a page holds page_size consecutive positions of
+ * every K/V head of one layer, and a request's row of `tables` names its pages in order.  The caller owns all memory.
+ * These calls need no model and run on the current device.  They allocate and synchronise nothing, so they can be
+ * captured into a graph; several may run at once as long as what one writes no other reads or writes.
+ * What they read from device memory (lengths, tables, slots, positions) is checked there: an entry outside its
+ * range is taken as said below and never leads outside the buffers described. */
+enum { ODB_F16 = 0, ODB_BF16 = 1, ODB_F32 = 2 };
+
+/* The pool of one layer: element (page, head, position inside the page, channel) of k and of v lies at
+ * page * page_stride + head * head_stride + position * pos_stride + channel elements.
+ * Requirements: page_size a power of two from 16 to 4096; head_dim 64, 128 or 256; dtype ODB_F16 or ODB_BF16; strides
+ * not negative and multiples of 8, pos_stride below 2^24; k and v aligned to 16 bytes; n_pages * page_size < 2^31. */
+typedef struct {
+    void *k, *v;          /* dev */
+    int n_pages, page_size, n_kv_heads, head_dim, dtype;
+    long long page_stride, head_stride, pos_stride;
+} odb_pages;
+
+/* Page tables and slot maps of a step, from the requests' lengths.  For request r (of n, 1 to 4096): held[r] positions own
+ * pages so far, wanted[r] shall.  A request that wants fewer gives its last pages back, which go on top of the stack
+ * free_pages (in order of the requests); then those that want more take pages off its top, again in order.  A request is
+ * refused, and keeps what it holds, if the pages taken by it and all before it exceed those that are there (so that after
+ * the first refused one no other gets pages either), or if wanted[r] is negative or beyond columns * page_size.
+ *   held, wanted   dev int32 [n]; held is clamped to [0, columns * page_size]
+ *   tables         dev int32 [n, columns], read and written: entries of pages that were taken; all others stay as they are
+ *   free_pages     dev int32 [n_pages], read and written; n_free dev int32 [1]: how many of its entries are free pages
+ *   row_first, row_count   dev int32 [n]: the positions that the step computes, row_count[r] of them from row_first[r] on;
+ *                  either may be NULL: held[r], and wanted[r] - held[r] (none where that is negative)
+ * written:
+ *   len            dev int32 [n]: wanted[r], or held[r] where refused
+ *   cu_rows        dev int32 [n + 1]: rows in front of each request; all are capped at rows_cap
+ *   slots, positions   dev int32 [rows_cap]: for every row its position and its slot, page * page_size + position inside the
+ *                  page; -1 where the position lies outside [0, len[r]) or its page outside the pool.  Entries behind the last row stay.
+ *   state          dev int32 [4]: free pages afterwards (the next call's n_free), pages taken, given back, requests refused
+ * The same call with the same inputs writes the same values again.  Buffers must not overlap.  Asynchronous on `stream`.
+ * Errors: ODB_E_INVALID_ARG for NULL buffers, n outside [1, 4096], columns < 1, columns * page_size > 2^30, rows_cap outside
+ * [1, 2^24], n_pages < 1, a page size or a pool outside the requirements above, or buffers that overlap. */
+int odb_page_tables(const int32_t *held_dev, const int32_t *wanted_dev, int n, int page_size, int32_t *tables_dev,
+                    int columns, int32_t *free_pages_dev, int n_pages, const int32_t *n_free_dev,
+                    const int32_t *row_first_dev, const int32_t *row_count_dev, int32_t *len_dev,
+                    int32_t *cu_rows_dev, int32_t *slots_dev, int32_t *positions_dev, int rows_cap,
+                    int32_t *state_dev, void *stream);
+
+/* Rotary angles.  Pair j of rot_dim / 2 turns by p * f_j at position p, f_j = base^(-2j/rot_dim), and for contexts longer than
+ * the original one
+ *   ODB_ROPE_LINEAR  f_j / factor
+ *   ODB_ROPE_NTK     base * factor^(rot_dim / (rot_dim - 2)) instead of base (rot_dim = 2: unchanged)
+ *   ODB_ROPE_YARN    f_j (w + (1 - w) / factor), w = (original_len * f_j / 2 pi - beta_slow) / (beta_fast - beta_slow)
+ *                    clamped to [0, 1] (YaRN, arXiv 2309.00071: by the turns that a pair makes in the original context) */
+enum { ODB_ROPE_PLAIN = 0, ODB_ROPE_LINEAR, ODB_ROPE_NTK, ODB_ROPE_YARN };
+typedef struct {
+    double base;
+    int scaling;
+    double factor;                  /* >= 1; ignored by ODB_ROPE_PLAIN */
+    int original_len;               /* ODB_ROPE_YARN: positions of the original context */
+    double beta_fast, beta_slow;    /* ODB_ROPE_YARN: 32 and 1 in the paper */
+    double magnitude;               /* cosines and sines are multiplied by it; 0: 0.1 ln(factor) + 1 for YARN, else 1 */
+} odb_rope;
+
+/* table[p][j] = (cos, sin) of pair j at position p, dev float [n_pos, rot_dim / 2, 2]; rounded once from 64 bits.
+ * Asynchronous on `stream`.  Errors: ODB_E_INVALID_ARG for NULL, n_pos outside [1, 2^22], rot_dim odd or outside [2, 256],
+ * base <= 1, factor < 1, beta_fast <= beta_slow, beta_slow < 0, original_len < 1, a negative magnitude, numbers that are not finite. */
+int odb_rope_table(float *table_dev, int n_pos, int rot_dim, const odb_rope *rope, void *stream);
+
+/* Norms and rotation of queries and keys, K/V to their pages, in one pass over the projection's output.  For every row:
+ * q and k of each head are divided by their root mean square, sqrt(mean of squares + eps), and multiplied by the gain
+ * (skipped where the gain is NULL); then the first rot_dim channels of each head turn by the angles of the row's
+ * position: pairs are (j, j + rot_dim / 2), or with `interleaved` (2j, 2j + 1).  Queries go to q_out, keys and values to the
+ * row's slot.  All in 32 bits with one rounding at the end.
+ *   q [rows, n_heads, head_dim], k, v [rows, n_kv_heads, head_dim]: dev, in_dtype ODB_F32 or the pages' dtype; the heads of a
+ *       row follow each other, rows are q_row, k_row, v_row elements apart (three parts of one buffer, say)
+ *   table       dev float [n_pos, rot_dim / 2, 2] as odb_rope_table writes it
+ *   positions, slots   dev int32 [rows].  A position outside [0, n_pos) marks a padding row: its queries become zero, nothing
+ *               is stored.  A slot outside the pool stores nothing.  Slots must differ: of two rows with the same slot
+ *               either's values may remain, piece by piece.
+ *   q_out       dev [rows, n_heads, head_dim] of the pages' dtype, rows q_out_row elements apart; may be q itself
+ *               (same dtype and stride), otherwise it must not overlap q, k or v
+ * Requirements: buffers aligned to 16 bytes, row strides multiples of 8, rot_dim a multiple of 16 in [16, head_dim].
+ * Asynchronous on `stream`.  rows = 0 launches nothing.  Errors: ODB_E_INVALID_ARG. */
+typedef struct {
+    const void *q, *k, *v;
+    int in_dtype, rows, n_heads;
+    long long q_row, k_row, v_row;
+    const float *q_gain, *k_gain;   /* dev [head_dim] each, or both NULL */
+    float eps;
+    const float *table;
+    int n_pos, rot_dim, interleaved;
+    const int32_t *positions, *slots;
+    void *q_out;
+    long long q_out_row;
+} odb_qk_rows;
+int odb_qk_norm_rope(const odb_qk_rows *rows, const odb_pages *pages, void *stream);
+
+/* Attention of new rows over their requests' pages: out = softmax(scale * q k^T over the visible keys) v.
+ * Request r has rows cu_rows[r] .. cu_rows[r + 1] - 1 at positions first_pos[r], first_pos[r] + 1, ...; a row at position p
+ * sees key i (whatever the pages hold there, the rows' own K/V included once they are stored) iff
+ *   i < kv_len[r],  and with causal i <= p,  and with window > 0  |p - i| < window or i < sinks.
+ * A row that sees no key becomes zero.  What lies at positions that a row does not see has no influence on it, not even
+ * if it is infinite or no number.  Query head h reads K/V head h / (n_heads / n_kv_heads).
+ *   q, out   dev [rows, n_heads, head_dim] of the pages' dtype, rows q_row / out_row elements apart
+ *   cu_rows  dev int32 [n + 1], rising from 0; NULL: one row per request (rows = n).  Rows that belong to no request stay.
+ *   kv_len   dev int32 [n], clamped to [0, columns * page_size];  tables dev int32 [n, columns]: an entry outside the
+ *            pool stands for positions that nobody sees
+ *   first_pos  dev int32 [n], or NULL: the rows are the last positions, kv_len[r] - their number
+ *   max_rows, max_len   upper bounds of a request's rows and positions, or 0 where none are known (rows; columns *
+ *            page_size).  They choose the way of computing; a bound that does not hold costs time, not correctness.
+ *   workspace  dev, odb_paged_attention_workspace() bytes, aligned to 256, NULL where that says 0; holds the
+ *            sums of keys that are split over workgroups, means nothing between calls, must not be shared by calls that
+ *            overlap in time
+ * Scores and sums are 32-bit; probabilities are rounded to the pages' dtype for the product with V.  The order of all
+ * additions follows from the arguments and the lengths alone, so the same call gives the same bits.
+ * Asynchronous on `stream`.  Errors: ODB_E_INVALID_ARG for NULL buffers, n outside [1, 4096], rows outside [0, 2^24] (0: nothing is
+ * launched), n_heads no multiple of n_kv_heads, columns < 1, columns * page_size > 2^30, a scale that is not positive and
+ * finite, window or sinks negative or above 2^30, a workspace that is too small, buffers not aligned to 16 bytes, row
+ * strides that are no multiples of 8, out overlapping q, pools outside the requirements above. */
+typedef struct {
+    const void *q;
+    void *out;
+    long long q_row, out_row;
+    const int32_t *cu_rows, *first_pos, *kv_len, *tables;
+    int columns, n, rows, n_heads;
+    float scale;
+    int causal, window, sinks, max_rows, max_len;
+    void *workspace;
+    size_t workspace_bytes;
+} odb_attention;
+int odb_paged_attention(const odb_attention *a, const odb_pages *pages, void *stream);
+/* Bytes of workspace that the call needs (fields that are device buffers are not read, workspace is ignored), or a negative error code. */
+long long odb_paged_attention_workspace(const odb_attention *a, const odb_pages *pages);
+
 /* Copies cached K (kv = 0, post-RoPE, logical channel order) or V (kv = 1) of
  * positions pos0 .. pos0+n-1 of one sequence and layer to host memory as
  * float [n, n_heads, head_dim].  Synchronous (device-wide). */

@@ -24,7 +24,8 @@ SYMBOLS = (
     "odb_last_error", "odb_profile_begin", "odb_profile_end", "odb_set_option", "odb_model_status",
     "odb_predict_length", "odb_accept_jump", "odb_block_step_shared", "odb_block_step_static",
     "odb_block_step_shared_rows", "odb_block_step_shared_logits", "odb_cache_truncate", "odb_generate",
-    "odb_speculative_jump",
+    "odb_speculative_jump", "odb_page_tables", "odb_rope_table", "odb_qk_norm_rope", "odb_paged_attention",
+    "odb_paged_attention_workspace",
 )
 
 KERNEL_CLASSES = ("gemm_qkv", "attention", "gemm_o", "gemm_gate_up", "gemm_down", "gemm_lm_head", "rmsnorm")
@@ -69,6 +70,34 @@ class odb_generate_stats(ctypes.Structure):
                 ("final_len", ctypes.c_int), ("n_events", ctypes.c_int), ("refresh_positions", ctypes.c_longlong),
                 ("step_rows", ctypes.c_longlong), ("refresh_ms", ctypes.c_double), ("step_ms", ctypes.c_double),
                 ("total_ms", ctypes.c_double)]
+
+
+class odb_pages(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("n_pages", ctypes.c_int), ("page_size", ctypes.c_int),
+                ("n_kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int), ("dtype", ctypes.c_int),
+                ("page_stride", ctypes.c_longlong), ("head_stride", ctypes.c_longlong), ("pos_stride", ctypes.c_longlong)]
+
+
+class odb_rope(ctypes.Structure):
+    _fields_ = [("base", ctypes.c_double), ("scaling", ctypes.c_int), ("factor", ctypes.c_double), ("original_len", ctypes.c_int),
+                ("beta_fast", ctypes.c_double), ("beta_slow", ctypes.c_double), ("magnitude", ctypes.c_double)]
+
+
+class odb_qk_rows(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("in_dtype", ctypes.c_int),
+                ("rows", ctypes.c_int), ("n_heads", ctypes.c_int), ("q_row", ctypes.c_longlong), ("k_row", ctypes.c_longlong),
+                ("v_row", ctypes.c_longlong), ("q_gain", ctypes.c_void_p), ("k_gain", ctypes.c_void_p), ("eps", ctypes.c_float),
+                ("table", ctypes.c_void_p), ("n_pos", ctypes.c_int), ("rot_dim", ctypes.c_int), ("interleaved", ctypes.c_int),
+                ("positions", ctypes.c_void_p), ("slots", ctypes.c_void_p), ("q_out", ctypes.c_void_p), ("q_out_row", ctypes.c_longlong)]
+
+
+class odb_attention(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("out", ctypes.c_void_p), ("q_row", ctypes.c_longlong), ("out_row", ctypes.c_longlong),
+                ("cu_rows", ctypes.c_void_p), ("first_pos", ctypes.c_void_p), ("kv_len", ctypes.c_void_p), ("tables", ctypes.c_void_p),
+                ("columns", ctypes.c_int), ("n", ctypes.c_int), ("rows", ctypes.c_int), ("n_heads", ctypes.c_int),
+                ("scale", ctypes.c_float), ("causal", ctypes.c_int), ("window", ctypes.c_int), ("sinks", ctypes.c_int),
+                ("max_rows", ctypes.c_int), ("max_len", ctypes.c_int), ("workspace", ctypes.c_void_p),
+                ("workspace_bytes", ctypes.c_size_t)]
 
 
 EVENT_KINDS = ("refresh", "step", "shared")
@@ -117,6 +146,12 @@ def lib() -> ctypes.CDLL:
     L.odb_set_option.argtypes = [vp, ci, ci]
     L.odb_model_status.argtypes = [vp]
     L.odb_block_step_static.argtypes = [vp, vp, vp, ci, ci, ci, cf, vp, vp, vp, vp]
+    L.odb_page_tables.argtypes = [vp, vp, ci, ci, vp, ci, vp, ci, vp, vp, vp, vp, vp, vp, vp, ci, vp, vp]
+    L.odb_rope_table.argtypes = [vp, ci, ci, vp, vp]
+    L.odb_qk_norm_rope.argtypes = [vp, vp, vp]
+    L.odb_paged_attention.argtypes = [vp, vp, vp]
+    L.odb_paged_attention_workspace.argtypes = [vp, vp]
+    L.odb_paged_attention_workspace.restype = ctypes.c_longlong
     L.odb_strerror.argtypes = [ci]
     L.odb_strerror.restype = ctypes.c_char_p
     L.odb_last_error.restype = ctypes.c_char_p
@@ -394,6 +429,174 @@ def odb_cache_read(cache: int, layer: int, kv: int, batch_index: int, pos0: int,
                    head_dim: int) -> np.ndarray:
     out = np.empty((n, n_heads, head_dim), np.float32)
     _check(lib().odb_cache_read(cache, layer, kv, batch_index, pos0, n, out.ctypes.data))
+    return out
+
+
+# ---- paged K/V ------------------------------------------------------------------------------
+# These calls run on the device of their tensors (all of a call's on one) and on that device's current stream.
+
+ROPE_SCALINGS = ("plain", "linear", "ntk", "yarn")
+
+
+def _dtype_code(dtype):
+    import torch
+    try:
+        return {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}[dtype]
+    except KeyError:
+        raise TypeError("expected float16, bfloat16 or float32, got %s" % dtype) from None
+
+
+def _ints(device, **tensors):
+    """Addresses of contiguous int32 tensors of one device (None stays None), as (tensor, shape or None) by name."""
+    import torch
+    for name, (t, shape) in tensors.items():
+        if t is None:
+            continue
+        if t.dtype is not torch.int32 or not t.is_contiguous() or t.device != device or (shape is not None and tuple(t.shape) != shape):
+            raise TypeError("%s must be a contiguous int32 tensor on %s%s" % (name, device, "" if shape is None else " of shape %s" % (shape,)))
+    return [None if t is None else t.data_ptr() for t, _ in tensors.values()]
+
+
+def _on(device, call, *args):
+    """call(*args, stream) with `device` current."""
+    import torch
+    if device.type != "cuda":
+        raise OdbError("expected CUDA tensors")
+    if device.index is None or torch.cuda.current_device() == device.index:
+        _check(call(*args, _stream()))
+    else:
+        with torch.cuda.device(device):
+            _check(call(*args, _stream()))
+
+
+def _pages(k_pages, v_pages) -> odb_pages:
+    """Pools [n_pages, n_kv_heads, page_size, head_dim] of any strides whose channels follow each other."""
+    if k_pages.dim() != 4 or k_pages.shape != v_pages.shape or k_pages.stride() != v_pages.stride() or k_pages.stride(3) != 1:
+        raise TypeError("k_pages and v_pages must be [n_pages, n_kv_heads, page_size, head_dim] with the same strides, the last one 1")
+    if k_pages.dtype is not v_pages.dtype or k_pages.device != v_pages.device:
+        raise TypeError("k_pages and v_pages must be of one dtype and device")
+    n, h, p, d = k_pages.shape
+    sn, sh, sp, _ = k_pages.stride()
+    return odb_pages(k_pages.data_ptr(), v_pages.data_ptr(), n, p, h, d, _dtype_code(k_pages.dtype), sn, sh, sp)
+
+
+def _head_rows(name, t, device, dtype, shape):
+    """Row stride of a [rows, heads, head_dim] tensor whose heads follow each other."""
+    if t.dim() != 3 or t.device != device or t.dtype is not dtype or tuple(t.shape) != shape:
+        raise TypeError("%s must be a %s tensor of shape %s on %s" % (name, dtype, shape, device))
+    if t.stride(2) != 1 or (t.stride(1) != t.shape[2] and t.shape[1] != 1):
+        raise TypeError("the heads of a row of %s must follow each other" % name)
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1] * t.shape[2])
+
+
+def odb_page_tables(held, wanted, tables, free_pages, n_free, page_size: int, n_pages: int, row_first=None, row_count=None,
+                    rows_cap: int = 0, slots=None, positions=None, out=None):
+    """held, wanted int32 [n]; tables int32 [n, columns] and free_pages int32 [n_pages], updated in place; n_free int32 [1];
+    row_first, row_count int32 [n] or None -> (len int32 [n], cu_rows int32 [n + 1], slots, positions int32 [rows_cap],
+    state int32 [4]).  `slots` and `positions` may be given (their length is then rows_cap; entries behind the last row
+    stay), as may `out` = (len, cu_rows, state)."""
+    import torch
+    dev, n = held.device, held.numel()
+    if held.dim() != 1 or tables.dim() != 2:
+        raise TypeError("held must be [n] and tables [n, columns]")
+    new = lambda m: torch.empty((m,), dtype=torch.int32, device=dev)          # noqa: E731
+    if slots is None:
+        slots = new(rows_cap)
+    if positions is None:
+        positions = new(slots.shape[0])
+    length, cu_rows, state = out if out is not None else (new(n), new(n + 1), new(4))
+    p = _ints(dev, held=(held, (n,)), wanted=(wanted, (n,)), tables=(tables, (n, tables.shape[1])), free_pages=(free_pages, (n_pages,)),
+              n_free=(n_free, (1,)), row_first=(row_first, (n,)), row_count=(row_count, (n,)), len=(length, (n,)),
+              cu_rows=(cu_rows, (n + 1,)), slots=(slots, (slots.numel(),)), positions=(positions, (slots.numel(),)), state=(state, (4,)))
+    _on(dev, lib().odb_page_tables, p[0], p[1], n, page_size, p[2], tables.shape[1], p[3], n_pages, p[4], p[5], p[6], p[7], p[8], p[9], p[10],
+        slots.numel(), p[11])
+    return length, cu_rows, slots, positions, state
+
+
+def odb_rope_table(n_pos: int, rot_dim: int, base: float, scaling: str = "plain", factor: float = 1.0, original_len: int = 0,
+                   beta_fast: float = 32.0, beta_slow: float = 1.0, magnitude: float = 0.0, out=None, device=None):
+    """-> float32 [n_pos, rot_dim / 2, 2] of (cos, sin).  scaling: "plain", "linear", "ntk" or "yarn"."""
+    import torch
+    if scaling not in ROPE_SCALINGS:
+        raise ValueError("scaling is one of %s" % (ROPE_SCALINGS,))
+    shape = (n_pos, rot_dim // 2, 2)
+    if out is None:
+        out = torch.empty(shape, dtype=torch.float32, device=device if device is not None else "cuda")
+    elif out.dtype is not torch.float32 or tuple(out.shape) != shape or not out.is_contiguous():
+        raise TypeError("out must be a contiguous float32 tensor of shape %s" % (shape,))
+    r = odb_rope(base, ROPE_SCALINGS.index(scaling), factor, original_len, beta_fast, beta_slow, magnitude)
+    _on(out.device, lib().odb_rope_table, out.data_ptr(), n_pos, rot_dim, ctypes.byref(r))
+    return out
+
+
+def odb_qk_norm_rope(q, k, v, k_pages, v_pages, table, positions, slots, q_gain=None, k_gain=None, eps: float = 1e-6,
+                     interleaved: bool = False, out=None):
+    """q [rows, n_heads, head_dim], k and v [rows, n_kv_heads, head_dim], float32 or the pools' dtype, rows of any stride (three
+    parts of one buffer, say); k_pages, v_pages [n_pages, n_kv_heads, page_size, head_dim]; table float32 [n_pos, rot_dim / 2, 2];
+    positions, slots int32 [rows]; gains float32 [head_dim] -> queries [rows, n_heads, head_dim] in the pools' dtype.  K/V of
+    the rows go to the pools.  out may be q."""
+    import torch
+    dev, pages = q.device, _pages(k_pages, v_pages)
+    rows, heads, dim = q.shape
+    kv = (rows, pages.n_kv_heads, dim)
+    if k_pages.device != dev or dim != pages.head_dim:
+        raise TypeError("the pools must lie on %s and have heads of %d" % (dev, dim))
+    if out is None:
+        out = torch.empty((rows, heads, dim), dtype=k_pages.dtype, device=dev)
+    if table.dtype is not torch.float32 or table.dim() != 3 or table.shape[2] != 2 or not table.is_contiguous() or table.device != dev:
+        raise TypeError("table must be a contiguous float32 tensor [n_pos, rot_dim / 2, 2] on %s" % dev)
+    for name, gain in (("q_gain", q_gain), ("k_gain", k_gain)):
+        if gain is not None and (gain.dtype is not torch.float32 or tuple(gain.shape) != (dim,) or not gain.is_contiguous() or gain.device != dev):
+            raise TypeError("%s must be a contiguous float32 tensor [head_dim] on %s" % (name, dev))
+    strides = [_head_rows("q", q, dev, q.dtype, (rows, heads, dim)), _head_rows("k", k, dev, q.dtype, kv), _head_rows("v", v, dev, q.dtype, kv),
+               _head_rows("out", out, dev, k_pages.dtype, (rows, heads, dim))]
+    at = _ints(dev, positions=(positions, (rows,)), slots=(slots, (rows,)))
+    if rows == 0:
+        return out
+    r = odb_qk_rows(q.data_ptr(), k.data_ptr(), v.data_ptr(), _dtype_code(q.dtype), rows, heads, strides[0], strides[1], strides[2],
+                    None if q_gain is None else q_gain.data_ptr(), None if k_gain is None else k_gain.data_ptr(), eps, table.data_ptr(),
+                    table.shape[0], 2 * table.shape[1], bool(interleaved), at[0], at[1], out.data_ptr(), strides[3])
+    _on(dev, lib().odb_qk_norm_rope, ctypes.byref(r), ctypes.byref(pages))
+    return out
+
+
+def odb_paged_attention_workspace(a: odb_attention, pages: odb_pages) -> int:
+    n = lib().odb_paged_attention_workspace(ctypes.byref(a), ctypes.byref(pages))
+    _check(min(n, 0))
+    return n
+
+
+def odb_paged_attention(q, k_pages, v_pages, tables, kv_len, *, causal: bool, cu_rows=None, first_pos=None, scale: Optional[float] = None,
+                        window: int = 0, sinks: int = 0, max_rows: int = 0, max_len: int = 0, out=None, workspace=None):
+    """q [rows, n_heads, head_dim] of the pools' dtype; tables int32 [n, columns]; kv_len int32 [n]; cu_rows int32 [n + 1] (None:
+    one row per request); first_pos int32 [n] (None: the rows are the last positions); scale defaults to head_dim ** -0.5
+    -> [rows, n_heads, head_dim].  The workspace comes from torch's allocator unless a uint8 tensor is given."""
+    import torch
+    dev, pages = q.device, _pages(k_pages, v_pages)
+    rows, heads, dim = q.shape
+    if k_pages.device != dev or dim != pages.head_dim:
+        raise TypeError("the pools must lie on %s and have heads of %d" % (dev, dim))
+    if tables.dim() != 2:
+        raise TypeError("tables must be [n, columns]")
+    n, columns = tables.shape
+    if cu_rows is None and rows != n:
+        raise ValueError("without cu_rows every request has one row (%d rows, %d requests)" % (rows, n))
+    if out is None:
+        out = torch.empty((rows, heads, dim), dtype=q.dtype, device=dev)
+    strides = [_head_rows("q", q, dev, k_pages.dtype, (rows, heads, dim)), _head_rows("out", out, dev, q.dtype, (rows, heads, dim))]
+    at = _ints(dev, cu_rows=(cu_rows, (n + 1,)), first_pos=(first_pos, (n,)), kv_len=(kv_len, (n,)), tables=(tables, (n, columns)))
+    if rows == 0:
+        return out
+    a = odb_attention(q.data_ptr(), out.data_ptr(), strides[0], strides[1], at[0], at[1], at[2], at[3], columns, n, rows, heads,
+                      dim ** -0.5 if scale is None else scale, bool(causal), window, sinks, max_rows, max_len, None, 0)
+    need = odb_paged_attention_workspace(a, pages)
+    if workspace is None and need:
+        workspace = torch.empty((need,), dtype=torch.uint8, device=dev)
+    if workspace is not None:
+        if workspace.dtype is not torch.uint8 or not workspace.is_contiguous() or workspace.device != dev:
+            raise TypeError("workspace must be a contiguous uint8 tensor on %s" % dev)
+        a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
+    _on(dev, lib().odb_paged_attention, ctypes.byref(a), ctypes.byref(pages))
     return out
 
 

@@ -9,6 +9,7 @@
 #include <new>
 
 #include "choose.h"
+#include "errors.h"
 #include "model.h"
 
 using namespace odb;
@@ -16,11 +17,9 @@ using namespace odb;
 struct odb_model { Model m; };
 struct odb_cache { Cache c; };
 
-namespace {
+static thread_local char g_err[512] = "";
 
-thread_local char g_err[512] = "";
-
-int fail(int code, const char *fmt, ...) {
+int odb::fail(int code, const char *fmt, ...) {
     va_list ap;
     va_start(ap, fmt);
     vsnprintf(g_err, sizeof(g_err), fmt, ap);
@@ -28,11 +27,7 @@ int fail(int code, const char *fmt, ...) {
     return code;
 }
 
-#define HIP_TRY(expr)                                                                         \
-    do {                                                                                      \
-        hipError_t e_ = (expr);                                                               \
-        if (e_ != hipSuccess) return fail(ODB_E_HIP, "%s: %s", #expr, hipGetErrorString(e_)); \
-    } while (0)
+namespace {
 
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 inline int ru(int x, int a) { return (x + a - 1) / a * a; }

@@ -1,0 +1,74 @@
+// Paged K/V: the structures and launchers behind odb_page_tables, odb_rope_table, odb_qk_norm_rope and odb_paged_attention.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/odb.h"
+#include "common.h"
+
+namespace odb {
+
+constexpr int kMaxRequests = 4096;
+
+struct PageTables {
+    const int32_t *held, *wanted, *first, *count;      // first / count may be null: the rows behind the held positions
+    int n, page_shift, columns, n_pages, rows_cap;
+    int32_t *tables, *free_pages;
+    const int32_t *n_free;
+    int32_t *len, *cu_rows, *slots, *positions, *state;
+};
+void launch_page_tables(const PageTables &a, hipStream_t s);
+
+// Angle per position of every pair, in turns: hi + lo (two doubles, so that far positions keep their fraction)
+constexpr int kMaxRotPairs = 128;
+struct RopeTable {
+    float *table;
+    int n_pos, pairs;
+    double magnitude;
+    double hi[kMaxRotPairs], lo[kMaxRotPairs];
+};
+void launch_rope_angles(const RopeTable &a, hipStream_t s);
+
+struct QkNormRope {
+    const void *q, *k, *v;
+    int in_dtype;
+    long long q_row, k_row, v_row;      // elements from row to row; the heads of a row follow each other
+    int rows, heads;
+    const float *q_gain, *k_gain;       // null: no norm
+    float eps;
+    const float *table;
+    int n_pos, rot, interleaved;
+    const int32_t *positions, *slots;
+    void *q_out;
+    long long q_out_row;
+    odb_pages pages;
+};
+void launch_qk_norm_rope(const QkNormRope &a, hipStream_t s);
+
+struct PagedAttn {
+    const void *q;
+    void *out;
+    long long q_row, out_row;
+    int out_mt;                         // > 0: out is in operand tiles [heads * head_dim / 32][out_mt][512] (see common.h)
+    const int32_t *cu_rows, *first, *kv_len, *tables;   // cu_rows null: request r is row r; first null: the rows are the last positions
+    int columns, n, rows, heads, group;
+    float sc;                           // scale * log2(e)
+    int causal, window, sinks;
+    odb_pages pages;
+    int page_shift;
+    // A request's keys are split over workgroups (split > 0: that many parts per K/V head are aimed at, not counting one more for
+    // every row tile); their sums go to `partial`, [item][tile rows][head_dim] and (reference, sum) to `ml`; `where` tells the
+    // joining kernel of each (row, head) the first item and how many there are.
+    int split;
+    long long items;                    // workgroups of the grid per K/V head
+    float *partial;
+    float2 *ml;
+    int2 *where;
+};
+int paged_attn_tiles(const odb_pages &p, int group, int max_rows);                // 16-row tiles per workgroup: 1, 2 or 4
+// parts aimed at (0: no split) and the grid's items per K/V head
+void paged_attn_split(const odb_pages &p, int n, int rows, int group, int nt, long long max_len, int *split, long long *items);
+size_t paged_attn_workspace(const odb_pages &p, int rows, int heads, int nt, int split, long long items);
+void launch_paged_attention(PagedAttn a, int nt, void *workspace, hipStream_t s);
+
+}  // namespace odb
