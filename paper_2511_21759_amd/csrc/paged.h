@@ -56,19 +56,20 @@ struct PagedAttn {
     int causal, window, sinks;
     odb_pages pages;
     int page_shift;
-    // A request's keys are split over workgroups (split > 0: that many parts per K/V head are aimed at, not counting one more for
-    // every row tile); their sums go to `partial`, [item][tile rows][head_dim] and (reference, sum) to `ml`; `where` tells the
-    // joining kernel of each (row, head) the first item and how many there are.
+    // split > 0: that many workgroups per K/V head share the blocks of all (request, row tile) pairs; the sums of a pair that lies in
+    // more than one go to `partial`, [2 split][heads of K/V][tile rows][head_dim], and (reference, sum) to `ml`; `where` tells the
+    // joining kernel of each (row, head) the first of them, and their number * 64 + row of the tile (0: the row is done).
     int split;
     long long items;                    // workgroups of the grid per K/V head
+    int tile_rows;
     float *partial;
     float2 *ml;
     int2 *where;
 };
 int paged_attn_tiles(const odb_pages &p, int group, int max_rows);                // 16-row tiles per workgroup: 1, 2 or 4
-// parts aimed at (0: no split) and the grid's items per K/V head
+// workgroups per K/V head that share the keys (0: no split) and the grid's items per K/V head
 void paged_attn_split(const odb_pages &p, int n, int rows, int group, int nt, long long max_len, int *split, long long *items);
-size_t paged_attn_workspace(const odb_pages &p, int rows, int heads, int nt, int split, long long items);
+size_t paged_attn_workspace(const odb_pages &p, int rows, int heads, int nt, int split);
 void launch_paged_attention(PagedAttn a, int nt, void *workspace, hipStream_t s);
 
 }  // namespace odb

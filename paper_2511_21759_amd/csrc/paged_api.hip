@@ -193,7 +193,7 @@ long long odb_paged_attention_workspace(const odb_attention *a, const odb_pages 
     PagedAttn p;
     int nt;
     const int rc = plan_attention(a, pages, false, p, nt);
-    return rc ? rc : (long long)paged_attn_workspace(*pages, p.rows, p.heads, nt, p.split, p.items);
+    return rc ? rc : (long long)paged_attn_workspace(*pages, p.rows, p.heads, nt, p.split);
 }
 
 int odb_paged_attention(const odb_attention *a, const odb_pages *pages, void *stream) {
@@ -207,7 +207,7 @@ int odb_paged_attention(const odb_attention *a, const odb_pages *pages, void *st
     if (!a->kv_len || !a->tables) return fail(ODB_E_INVALID_ARG, "%s: NULL kv_len or tables", who);
     if (overlap(Range{a->out, span(a->rows, a->out_row, a->n_heads, dim, 2)}, Range{a->q, span(a->rows, a->q_row, a->n_heads, dim, 2)}))
         return fail(ODB_E_INVALID_ARG, "%s: out overlaps q", who);
-    const size_t need = paged_attn_workspace(*pages, p.rows, p.heads, nt, p.split, p.items);
+    const size_t need = paged_attn_workspace(*pages, p.rows, p.heads, nt, p.split);
     if (need && (!a->workspace || (uintptr_t)a->workspace & 255 || a->workspace_bytes < need))
         return fail(ODB_E_INVALID_ARG, "%s: a workspace of %zu bytes aligned to 256, given %zu", who, need, a->workspace ? a->workspace_bytes : 0);
     if (a->rows == 0) return ODB_OK;

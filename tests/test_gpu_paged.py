@@ -263,6 +263,17 @@ def test_long_keys_split_over_workgroups(page, max_len):
     rq.check(rq.run(causal=True, cu=False, max_len=max_len), causal=True)
 
 
+@pytest.mark.parametrize("n,kv", [(64, 1), (65, 1), (300, 1), (300, 2), (700, 4)])
+@pytest.mark.parametrize("max_len", [0, 64])
+def test_many_requests(n, kv, max_len):
+    """Lists of requests longer than a wave, with and without split keys; most of them short, some without rows or keys."""
+    rng = random.Random(n)
+    lens = [rng.choice([0, 1, 17, 40, rng.randint(1, 60), 700 if rng.random() < 0.05 else 33]) for _ in range(n)]
+    rows = [rng.choice([0, 1, 1, 1, min(3, max(1, length))]) for length in lens]
+    rq = Requests(n + kv, rows, lens, 2 * kv, kv, 64, "f16", 16)
+    rq.check(rq.run(causal=True, max_len=max_len), causal=True)
+
+
 @pytest.mark.parametrize("cache,dim", [("f16", 64), ("bf16", 128), ("f16", 256)])
 @pytest.mark.parametrize("causal,window,sinks", [(False, 0, 0), (True, 0, 0), (True, 1, 0), (True, 20, 3), (False, 20, 3), (True, 70, 40), (False, 300, 17), (True, 64, 2000)])
 def test_ragged_rows_masks_and_sinks(cache, dim, causal, window, sinks):
