@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Dict, Optional, Tuple
 
 import numpy as np
@@ -433,60 +434,67 @@ def odb_cache_read(cache: int, layer: int, kv: int, batch_index: int, pos0: int,
 
 
 # ---- paged K/V ------------------------------------------------------------------------------
-# These calls run on the device of their tensors (all of a call's on one) and on that device's current stream.
+# These calls run on the device of their tensors (all of a call's on one) and on that device's current stream.  A small one is
+# bound by its host side (about 4 us for the launch itself), so structures are packed and not filled field by field, and
+# checks look at each tensor once.
 
 ROPE_SCALINGS = ("plain", "linear", "ntk", "yarn")
+_PACK_PAGES, _PACK_QK_ROWS, _PACK_ATTENTION = (struct.Struct(f).pack for f in ("@PPiiiiiqqq", "@PPPiiiqqqPPfPiiiPPPq", "@PPqqPPPPiiiifiiiiiPN"))
+_torch = _raw_stream = None
 
 
-def _dtype_code(dtype):
+def _load_torch():
+    global _torch, _raw_stream, _DTYPES
     import torch
-    try:
-        return {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}[dtype]
-    except KeyError:
-        raise TypeError("expected float16, bfloat16 or float32, got %s" % dtype) from None
+    _torch = torch
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)          # (see _stream)
+    _DTYPES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
+    return torch
 
 
-def _ints(device, **tensors):
-    """Addresses of contiguous int32 tensors of one device (None stays None), as (tensor, shape or None) by name."""
-    import torch
-    for name, (t, shape) in tensors.items():
-        if t is None:
-            continue
-        if t.dtype is not torch.int32 or not t.is_contiguous() or t.device != device or (shape is not None and tuple(t.shape) != shape):
-            raise TypeError("%s must be a contiguous int32 tensor on %s%s" % (name, device, "" if shape is None else " of shape %s" % (shape,)))
-    return [None if t is None else t.data_ptr() for t, _ in tensors.values()]
+def _not_ints(name, shape):
+    raise TypeError("%s must be a contiguous int32 tensor of shape %s on the device of the others" % (name, shape))
 
 
-def _on(device, call, *args):
-    """call(*args, stream) with `device` current."""
-    import torch
-    if device.type != "cuda":
+def _ints(name, t, shape, index, i32):
+    """Address of a contiguous int32 tensor of that shape on that device."""
+    if t.dtype is not i32 or t.shape != shape or t.get_device() != index or not t.is_contiguous():
+        _not_ints(name, shape)
+    return t.data_ptr()
+
+
+def _on(index, call, *args):
+    """call(*args, stream) with device `index` current."""
+    if index < 0:
         raise OdbError("expected CUDA tensors")
-    if device.index is None or torch.cuda.current_device() == device.index:
-        _check(call(*args, _stream()))
+    if _torch.cuda.current_device() == index:
+        rc = call(*args, _raw_stream(index) if _raw_stream is not None else _stream())
+        if rc:
+            _check(rc)
     else:
-        with torch.cuda.device(device):
+        with _torch.cuda.device(index):
             _check(call(*args, _stream()))
 
 
-def _pages(k_pages, v_pages) -> odb_pages:
-    """Pools [n_pages, n_kv_heads, page_size, head_dim] of any strides whose channels follow each other."""
-    if k_pages.dim() != 4 or k_pages.shape != v_pages.shape or k_pages.stride() != v_pages.stride() or k_pages.stride(3) != 1:
+def _pages(k_pages, v_pages):
+    """Pools [n_pages, n_kv_heads, page_size, head_dim] of any strides whose channels follow each other, as a packed odb_pages."""
+    shape, strides = k_pages.shape, k_pages.stride()
+    if len(shape) != 4 or v_pages.shape != shape or v_pages.stride() != strides or strides[3] != 1:
         raise TypeError("k_pages and v_pages must be [n_pages, n_kv_heads, page_size, head_dim] with the same strides, the last one 1")
-    if k_pages.dtype is not v_pages.dtype or k_pages.device != v_pages.device:
-        raise TypeError("k_pages and v_pages must be of one dtype and device")
-    n, h, p, d = k_pages.shape
-    sn, sh, sp, _ = k_pages.stride()
-    return odb_pages(k_pages.data_ptr(), v_pages.data_ptr(), n, p, h, d, _dtype_code(k_pages.dtype), sn, sh, sp)
+    if v_pages.dtype is not k_pages.dtype or v_pages.get_device() != k_pages.get_device() or k_pages.dtype not in _DTYPES:
+        raise TypeError("k_pages and v_pages must be float16 or bfloat16, of one dtype and device")
+    return _PACK_PAGES(k_pages.data_ptr(), v_pages.data_ptr(), shape[0], shape[2], shape[1], shape[3], _DTYPES[k_pages.dtype],
+                       strides[0], strides[1], strides[2])
 
 
-def _head_rows(name, t, device, dtype, shape):
+def _head_rows(name, t, index, dtype, shape):
     """Row stride of a [rows, heads, head_dim] tensor whose heads follow each other."""
-    if t.dim() != 3 or t.device != device or t.dtype is not dtype or tuple(t.shape) != shape:
-        raise TypeError("%s must be a %s tensor of shape %s on %s" % (name, dtype, shape, device))
-    if t.stride(2) != 1 or (t.stride(1) != t.shape[2] and t.shape[1] != 1):
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != index:
+        raise TypeError("%s must be a %s tensor of shape %s on the device of the others" % (name, dtype, tuple(shape)))
+    row, head, channel = t.stride()
+    if channel != 1 or (head != shape[2] and shape[1] != 1):
         raise TypeError("the heads of a row of %s must follow each other" % name)
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1] * t.shape[2])
+    return row if shape[0] > 1 else max(row, shape[1] * shape[2])
 
 
 def odb_page_tables(held, wanted, tables, free_pages, n_free, page_size: int, n_pages: int, row_first=None, row_count=None,
@@ -495,37 +503,40 @@ def odb_page_tables(held, wanted, tables, free_pages, n_free, page_size: int, n_
     row_first, row_count int32 [n] or None -> (len int32 [n], cu_rows int32 [n + 1], slots, positions int32 [rows_cap],
     state int32 [4]).  `slots` and `positions` may be given (their length is then rows_cap; entries behind the last row
     stay), as may `out` = (len, cu_rows, state)."""
-    import torch
-    dev, n = held.device, held.numel()
-    if held.dim() != 1 or tables.dim() != 2:
-        raise TypeError("held must be [n] and tables [n, columns]")
-    new = lambda m: torch.empty((m,), dtype=torch.int32, device=dev)          # noqa: E731
+    torch = _torch or _load_torch()
+    index, n, i32, (rows, columns) = held.get_device(), held.numel(), torch.int32, tables.shape if tables.dim() == 2 else (-1, -1)
+    if rows != n:
+        _not_ints("tables", "[n, columns]")
     if slots is None:
-        slots = new(rows_cap)
+        slots = held.new_empty((rows_cap,))
+    cap = slots.numel()
     if positions is None:
-        positions = new(slots.shape[0])
-    length, cu_rows, state = out if out is not None else (new(n), new(n + 1), new(4))
-    p = _ints(dev, held=(held, (n,)), wanted=(wanted, (n,)), tables=(tables, (n, tables.shape[1])), free_pages=(free_pages, (n_pages,)),
-              n_free=(n_free, (1,)), row_first=(row_first, (n,)), row_count=(row_count, (n,)), len=(length, (n,)),
-              cu_rows=(cu_rows, (n + 1,)), slots=(slots, (slots.numel(),)), positions=(positions, (slots.numel(),)), state=(state, (4,)))
-    _on(dev, lib().odb_page_tables, p[0], p[1], n, page_size, p[2], tables.shape[1], p[3], n_pages, p[4], p[5], p[6], p[7], p[8], p[9], p[10],
-        slots.numel(), p[11])
+        positions = held.new_empty((cap,))
+    per = (n,)
+    p_held = _ints("held", held, per, index, i32)
+    length, cu_rows, state = held.new_empty((2 * n + 5,)).split((n, n + 1, 4)) if out is None else out
+    _on(index, lib().odb_page_tables, p_held, _ints("wanted", wanted, per, index, i32), n, page_size, _ints("tables", tables, (n, columns), index, i32),
+        columns, _ints("free_pages", free_pages, (n_pages,), index, i32), n_pages, _ints("n_free", n_free, (1,), index, i32),
+        None if row_first is None else _ints("row_first", row_first, per, index, i32),
+        None if row_count is None else _ints("row_count", row_count, per, index, i32), _ints("len", length, per, index, i32),
+        _ints("cu_rows", cu_rows, (n + 1,), index, i32), _ints("slots", slots, (cap,), index, i32),
+        _ints("positions", positions, (cap,), index, i32), cap, _ints("state", state, (4,), index, i32))
     return length, cu_rows, slots, positions, state
 
 
 def odb_rope_table(n_pos: int, rot_dim: int, base: float, scaling: str = "plain", factor: float = 1.0, original_len: int = 0,
                    beta_fast: float = 32.0, beta_slow: float = 1.0, magnitude: float = 0.0, out=None, device=None):
     """-> float32 [n_pos, rot_dim / 2, 2] of (cos, sin).  scaling: "plain", "linear", "ntk" or "yarn"."""
-    import torch
+    torch = _torch or _load_torch()
     if scaling not in ROPE_SCALINGS:
         raise ValueError("scaling is one of %s" % (ROPE_SCALINGS,))
     shape = (n_pos, rot_dim // 2, 2)
     if out is None:
         out = torch.empty(shape, dtype=torch.float32, device=device if device is not None else "cuda")
-    elif out.dtype is not torch.float32 or tuple(out.shape) != shape or not out.is_contiguous():
+    elif out.dtype is not torch.float32 or out.shape != shape or not out.is_contiguous():
         raise TypeError("out must be a contiguous float32 tensor of shape %s" % (shape,))
     r = odb_rope(base, ROPE_SCALINGS.index(scaling), factor, original_len, beta_fast, beta_slow, magnitude)
-    _on(out.device, lib().odb_rope_table, out.data_ptr(), n_pos, rot_dim, ctypes.byref(r))
+    _on(out.get_device(), lib().odb_rope_table, out.data_ptr(), n_pos, rot_dim, ctypes.byref(r))
     return out
 
 
@@ -535,68 +546,70 @@ def odb_qk_norm_rope(q, k, v, k_pages, v_pages, table, positions, slots, q_gain=
     parts of one buffer, say); k_pages, v_pages [n_pages, n_kv_heads, page_size, head_dim]; table float32 [n_pos, rot_dim / 2, 2];
     positions, slots int32 [rows]; gains float32 [head_dim] -> queries [rows, n_heads, head_dim] in the pools' dtype.  K/V of
     the rows go to the pools.  out may be q."""
-    import torch
-    dev, pages = q.device, _pages(k_pages, v_pages)
-    rows, heads, dim = q.shape
-    kv = (rows, pages.n_kv_heads, dim)
-    if k_pages.device != dev or dim != pages.head_dim:
-        raise TypeError("the pools must lie on %s and have heads of %d" % (dev, dim))
+    torch = _torch or _load_torch()
+    index, pages, dtype, i32, f32 = q.get_device(), _pages(k_pages, v_pages), q.dtype, torch.int32, torch.float32
+    shape = rows, heads, dim = q.shape
+    kv = (rows, k_pages.shape[1], dim)
+    if k_pages.get_device() != index or dim != k_pages.shape[3] or dtype not in _DTYPES:
+        raise TypeError("q and the pools must lie on one device and have heads of the same size, of float16, bfloat16 or float32")
     if out is None:
-        out = torch.empty((rows, heads, dim), dtype=k_pages.dtype, device=dev)
-    if table.dtype is not torch.float32 or table.dim() != 3 or table.shape[2] != 2 or not table.is_contiguous() or table.device != dev:
-        raise TypeError("table must be a contiguous float32 tensor [n_pos, rot_dim / 2, 2] on %s" % dev)
-    for name, gain in (("q_gain", q_gain), ("k_gain", k_gain)):
-        if gain is not None and (gain.dtype is not torch.float32 or tuple(gain.shape) != (dim,) or not gain.is_contiguous() or gain.device != dev):
-            raise TypeError("%s must be a contiguous float32 tensor [head_dim] on %s" % (name, dev))
-    strides = [_head_rows("q", q, dev, q.dtype, (rows, heads, dim)), _head_rows("k", k, dev, q.dtype, kv), _head_rows("v", v, dev, q.dtype, kv),
-               _head_rows("out", out, dev, k_pages.dtype, (rows, heads, dim))]
-    at = _ints(dev, positions=(positions, (rows,)), slots=(slots, (rows,)))
-    if rows == 0:
-        return out
-    r = odb_qk_rows(q.data_ptr(), k.data_ptr(), v.data_ptr(), _dtype_code(q.dtype), rows, heads, strides[0], strides[1], strides[2],
-                    None if q_gain is None else q_gain.data_ptr(), None if k_gain is None else k_gain.data_ptr(), eps, table.data_ptr(),
-                    table.shape[0], 2 * table.shape[1], bool(interleaved), at[0], at[1], out.data_ptr(), strides[3])
-    _on(dev, lib().odb_qk_norm_rope, ctypes.byref(r), ctypes.byref(pages))
+        out = q.new_empty(shape, dtype=k_pages.dtype)
+    if table.dtype is not f32 or table.dim() != 3 or table.shape[2] != 2 or table.get_device() != index or not table.is_contiguous():
+        raise TypeError("table must be a contiguous float32 tensor [n_pos, rot_dim / 2, 2] on the device of the others")
+    for gain in (q_gain, k_gain):
+        if gain is not None and (gain.dtype is not f32 or gain.shape != (dim,) or gain.get_device() != index or not gain.is_contiguous()):
+            raise TypeError("q_gain and k_gain must be contiguous float32 tensors [head_dim] on the device of the others")
+    r = _PACK_QK_ROWS(q.data_ptr(), k.data_ptr(), v.data_ptr(), _DTYPES[dtype], rows, heads, _head_rows("q", q, index, dtype, shape),
+                      _head_rows("k", k, index, dtype, kv), _head_rows("v", v, index, dtype, kv), 0 if q_gain is None else q_gain.data_ptr(),
+                      0 if k_gain is None else k_gain.data_ptr(), eps, table.data_ptr(), table.shape[0], 2 * table.shape[1], bool(interleaved),
+                      _ints("positions", positions, (rows,), index, i32), _ints("slots", slots, (rows,), index, i32), out.data_ptr(),
+                      _head_rows("out", out, index, k_pages.dtype, shape))
+    if rows:
+        _on(index, lib().odb_qk_norm_rope, r, pages)
     return out
 
 
-def odb_paged_attention_workspace(a: odb_attention, pages: odb_pages) -> int:
-    n = lib().odb_paged_attention_workspace(ctypes.byref(a), ctypes.byref(pages))
-    _check(min(n, 0))
+def odb_paged_attention_workspace(attention, pages) -> int:
+    """Of an odb_attention and odb_pages, or their bytes."""
+    n = lib().odb_paged_attention_workspace(*(x if isinstance(x, bytes) else ctypes.byref(x) for x in (attention, pages)))
+    if n < 0:
+        _check(n)
     return n
 
 
 def odb_paged_attention(q, k_pages, v_pages, tables, kv_len, *, causal: bool, cu_rows=None, first_pos=None, scale: Optional[float] = None,
                         window: int = 0, sinks: int = 0, max_rows: int = 0, max_len: int = 0, out=None, workspace=None):
-    """q [rows, n_heads, head_dim] of the pools' dtype; tables int32 [n, columns]; kv_len int32 [n]; cu_rows int32 [n + 1] (None:
+    """q [rows, n_heads, head_dim] of the pages' dtype; tables int32 [n, columns]; kv_len int32 [n]; cu_rows int32 [n + 1] (None:
     one row per request); first_pos int32 [n] (None: the rows are the last positions); scale defaults to head_dim ** -0.5
     -> [rows, n_heads, head_dim].  The workspace comes from torch's allocator unless a uint8 tensor is given."""
-    import torch
-    dev, pages = q.device, _pages(k_pages, v_pages)
-    rows, heads, dim = q.shape
-    if k_pages.device != dev or dim != pages.head_dim:
-        raise TypeError("the pools must lie on %s and have heads of %d" % (dev, dim))
+    torch = _torch or _load_torch()
+    index, pages, i32 = q.get_device(), _pages(k_pages, v_pages), torch.int32
+    shape = rows, heads, dim = q.shape
+    if k_pages.get_device() != index or dim != k_pages.shape[3]:
+        raise TypeError("q and the pools must lie on one device and have heads of the same size")
     if tables.dim() != 2:
-        raise TypeError("tables must be [n, columns]")
+        _not_ints("tables", "[n, columns]")
     n, columns = tables.shape
     if cu_rows is None and rows != n:
         raise ValueError("without cu_rows every request has one row (%d rows, %d requests)" % (rows, n))
     if out is None:
-        out = torch.empty((rows, heads, dim), dtype=q.dtype, device=dev)
-    strides = [_head_rows("q", q, dev, k_pages.dtype, (rows, heads, dim)), _head_rows("out", out, dev, q.dtype, (rows, heads, dim))]
-    at = _ints(dev, cu_rows=(cu_rows, (n + 1,)), first_pos=(first_pos, (n,)), kv_len=(kv_len, (n,)), tables=(tables, (n, columns)))
+        out = q.new_empty(shape)
+    fields = (q.data_ptr(), out.data_ptr(), _head_rows("q", q, index, k_pages.dtype, shape), _head_rows("out", out, index, q.dtype, shape),
+              0 if cu_rows is None else _ints("cu_rows", cu_rows, (n + 1,), index, i32),
+              0 if first_pos is None else _ints("first_pos", first_pos, (n,), index, i32), _ints("kv_len", kv_len, (n,), index, i32),
+              _ints("tables", tables, (n, columns), index, i32), columns, n, rows, heads, dim ** -0.5 if scale is None else scale, bool(causal),
+              window, sinks, max_rows, max_len)
+    if workspace is not None and (workspace.dtype is not torch.uint8 or workspace.get_device() != index or not workspace.is_contiguous()):
+        raise TypeError("workspace must be a contiguous uint8 tensor on the device of the others")
     if rows == 0:
         return out
-    a = odb_attention(q.data_ptr(), out.data_ptr(), strides[0], strides[1], at[0], at[1], at[2], at[3], columns, n, rows, heads,
-                      dim ** -0.5 if scale is None else scale, bool(causal), window, sinks, max_rows, max_len, None, 0)
+    a = _PACK_ATTENTION(*fields, 0, 0)
     need = odb_paged_attention_workspace(a, pages)
-    if workspace is None and need:
-        workspace = torch.empty((need,), dtype=torch.uint8, device=dev)
-    if workspace is not None:
-        if workspace.dtype is not torch.uint8 or not workspace.is_contiguous() or workspace.device != dev:
-            raise TypeError("workspace must be a contiguous uint8 tensor on %s" % dev)
-        a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
-    _on(dev, lib().odb_paged_attention, ctypes.byref(a), ctypes.byref(pages))
+    if need:
+        if workspace is None:
+            workspace = q.new_empty((need,), dtype=torch.uint8)
+        a = _PACK_ATTENTION(*fields, workspace.data_ptr(), workspace.numel())
+    _on(index, lib().odb_paged_attention, a, pages)
     return out
 
 

@@ -139,8 +139,12 @@ int odb_rope_table(float *table, int n_pos, int rot_dim, const odb_rope *rope, v
     const long double two_pi = 6.28318530717958647692528676655900577L;
     long double base = r.base;
     if (r.scaling == ODB_ROPE_NTK && rot_dim > 2) base *= powl(r.factor, (long double)rot_dim / (rot_dim - 2));
-    for (int j = 0; j < a.pairs; j++) {
-        long double f = powl(base, -2.0L * j / rot_dim);
+    // (a power for every 16th pair, products in between: they add at most 15 roundings of 2^-64)
+    const long double ratio = powl(base, -2.0L / rot_dim);
+    long double power = 1.0L;
+    for (int j = 0; j < a.pairs; j++, power *= ratio) {
+        if (j % 16 == 0) power = powl(base, -2.0L * j / rot_dim);
+        long double f = power;
         if (r.scaling == ODB_ROPE_LINEAR) f /= r.factor;
         if (yarn) {
             long double w = (r.original_len * f / two_pi - r.beta_slow) / ((long double)r.beta_fast - r.beta_slow);
