@@ -66,9 +66,10 @@ struct PagedAttn {
     float2 *ml;
     int2 *where;
 };
-int paged_attn_tiles(const odb_pages &p, int group, int max_rows);                // 16-row tiles per workgroup: 1, 2 or 4
-// workgroups per K/V head that share the keys (0: no split) and the grid's items per K/V head
-void paged_attn_split(const odb_pages &p, int n, int rows, int group, int nt, long long max_len, int *split, long long *items);
+// The way of a call: nt 16-row tiles per workgroup whose waves split the keys (1, 2 or 4), or kManyRows, where they split the rows;
+// workgroups per K/V head that share the keys (0: no split), and the grid's items per K/V head.
+constexpr int kManyRows = 0;
+void paged_attn_plan(const odb_pages &p, int n, int rows, int group, int max_rows, long long max_len, int *nt, int *split, long long *items);
 size_t paged_attn_workspace(const odb_pages &p, int rows, int heads, int nt, int split);
 void launch_paged_attention(PagedAttn a, int nt, void *workspace, hipStream_t s);
 

@@ -80,8 +80,7 @@ int plan_attention(const odb_attention *a, const odb_pages *pages, bool buffers,
     p.pages = *pages;
     p.page_shift = page_shift(pages->page_size);
     const int max_rows = a->max_rows > 0 && a->max_rows < a->rows ? a->max_rows : a->rows;
-    nt = paged_attn_tiles(*pages, p.group, max_rows);
-    paged_attn_split(*pages, a->n, a->rows, p.group, nt, a->max_len > 0 && a->max_len < most ? a->max_len : most, &p.split, &p.items);
+    paged_attn_plan(*pages, a->n, a->rows, p.group, max_rows, a->max_len > 0 && a->max_len < most ? a->max_len : most, &nt, &p.split, &p.items);
     if (p.items * pages->n_kv_heads > 0x7fffffffll || (long long)a->rows * a->n_heads > 0x7fffffffll)
         return fail(ODB_E_INVALID_ARG, "%s: %d rows of %d heads are too many for one launch", who, a->rows, a->n_heads);
     return ODB_OK;

@@ -70,9 +70,10 @@ __device__ __forceinline__ Request request_of(const PagedAttn &a, int r) {
     return q;
 }
 
-// The 32-key blocks that rows at positions pmin .. pmax may see: `head` blocks from key 0 (the first positions that stay
+// The blocks of 2^SHIFT keys that rows at positions pmin .. pmax may see: `head` blocks from key 0 (the first positions that stay
 // visible), then those from block `from` on; `count` in all.
 struct Blocks { int head, from, count; };
+template <int SHIFT = 5>
 __device__ __forceinline__ Blocks blocks_of(const PagedAttn &a, int len, int pmin, int pmax) {
     int lo = 0, hi = len;
     if (a.causal) hi = min(hi, pmax + 1);
@@ -81,10 +82,11 @@ __device__ __forceinline__ Blocks blocks_of(const PagedAttn &a, int len, int pmi
         hi = min(hi, pmax < 0 ? 0 : pmax > kFar - a.window ? kFar : pmax + a.window);
     }
     Blocks b;
-    const int last = hi > lo ? (hi + 31) >> 5 : 0;
-    b.from = hi > lo ? lo >> 5 : 0;
+    constexpr int M = (1 << SHIFT) - 1;
+    const int last = hi > lo ? (hi + M) >> SHIFT : 0;
+    b.from = hi > lo ? lo >> SHIFT : 0;
     const int stay = min(a.window ? a.sinks : 0, a.causal ? min(len, pmax + 1) : len);
-    b.head = stay > 0 ? (stay + 31) >> 5 : 0;
+    b.head = stay > 0 ? (stay + M) >> SHIFT : 0;
     if (last > b.from) {
         b.head = min(b.head, b.from);
         b.count = b.head + last - b.from;
@@ -94,7 +96,8 @@ __device__ __forceinline__ Blocks blocks_of(const PagedAttn &a, int len, int pmi
     }
     return b;
 }
-__device__ __forceinline__ int block_key(const Blocks &b, int i) { return (i < b.head ? i : b.from + i - b.head) * 32; }
+template <int SHIFT = 5>
+__device__ __forceinline__ int block_key(const Blocks &b, int i) { return (i < b.head ? i : b.from + i - b.head) << SHIFT; }
 
 // positions of a tile's first and last row
 __device__ __forceinline__ void tile_span(const Request &q, int group, int tile, int tile_rows, int &pmin, int &pmax) {
@@ -199,14 +202,139 @@ __device__ __forceinline__ void store_out8(const PagedAttn &a, int row, int head
     }
 }
 
-// ---- the kernel -------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ void store_out4(const PagedAttn &a, int row, int head, int dim, int c, const uint2 &v) {
+    if (a.out_mt > 0) {
+        const int kk = head * dim + c;
+        u16 *p = (u16 *)a.out + ((size_t)(kk >> 5) * a.out_mt + (row >> 4)) * kTileElems + tile_elem(row & 15, kk & 31);
+        *reinterpret_cast<uint2 *>(p) = v;
+    } else {
+        *reinterpret_cast<uint2 *>((u16 *)a.out + (size_t)row * a.out_row + (size_t)head * dim + c) = v;
+    }
+}
 
-// Where the 16-byte piece `c` of key row `key` lies in a wave's V block: pieces are exchanged inside 256 bytes so that the
+// ---- pieces of the loops ----------------------------------------------------------------------------------------------
+
+// Probabilities of 32 keys for a row tile from its scores z (keys that are not seen: -infinity), as the operand of the product
+// with V; the reference is raised, and sums and O rescaled, where a score passes it by too much.  It is common to the four lanes of
+// a row and only has to keep exp2 in range, so after the first blocks that is rare, and the common path has no exchange of lanes.
+template <class T, int CT>
+__device__ __forceinline__ frag_t probabilities(f32x4 (&z)[2], float sc, float &mref, f32x4 &lsum, f32x4 (&o)[CT]) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int s = 0; s < 2; s++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) top = fmaxf(top, z[s][e]);
+    if (__any(top * sc > mref + kRaise)) {
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float up = fmaxf(mref, top * sc - kShift);
+        const float f = __builtin_amdgcn_exp2f(mref - (up == -INFINITY ? 0.f : up));
+        lsum *= f;
+#pragma unroll
+        for (int c = 0; c < CT; c++) o[c] *= f;
+        mref = up;
+    }
+    const float ref = mref == -INFINITY ? 0.f : mref;
+    float p[2][4];
+#pragma unroll
+    for (int s = 0; s < 2; s++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) p[s][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[s][e], sc, -ref));
+    // Probabilities are rounded to the type of V for the matrix cores; the sum that divides them at the end is that of the
+    // rounded ones, so what equal rounding errors have in common drops out.
+    return frag_t{{Num<T>::pack(p[0][0], p[0][1]), Num<T>::pack(p[0][2], p[0][3]), Num<T>::pack(p[1][0], p[1][1]), Num<T>::pack(p[1][2], p[1][3])}};
+}
+
+// Values of V that are infinite or no number must not reach a row that does not see their key, not even times zero.  In blocks
+// that not all rows see in full they are looked for; where there are any, they are added one by one to the rows that see them
+// (add_odd) and the product has zeros in their place (clear_odd).
+template <class T>
+__device__ __forceinline__ int has_odd(const frag_t &v) {
+    int odd = 0;
+#pragma unroll
+    for (int w = 0; w < 4; w++)
+        odd |= (int)((v.w[w] & Num<T>::kExp) == Num<T>::kExp) | (int)(((v.w[w] >> 16) & Num<T>::kExp) == Num<T>::kExp);
+    return odd;
+}
+template <class T>
+__device__ __forceinline__ void clear_odd(frag_t &v) {
+#pragma unroll
+    for (int w = 0; w < 4; w++) {
+        if ((v.w[w] & Num<T>::kExp) == Num<T>::kExp) v.w[w] &= 0xffff0000u;
+        if (((v.w[w] >> 16) & Num<T>::kExp) == Num<T>::kExp) v.w[w] &= 0xffffu;
+    }
+}
+
+// Where the 16-byte piece `c` of key row `key` lies in a block of V: pieces are exchanged inside 256 bytes so that the
 // 8-byte reads of eight neighbouring keys, 32 bytes of each, fall on all 64 banks.
 template <int DH>
 __device__ __forceinline__ int v_piece(int key, int c) {
     return key * (DH / 8) + (DH == 64 ? c ^ (((key >> 1) & 3) << 1) : c ^ ((key & 7) << 1));
 }
+
+template <class T, int DH, class See>
+__device__ __forceinline__ void add_odd(const unsigned char *v_block, int lane, const frag_t &pf, See see, f32x4 (&o)[DH / 16]) {
+    int dl = lane;                            // (hidden from the compiler, which else keeps this part's addresses in registers)
+    asm volatile("" : "+v"(dl));
+    for (int key = 0; key < 32; key++) {
+        const int src = (dl & 15) + 16 * ((key >> 2) & 3);       // the lane that holds the row's probability of this key
+        const uint32_t w0 = (uint32_t)__shfl((int)pf.w[0], src), w1 = (uint32_t)__shfl((int)pf.w[1], src);
+        const uint32_t w2 = (uint32_t)__shfl((int)pf.w[2], src), w3 = (uint32_t)__shfl((int)pf.w[3], src);
+        const uint32_t a0 = key & 16 ? w2 : w0, a1 = key & 16 ? w3 : w1, word = key & 2 ? a1 : a0;
+        const float p = Num<T>::value(key & 1 ? word >> 16 : word & 0xffffu);
+        const bool seen = see(key);
+#pragma unroll
+        for (int c = 0; c < DH / 16; c++)
+#pragma unroll
+            for (int d = 0; d < 4; d++) {
+                const int ch = c * 16 + 4 * (dl >> 4) + d;
+                const uint32_t v = *reinterpret_cast<const u16 *>(v_block + 16 * v_piece<DH>(key, ch >> 3) + 2 * (ch & 7));
+                if ((int)seen & (int)((v & Num<T>::kExp) == Num<T>::kExp)) o[c][d] += p * Num<T>::value(v);
+            }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+
+// V^T of a 32-key block in operand order: a lane's channel is (lane & 15) of tile c, its keys 4 (lane >> 4) + 0..3 of each 16
+template <int DH>
+__device__ __forceinline__ frag_t v_operand(const unsigned char *v_block, int lane, int c) {
+    typedef const __attribute__((address_space(3))) s16x4 *lds_ptr;
+    const int li = lane & 15, row = 4 * (lane >> 4) + (li >> 2), at = 2 * c + ((li >> 1) & 1);
+    const unsigned char *p0 = v_block + 16 * v_piece<DH>(row, at) + 8 * (li & 1), *p1 = p0 + 16 * DH * 2;
+    const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(lds_ptr)p0));
+    const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(lds_ptr)p1));
+    return frag_t{{lo.x, lo.y, hi.x, hi.y}};
+}
+
+// Load of 16 bytes at a scalar address plus a lane's offset.  STREAM: data that is read once, past the caches' replacement.
+template <bool STREAM>
+__device__ __forceinline__ frag_t ld_at(const u16 *uniform, unsigned lane_bytes) {
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    typedef const __attribute__((address_space(1))) char *global_bytes;
+    typedef const __attribute__((address_space(1))) u32x4 *global_ptr;
+    global_bytes base = (global_bytes)(uintptr_t)uniform;
+    asm("" : "+s"(base));                                         // (keeps the sum of a scalar base and a 32-bit offset apart)
+    const global_ptr p = (global_ptr)(base + lane_bytes);
+    return __builtin_bit_cast(frag_t, STREAM ? __builtin_nontemporal_load(p) : *p);
+}
+
+// the keys that a row at position p sees: lo .. hi - 1 and 0 .. stay - 1
+struct Sight { int lo, hi, stay; };
+__device__ __forceinline__ Sight sight_of(const PagedAttn &a, int len, int pos) {
+    const int p = min(pos, kFar - 1), end = a.causal ? min(len, p + 1) : len;
+    return Sight{a.window ? p - a.window + 1 : 0, a.window ? min(end, p + a.window) : end, a.window ? min(a.sinks, end) : 0};
+}
+// (no branches: bitwise operators)
+__device__ __forceinline__ bool sees(const Sight &s, int key, int page) {
+    return ((int)(page >= 0) & (((int)(key >= s.lo) & (int)(key < s.hi)) | (int)(key < s.stay))) != 0;
+}
+// is every one of n keys from key0 on visible to every row at positions pmin .. pmax?
+__device__ __forceinline__ bool all_seen(const PagedAttn &a, int len, int key0, int n, int pmin, int pmax) {
+    const int last = key0 + n - 1;
+    return last < len && (!a.causal || last <= pmin) && (!a.window || last < a.sinks || (key0 > pmax - a.window && last - pmin < a.window));
+}
+
+// ---- few rows: the waves of a workgroup split the keys -----------------------------------------------------------------
 
 // With keys split (a.split workgroups per K/V head), the blocks of all (request, row tile) pairs lie behind each other and every
 // workgroup takes an equal piece of that list, wherever it starts and ends: all finish together, however ragged the lengths are.
@@ -240,17 +368,6 @@ __global__ __launch_bounds__(256, DH == 256 || NT == 4 ? 1 : 2) void paged_attn_
     const unsigned k_off = 2u * (li * (unsigned)pos_stride + 8 * g), v_off = 2u * (v_key * (unsigned)pos_stride + v_ch * 8);    // bytes
     unsigned char *mine = lds + wave * WAVE_LDS;
     const frag_t ones = {{Num<T>::kOnes, Num<T>::kOnes, Num<T>::kOnes, Num<T>::kOnes}};
-    // K/V of a request with one row tile are read once: past the caches' replacement
-    auto ld = [](const u16 *uniform, unsigned lane_bytes) -> frag_t {
-        typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-        typedef const __attribute__((address_space(1))) char *global_bytes;
-        typedef const __attribute__((address_space(1))) u32x4 *global_ptr;
-        global_bytes base = (global_bytes)(uintptr_t)uniform;
-        asm("" : "+s"(base));                                     // (keeps the sum of a scalar base and a 32-bit offset apart)
-        const global_ptr p = (global_ptr)(base + lane_bytes);
-        return __builtin_bit_cast(frag_t, NT == 1 ? __builtin_nontemporal_load(p) : *p);
-    };
-
     Request rq = pl.q;
     int request = pl.r, tiles = tiles_of(a, rq, TILE_ROWS), nb = split ? request_blocks(a, rq) : 1;
     int tile = __builtin_amdgcn_readfirstlane((int)(pl.at / nb)), b_lo = __builtin_amdgcn_readfirstlane((int)(pl.at - (long long)tile * nb));
@@ -272,14 +389,11 @@ __global__ __launch_bounds__(256, DH == 256 || NT == 4 ? 1 : 2) void paged_attn_
 
         // queries of the tile, in operand order; rows behind the last repeat it and are not written
         frag_t q[NT][KS];
-        int see_lo[NT], see_hi[NT], stay[NT];                     // the lane's row sees keys see_lo .. see_hi - 1 and 0 .. stay - 1
+        Sight sight[NT];                                          // of the lane's row of each tile
 #pragma unroll
         for (int t = 0; t < NT; t++) {
             const int rho = min(rho0 + t * 16 + (ql & 15), n_rows - 1), i = rho / G, hq = head * G + (rho - i * G);
-            const int p = min(rq.first + i, kFar - 1), end = a.causal ? min(rq.len, p + 1) : rq.len;
-            see_lo[t] = a.window ? p - a.window + 1 : 0;
-            see_hi[t] = a.window ? min(end, p + a.window) : end;
-            stay[t] = a.window ? min(a.sinks, end) : 0;
+            sight[t] = sight_of(a, rq.len, rq.first + i);
             const u16 *src = (const u16 *)a.q + (size_t)(rq.row0 + i) * a.q_row + (size_t)hq * DH + 8 * (ql >> 4);
 #pragma unroll
             for (int k = 0; k < KS; k++) q[t][k] = ld_frag(src + 32 * k);
@@ -305,13 +419,13 @@ __global__ __launch_bounds__(256, DH == 256 || NT == 4 ? 1 : 2) void paged_attn_
         auto tile_base = [&](int page, int key) -> size_t { return (size_t)max(page, 0) * page_stride + (size_t)(key & page_mask) * pos_stride; };
         auto load_k = [&](size_t base0, size_t base1, unsigned off) {
 #pragma unroll
-            for (int k = 0; k < KS; k++) kf[0][k] = ld(kp + base0 + 32 * k, off);
+            for (int k = 0; k < KS; k++) kf[0][k] = ld_at<NT == 1>(kp + base0 + 32 * k, off);     // (a request with one row tile reads its K/V once)
 #pragma unroll
-            for (int k = 0; k < KS; k++) kf[1][k] = ld(kp + base1 + 32 * k, off);
+            for (int k = 0; k < KS; k++) kf[1][k] = ld_at<NT == 1>(kp + base1 + 32 * k, off);
         };
         auto load_v = [&](size_t base0, size_t base1, unsigned off) {
 #pragma unroll
-            for (int j = 0; j < VL; j++) vf[j] = ld(vp + (j < VL / 2 ? base0 : base1) + (size_t)(j % (VL / 2) * KEYS) * pos_stride, off);
+            for (int j = 0; j < VL; j++) vf[j] = ld_at<NT == 1>(vp + (j < VL / 2 ? base0 : base1) + (size_t)(j % (VL / 2) * KEYS) * pos_stride, off);
         };
 
         int b = b_lo + wave;
@@ -338,12 +452,8 @@ __global__ __launch_bounds__(256, DH == 256 || NT == 4 ? 1 : 2) void paged_attn_
                 base0 = tile_base(npg0, nkey);
                 base1 = tile_base(npg1, nkey + 16);
                 // is every key of the block visible to every row of the tile?
-                const bool plain = pg0 >= 0 && pg1 >= 0 && key0 + 31 < rq.len && (!a.causal || key0 + 31 <= pmin) &&
-                                   (!a.window || key0 + 31 < a.sinks || (key0 > pmax - a.window && key0 + 31 - pmin < a.window));
-                // (no branches: bitwise operators)
-                auto visible = [&](int t, int key, int page) -> bool {
-                    return ((int)(page >= 0) & (((int)(key >= see_lo[t]) & (int)(key < see_hi[t])) | (int)(key < stay[t]))) != 0;
-                };
+                const bool plain = pg0 >= 0 && pg1 >= 0 && all_seen(a, rq.len, key0, 32, pmin, pmax);
+                auto visible = [&](int t, int key, int page) -> bool { return sees(sight[t], key, page); };
                 f32x4 st[2][2];                                       // scores of this row tile and the next
                 auto scores = [&](int t) {
 #pragma unroll
@@ -358,13 +468,9 @@ __global__ __launch_bounds__(256, DH == 256 || NT == 4 ? 1 : 2) void paged_attn_
                 if (NT == 1) load_k(base0, base1, k_next);            // the registers of K are free for the next block
                 bool dirty = false;
                 if (!plain) {
-                    // a value that is no number must not reach a row that does not see its key, not even times zero
                     int odd = 0;
 #pragma unroll
-                    for (int j = 0; j < VL; j++)
-#pragma unroll
-                        for (int w = 0; w < 4; w++)
-                            odd |= (int)((vf[j].w[w] & Num<T>::kExp) == Num<T>::kExp) | (int)(((vf[j].w[w] >> 16) & Num<T>::kExp) == Num<T>::kExp);
+                    for (int j = 0; j < VL; j++) odd |= has_odd<T>(vf[j]);
                     dirty = __any(odd);
                 }
                 __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -373,29 +479,13 @@ __global__ __launch_bounds__(256, DH == 256 || NT == 4 ? 1 : 2) void paged_attn_
                     *reinterpret_cast<frag_t *>(mine + 16 * v_piece<DH>(v_key + j % (8 / KEYS) * KEYS, v_ch) + j / (8 / KEYS) * (8 * DH * 2)) = vf[j];
                 __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
                 load_v(base0, base1, v_next);
-                // V^T in operand order: a lane's channel is li of tile c, its keys 4 g .. 4 g + 3 of each 16
-                auto v_tile = [&](int c) -> frag_t {
-                    typedef __attribute__((address_space(3))) s16x4 *lds_ptr;
-                    const int row = 4 * g + (li >> 2), at = 2 * c + ((li >> 1) & 1);
-                    unsigned char *p0 = mine + 16 * v_piece<DH>(row, at) + 8 * (li & 1), *p1 = p0 + 16 * DH * 2;
-                    const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)p0));
-                    const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)p1));
-                    return frag_t{{lo.x, lo.y, hi.x, hi.y}};
-                };
-                auto clear_odd = [](frag_t &v) {
-#pragma unroll
-                    for (int w = 0; w < 4; w++) {
-                        if ((v.w[w] & Num<T>::kExp) == Num<T>::kExp) v.w[w] &= 0xffff0000u;
-                        if (((v.w[w] >> 16) & Num<T>::kExp) == Num<T>::kExp) v.w[w] &= 0xffffu;
-                    }
-                };
                 frag_t vt[NT > 1 ? CT : 1];                           // held for several row tiles
                 if (NT > 1) {
 #pragma unroll
-                    for (int c = 0; c < CT; c++) vt[c] = v_tile(c);
+                    for (int c = 0; c < CT; c++) vt[c] = v_operand<DH>(mine, lane, c);
                     if (__builtin_expect(dirty, 0))
 #pragma unroll
-                        for (int c = 0; c < CT; c++) clear_odd(vt[c]);
+                        for (int c = 0; c < CT; c++) clear_odd<T>(vt[c]);
                 }
 
                 // row tiles one after the other, the next one's scores under way in the matrix cores while this one's probabilities are made
@@ -404,68 +494,21 @@ __global__ __launch_bounds__(256, DH == 256 || NT == 4 ? 1 : 2) void paged_attn_
                     if (t + 1 < NT) scores(t + 1);
                     if (NT > 1 && t + 2 == NT) load_k(base0, base1, k_next);
                     f32x4 (&z)[2] = st[t & 1];
-                    float top = -INFINITY;
                     if (!plain) {
 #pragma unroll
                         for (int s = 0; s < 2; s++)
 #pragma unroll
                             for (int e = 0; e < 4; e++) z[s][e] = visible(t, key0 + s * 16 + 4 * g + e, s ? pg1 : pg0) ? z[s][e] : -INFINITY;
                     }
-#pragma unroll
-                    for (int s = 0; s < 2; s++)
-#pragma unroll
-                        for (int e = 0; e < 4; e++) top = fmaxf(top, z[s][e]);
-                    // The reference is common to the four lanes of a row and only has to keep exp2 in range: it is raised, with a
-                    // maximum across the lanes and a rescaling, when a score passes it by too much, which after the first blocks is rare.
-                    if (__any(top * a.sc > mref[t] + kRaise)) {
-                        top = fmaxf(top, __shfl_xor(top, 16));
-                        top = fmaxf(top, __shfl_xor(top, 32));
-                        const float up = fmaxf(mref[t], top * a.sc - kShift);
-                        const float f = __builtin_amdgcn_exp2f(mref[t] - (up == -INFINITY ? 0.f : up));
-                        lsum[t] *= f;
-#pragma unroll
-                        for (int c = 0; c < CT; c++) o[t][c] *= f;
-                        mref[t] = up;
-                    }
-                    const float ref = mref[t] == -INFINITY ? 0.f : mref[t];
-                    float p[2][4];
-#pragma unroll
-                    for (int s = 0; s < 2; s++)
-#pragma unroll
-                        for (int e = 0; e < 4; e++) p[s][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[s][e], a.sc, -ref));
-                    // Probabilities are rounded to the type of V for the matrix cores; the sum that divides them at the end is that of the
-                    // rounded ones, so what equal rounding errors have in common drops out.
-                    frag_t pf;
-                    pf.w[0] = Num<T>::pack(p[0][0], p[0][1]);
-                    pf.w[1] = Num<T>::pack(p[0][2], p[0][3]);
-                    pf.w[2] = Num<T>::pack(p[1][0], p[1][1]);
-                    pf.w[3] = Num<T>::pack(p[1][2], p[1][3]);
+                    const frag_t pf = probabilities<T, CT>(z, a.sc, mref[t], lsum[t], o[t]);
                     if (__builtin_expect(dirty, 0)) {
-                        // rare: values that are infinite or no number, in a block that not all rows see in full.  They are added one by
-                        // one to the rows that see them; the product has zeros in their place.
-                        int dl = lane;                            // (hidden, as below)
-                        asm volatile("" : "+v"(dl));
-                        for (int key = 0; key < 32; key++) {
-                            const int src = (dl & 15) + 16 * ((key >> 2) & 3);       // the lane that holds the row's probability of this key
-                            const uint32_t w0 = (uint32_t)__shfl((int)pf.w[0], src), w1 = (uint32_t)__shfl((int)pf.w[1], src);
-                            const uint32_t w2 = (uint32_t)__shfl((int)pf.w[2], src), w3 = (uint32_t)__shfl((int)pf.w[3], src);
-                            const uint32_t a0 = key & 16 ? w2 : w0, a1 = key & 16 ? w3 : w1, word = key & 2 ? a1 : a0;
-                            const float pk = Num<T>::value(key & 1 ? word >> 16 : word & 0xffffu);
-                            const bool see = visible(t, key0 + key, key & 16 ? pg1 : pg0);
-#pragma unroll
-                            for (int c = 0; c < CT; c++)
-#pragma unroll
-                                for (int d = 0; d < 4; d++) {
-                                    const int ch = c * 16 + 4 * (dl >> 4) + d;
-                                    const uint32_t v = *reinterpret_cast<const u16 *>(mine + 16 * v_piece<DH>(key, ch >> 3) + 2 * (ch & 7));
-                                    if ((int)see & (int)((v & Num<T>::kExp) == Num<T>::kExp)) o[t][c][d] += pk * Num<T>::value(v);
-                                }
-                        }
+                        add_odd<T, DH>(mine, lane, pf, [&](int key) { return visible(t, key0 + key, key & 16 ? pg1 : pg0); }, o[t]);
                         if (NT == 1) {
-                            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                            int dl = lane;
+                            asm volatile("" : "+v"(dl));
                             for (int j = 0; j < VL; j++) {
                                 frag_t *at = reinterpret_cast<frag_t *>(mine + 16 * (dl + 64 * j)), v = *at;
-                                clear_odd(v);
+                                clear_odd<T>(v);
                                 *at = v;
                             }
                             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -473,14 +516,14 @@ __global__ __launch_bounds__(256, DH == 256 || NT == 4 ? 1 : 2) void paged_attn_
                     }
                     lsum[t] = Num<T>::mfma(ones, pf, lsum[t]);
 #pragma unroll
-                    for (int c = 0; c < CT; c++) o[t][c] = Num<T>::mfma(NT > 1 ? vt[c] : v_tile(c), pf, o[t][c]);
+                    for (int c = 0; c < CT; c++) o[t][c] = Num<T>::mfma(NT > 1 ? vt[c] : v_operand<DH>(mine, lane, c), pf, o[t][c]);
                 }
                 key0 = nkey; pg0 = npg0; pg1 = npg1;
                 if (b + 8 < b_hi) {
                     nkey = block_key(bl, b + 8);
                     npg0 = page_of(nkey);
                     npg1 = page_of(nkey + 16);
-            }
+                }
             }
         }
 
@@ -561,6 +604,192 @@ __global__ __launch_bounds__(256, DH == 256 || NT == 4 ? 1 : 2) void paged_attn_
     }
 }
 
+// ---- many rows: the waves of a workgroup split the rows and share K and V in LDS ----------------------------------------
+
+// Stages of SK keys, K and V, are loaded through registers into one of two LDS buffers while the other is worked on, one barrier
+// per stage; a wave holds NT row tiles for all keys, so nothing has to be merged at the end.  Bound by the vector ALU beside the matrix
+// cores: 32 keys of a row tile are 17 MFMAs of 16 cycles, and 8 exponentials of 16 and about 20 other instructions of 4 per lane.
+template <int DH>
+struct RowsShape {
+    static constexpr int NT = DH == 256 ? 1 : 2, TILE_ROWS = 64 * NT, SHIFT = DH == 256 ? 5 : 6, SK = 1 << SHIFT;
+};
+// Where piece c of a key of K lies: the 16 keys that one operand load reads fall on different banks.
+template <int DH>
+__device__ __forceinline__ int k_piece(int key, int c) {
+    return key * (DH / 8) + (DH == 64 ? c ^ ((key >> 1) & 7) : c ^ (key & 15));
+}
+
+template <class T, int DH>
+__global__ __launch_bounds__(256, DH == 256 ? 1 : 2) void paged_rows_kernel(PagedAttn a) {
+    typedef RowsShape<DH> Shape;
+    constexpr int NT = Shape::NT, SK = Shape::SK, SHIFT = Shape::SHIFT, KS = DH / 32, CT = DH / 16;
+    constexpr int WK = SK / 4, KEYS = 512 / DH, LD = WK / KEYS;              // keys that a wave stages; per load; loads each of K and V
+    constexpr int BUF = 2 * SK * DH * 2;                                    // bytes of a stage
+    extern __shared__ __align__(16) unsigned char stages[];
+    __shared__ int odd_flag[2][4];
+
+    const int kv = a.pages.n_kv_heads, head = (int)(blockIdx.x % (unsigned)kv), x = (int)(blockIdx.x / (unsigned)kv);
+    Place pl;
+    if (!find_place(a, Shape::TILE_ROWS, false, [&](long long) { return (long long)x; }, pl)) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, li = lane & 15;
+    const Request rq = pl.q;
+    const int G = a.group, n_rows = rq.m * G;
+    const int tile = tiles_of(a, rq, Shape::TILE_ROWS) - 1 - __builtin_amdgcn_readfirstlane((int)pl.at);    // those that see the most first
+    int pmin, pmax, wmin, wmax;                                             // positions of the tile's rows and of this wave's
+    tile_span(rq, G, tile, Shape::TILE_ROWS, pmin, pmax);
+    tile_span(rq, G, tile * 4 + wave, 16 * NT, wmin, wmax);
+    const Blocks bl = blocks_of<SHIFT>(a, rq.len, pmin, pmax);
+    const int rho0 = (tile * 4 + wave) * 16 * NT;
+    const bool idle = rho0 >= n_rows;                                       // (a wave without rows helps to load)
+
+    frag_t q[NT][KS];
+    Sight sight[NT];
+#pragma unroll
+    for (int t = 0; t < NT; t++) {
+        const int rho = min(rho0 + t * 16 + li, n_rows - 1), i = rho / G, hq = head * G + (rho - i * G);
+        sight[t] = sight_of(a, rq.len, rq.first + i);
+        const u16 *src = (const u16 *)a.q + (size_t)(rq.row0 + i) * a.q_row + (size_t)hq * DH + 8 * g;
+#pragma unroll
+        for (int k = 0; k < KS; k++) q[t][k] = ld_frag(src + 32 * k);
+    }
+    f32x4 o[NT][CT], lsum[NT];
+    float mref[NT];
+#pragma unroll
+    for (int t = 0; t < NT; t++) {
+        mref[t] = -INFINITY;
+        lsum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < CT; c++) o[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    const frag_t ones = {{Num<T>::kOnes, Num<T>::kOnes, Num<T>::kOnes, Num<T>::kOnes}};
+
+    const u16 *kp = (const u16 *)a.pages.k + (size_t)head * a.pages.head_stride, *vp = (const u16 *)a.pages.v + (size_t)head * a.pages.head_stride;
+    const int32_t *table = a.tables + (size_t)pl.r * a.columns;
+    const int page_mask = (1 << a.page_shift) - 1;
+    const size_t pos_stride = a.pages.pos_stride, page_stride = a.pages.page_stride;
+    const int s_key = lane / (DH / 8), s_ch = lane % (DH / 8);
+    const unsigned s_off = 2u * (s_key * (unsigned)pos_stride + s_ch * 8);
+    auto page_of = [&](int key) -> int {
+        const int id = key < rq.len ? ld_scalar(table, key >> a.page_shift) : -1;
+        return id >= 0 && id < a.pages.n_pages ? id : -1;
+    };
+    // pages of the 16-key tiles of a stage, and the one that holds the keys which this wave stages
+    struct Stage { int key0, page[SK / 16], mine; };
+    auto stage_of = [&](int b) {
+        Stage s;
+        s.key0 = block_key<SHIFT>(bl, b);
+#pragma unroll
+        for (int i = 0; i < SK / 16; i++) s.page[i] = page_of(s.key0 + 16 * i);
+        s.mine = page_of(s.key0 + WK * wave);
+        return s;
+    };
+    frag_t kr[LD], vr[LD];
+    auto load = [&](const Stage &s) {
+        const size_t base = (size_t)max(s.mine, 0) * page_stride + (size_t)((s.key0 + WK * wave) & page_mask) * pos_stride;
+#pragma unroll
+        for (int j = 0; j < LD; j++) kr[j] = ld_at<false>(kp + base + (size_t)(j * KEYS) * pos_stride, s_off);
+#pragma unroll
+        for (int j = 0; j < LD; j++) vr[j] = ld_at<false>(vp + base + (size_t)(j * KEYS) * pos_stride, s_off);
+    };
+    auto store = [&](int buf, bool look) {
+        unsigned char *k0 = stages + buf * BUF, *v0 = k0 + SK * DH * 2;
+        int odd = 0;
+#pragma unroll
+        for (int j = 0; j < LD; j++) {
+            const int key = WK * wave + s_key + j * KEYS;
+            *reinterpret_cast<frag_t *>(k0 + 16 * k_piece<DH>(key, s_ch)) = kr[j];
+            *reinterpret_cast<frag_t *>(v0 + 16 * v_piece<DH>(key, s_ch)) = vr[j];
+            if (look) odd |= has_odd<T>(vr[j]);
+        }
+        if (look) {
+            odd = __any(odd);
+            if (lane == 0) odd_flag[buf][wave] = odd;
+        }
+    };
+    // does every row of the tile see every key of the stage?
+    auto plain_stage = [&](const Stage &s) {
+        bool there = true;
+#pragma unroll
+        for (int i = 0; i < SK / 16; i++) there = there && s.page[i] >= 0;
+        return there && all_seen(a, rq.len, s.key0, SK, pmin, pmax);
+    };
+
+    if (bl.count > 0) {
+        Stage cur = stage_of(0), next = bl.count > 1 ? stage_of(1) : cur;
+        load(cur);
+        bool plain = plain_stage(cur);
+        store(0, !plain);
+        __syncthreads();
+        for (int b = 0; b < bl.count; b++) {
+            const int buf = b & 1;
+            const Stage after = b + 2 < bl.count ? stage_of(b + 2) : next;
+            load(next);                                                     // (behind the last stage once more the same one)
+            const unsigned char *k0 = stages + buf * BUF, *v0 = k0 + SK * DH * 2;
+            const bool dirty = !plain && (odd_flag[buf][0] | odd_flag[buf][1] | odd_flag[buf][2] | odd_flag[buf][3]) != 0;
+#pragma unroll
+            for (int h = 0; h < SK / 32; h++) {
+                const int key0 = cur.key0 + 32 * h, pg0 = cur.page[2 * h], pg1 = cur.page[2 * h + 1];
+                // keys that none of this wave's rows sees
+                const bool none = idle || key0 >= rq.len || (a.causal && key0 > wmax) ||
+                                  (a.window && key0 >= a.sinks && (key0 + 31 <= wmin - a.window || key0 - wmax >= a.window));
+                if (none) continue;
+                const bool all = plain || (pg0 >= 0 && pg1 >= 0 && all_seen(a, rq.len, key0, 32, wmin, wmax));
+                const unsigned char *kb = k0 + 32 * h * DH * 2, *vb = v0 + 32 * h * DH * 2;
+                frag_t kf[2][KS];
+#pragma unroll
+                for (int s = 0; s < 2; s++)
+#pragma unroll
+                    for (int k = 0; k < KS; k++) kf[s][k] = *reinterpret_cast<const frag_t *>(kb + 16 * k_piece<DH>(16 * s + li, 4 * k + g));
+                f32x4 z[NT][2];
+#pragma unroll
+                for (int t = 0; t < NT; t++)
+#pragma unroll
+                    for (int s = 0; s < 2; s++) {
+                        z[t][s] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int k = 0; k < KS; k++) z[t][s] = Num<T>::mfma(kf[s][k], q[t][k], z[t][s]);
+                    }
+                frag_t vt[CT];
+#pragma unroll
+                for (int c = 0; c < CT; c++) vt[c] = v_operand<DH>(vb, lane, c);
+                if (__builtin_expect(dirty, 0))
+#pragma unroll
+                    for (int c = 0; c < CT; c++) clear_odd<T>(vt[c]);
+#pragma unroll
+                for (int t = 0; t < NT; t++) {
+                    if (!all) {
+#pragma unroll
+                        for (int s = 0; s < 2; s++)
+#pragma unroll
+                            for (int e = 0; e < 4; e++) z[t][s][e] = sees(sight[t], key0 + s * 16 + 4 * g + e, s ? pg1 : pg0) ? z[t][s][e] : -INFINITY;
+                    }
+                    const frag_t pf = probabilities<T, CT>(z[t], a.sc, mref[t], lsum[t], o[t]);
+                    if (__builtin_expect(dirty, 0))
+                        add_odd<T, DH>(vb, lane, pf, [&](int key) { return sees(sight[t], key0 + key, key & 16 ? pg1 : pg0); }, o[t]);
+                    lsum[t] = Num<T>::mfma(ones, pf, lsum[t]);
+#pragma unroll
+                    for (int c = 0; c < CT; c++) o[t][c] = Num<T>::mfma(vt[c], pf, o[t][c]);
+                }
+            }
+            plain = plain_stage(next);
+            store(buf ^ 1, !plain);
+            __syncthreads();
+            cur = next;
+            next = after;
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < NT; t++) {
+        const int rho = rho0 + t * 16 + li;
+        if (rho >= n_rows) continue;
+        const int i = rho / G, hq = head * G + (rho - i * G);
+        const float l = lsum[t][0], f = l > 0.f ? 1.0f / l : l == 0.f ? 0.f : l;          // a row that sees nothing is zero
+#pragma unroll
+        for (int c = 0; c < CT; c++)
+            store_out4(a, rq.row0 + i, hq, DH, c * 16 + 4 * g, uint2{Num<T>::pack(o[t][c][0] * f, o[t][c][1] * f), Num<T>::pack(o[t][c][2] * f, o[t][c][3] * f)});
+    }
+}
+
 // Adds the parts of a row in order.  WPR waves per (row, head) - one where there are many rows, which have few parts each, 16
 // where there are few, which have many: the parts' references and sums first, a part per lane, then their O, a part per wave in turn.
 template <class T, int DH, int WPR>
@@ -629,7 +858,15 @@ void launch_nt(const PagedAttn &a, hipStream_t s) {
 }
 
 template <class T, int DH>
+void launch_rows(const PagedAttn &a, hipStream_t s) {
+    constexpr int bytes = 2 * 2 * RowsShape<DH>::SK * DH * 2;
+    allow_lds<paged_rows_kernel<T, DH>>(bytes);
+    paged_rows_kernel<T, DH><<<dim3((unsigned)(a.items * a.pages.n_kv_heads)), 256, bytes, s>>>(a);
+}
+
+template <class T, int DH>
 void launch_dim(const PagedAttn &a, int nt, hipStream_t s) {
+    if (nt == kManyRows) return launch_rows<T, DH>(a, s);
     if (nt == 1) return launch_nt<T, DH, 1>(a, s);
     if (nt == 2 || DH == 256) return launch_nt<T, DH, 2>(a, s);
     if constexpr (DH != 256) launch_nt<T, DH, 4>(a, s);
@@ -648,22 +885,25 @@ inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
 }  // namespace
 
-int paged_attn_tiles(const odb_pages &p, int group, int max_rows) {
-    const long long rows = (long long)max_rows * group;
-    return rows <= 16 ? 1 : rows <= 32 || p.head_dim == 256 ? 2 : 4;
-}
-
-void paged_attn_split(const odb_pages &p, int n, int rows, int group, int nt, long long max_len, int *split, long long *items) {
+void paged_attn_plan(const odb_pages &p, int n, int rows, int group, int max_rows, long long max_len, int *nt, int *split, long long *items) {
+    const long long most = (long long)max_rows * group;
     // Every request has at most one row tile that is not full.
-    const long long tiles = (n < rows ? n : rows) + (long long)rows * group / (16 * nt);
-    const long long blocks = (max_len + 31) / 32;
+    auto tiles = [&](int tile_rows) { return (long long)(n < rows ? n : rows) + (long long)rows * group / tile_rows; };
+    const int many = p.head_dim == 256 ? 64 : 128;
+    if (most >= many && tiles(many) * p.n_kv_heads >= 256) {
+        *nt = kManyRows;
+        *split = 0;
+        *items = tiles(many);
+        return;
+    }
+    *nt = most <= 16 ? 1 : most <= 32 || p.head_dim == 256 ? 2 : 4;
     // One round of workgroups.  Two per CU hide each other's starts and ends where a tile is 16 rows (64 single tokens over 555 MB:
     // 107 us, with one 110, with four 107; two over 985 MB 156, 153, 158); with more rows every cut costs more sums (8 x 32 rows: one
     // 59 us, two 62, four 68).
-    const int aim = (256 * (nt == 1 && p.head_dim != 256 ? 2 : 1) + p.n_kv_heads - 1) / p.n_kv_heads;
+    const int aim = (256 * (*nt == 1 && p.head_dim != 256 ? 2 : 1) + p.n_kv_heads - 1) / p.n_kv_heads;
     // With four row tiles for every workgroup the lengths even out by themselves, and a tile then reads only the keys it sees.
-    *split = tiles >= 4 * aim || blocks <= 2 * kLeastBlocks ? 0 : aim;
-    *items = *split ? *split : tiles;
+    *split = tiles(16 * *nt) >= 4 * aim || (max_len + 31) / 32 <= 2 * kLeastBlocks ? 0 : aim;
+    *items = *split ? *split : tiles(16 * *nt);
 }
 
 size_t paged_attn_workspace(const odb_pages &p, int rows, int heads, int nt, int split) {
@@ -674,7 +914,7 @@ size_t paged_attn_workspace(const odb_pages &p, int rows, int heads, int nt, int
 
 void launch_paged_attention(PagedAttn a, int nt, void *workspace, hipStream_t s) {
     if (a.rows < 1) return;
-    a.tile_rows = nt * 16;
+    a.tile_rows = nt * 16;              // (of the kernel that can split keys)
     if (a.split > 0) {
         const size_t tile_rows = 2 * (size_t)a.split * a.pages.n_kv_heads * nt * 16;
         char *w = (char *)workspace;

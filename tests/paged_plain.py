@@ -118,3 +118,31 @@ def attention(q, k_pages, v_pages, tables, kv_len, rows, first, scale, causal, w
                     big[row, h * group:(h + 1) * group] = (q[row, h * group:(h + 1) * group].abs() @ k.abs().t()).amax(-1) * scale
             row += 1
     return out, size, big
+
+
+def attention_many(q, k_pages, v_pages, tables, kv_len, rows, first, scale, causal, window, sinks):
+    """attention() for many rows of requests whose visible positions hold numbers and lie in pages of the pool: all rows of a head at once."""
+    page, dim = k_pages.shape[2:]
+    group = q.shape[1] // k_pages.shape[1]
+    out, size, big = torch.zeros_like(q), torch.zeros_like(q), torch.zeros(q.shape[:2], dtype=torch.float64)
+    row = 0
+    for r, m in enumerate(rows):
+        length = kv_len[r]
+        if m == 0:
+            continue
+        p = ((length - m if first is None else first[r]) + torch.arange(m))[:, None]
+        key = torch.arange(length)[None, :]
+        seen = torch.ones(m, length, dtype=torch.bool)
+        if causal:
+            seen &= key <= p
+        if window:
+            seen &= ((p - key).abs() < window) | (key < sinks)
+        ids = torch.tensor([int(x) for x in tables[r, :-(-length // page)]], dtype=torch.long)
+        for h in range(q.shape[1]):
+            k, v = (x[ids, h // group].reshape(-1, dim)[:length].double() for x in (k_pages, v_pages))
+            x = q[row:row + m, h]
+            z = torch.softmax((x @ k.t() * scale).masked_fill(~seen, float("-inf")), -1).nan_to_num(0.0)
+            out[row:row + m, h], size[row:row + m, h] = z @ v, z @ v.abs()
+            big[row:row + m, h] = (x.abs() @ k.abs().t()).masked_fill(~seen, 0.0).amax(-1) * scale
+        row += m
+    return out, size, big

@@ -227,10 +227,10 @@ class Requests:
         return B.odb_paged_attention(self.q.cuda(), self.k.cuda(), self.v.cuda(), ints(self.tables), ints(self.lens), cu_rows=cu_rows,
                                      first_pos=None if first is None else ints(first), **kw)
 
-    def check(self, got, first=None, causal=False, window=0, sinks=0, scale=None):
+    def check(self, got, first=None, causal=False, window=0, sinks=0, scale=None, oracle=plain.attention):
         dim, dt = self.q.shape[2], self.q.dtype
         scale = dim ** -0.5 if scale is None else scale
-        want, size, big = plain.attention(self.q.double(), self.k, self.v, self.tables, self.lens, self.rows, first, scale, causal, window, sinks)
+        want, size, big = oracle(self.q.double(), self.k, self.v, self.tables, self.lens, self.rows, first, scale, causal, window, sinks)
         u = half_step(dt)
         # a probability is off by its rounding to the type, u, by that of the score's sum, dim F of sum |q||k| and F more for its
         # product with the scale, and by exp2, 4 F; numerator and denominator both; the sums over the keys add their number times F
@@ -280,6 +280,46 @@ def test_ragged_rows_masks_and_sinks(cache, dim, causal, window, sinks):
     rows, lens = [5, 1, 33, 0, 70, 16], [40, 17, 210, 30, 70, 601]
     rq = Requests(dim + window, rows, lens, 6, 2, dim, cache, 32)
     rq.check(rq.run(causal=causal, window=window, sinks=sinks), causal=causal, window=window, sinks=sinks)
+
+
+MANY = [("f16", 64, 64, 64), ("bf16", 128, 64, 64), ("bf16", 128, 96, 32), ("f16", 256, 40, 40), ("f16", 64, 120, 24)]
+
+
+@pytest.mark.parametrize("cache,dim,heads,kv", MANY)
+@pytest.mark.parametrize("causal,window,sinks", [(False, 0, 0), (True, 0, 0), (True, 33, 5), (False, 100, 70), (True, 1, 0)])
+def test_many_rows(cache, dim, heads, kv, causal, window, sinks):
+    """Calls whose waves split the rows of a tile: row tiles and stages that are not full, requests without rows, lengths of one."""
+    rows, lens = [260, 1, 0, 131, 64], [301, 1, 70, 131, 530]
+    rq = Requests(dim + window + heads, rows, lens, heads, kv, dim, cache, 16)
+    rq.check(rq.run(causal=causal, window=window, sinks=sinks), causal=causal, window=window, sinks=sinks, oracle=plain.attention_many)
+
+
+def test_many_rows_at_given_positions_and_with_hidden_numbers():
+    rows, lens, first = [200, 200, 130], [400, 250, 130], [150, -20, 100]
+    rq = Requests(71, rows, lens, 64, 64, 64, "f16", 32)
+    for causal in (False, True):
+        rq.check(rq.run(first=first, causal=causal), first=first, causal=causal, oracle=plain.attention_many)
+    # a key that half of a tile's rows see holds no number: the others stay as they were
+    clean = rq.run(first=first, causal=True).cpu()
+    page_id, at = int(rq.tables[0, 200 // 32]), 200 % 32
+    for pool in (rq.v, rq.k):
+        keep = pool[page_id, :, at].clone()
+        pool[page_id, :, at] = float("nan")
+        got = rq.run(first=first, causal=True).cpu()
+        assert torch.equal(got[:50], clean[:50]) and torch.isnan(got[50:200]).all() and torch.equal(got[200:], clean[200:])
+        pool[page_id, :, at] = keep
+    # a page outside the pool, in the middle and at the end
+    rq.tables[0, 3], rq.tables[2, 4] = -1, rq.k.shape[0]
+    gone = torch.ones(400, dtype=torch.bool)
+    gone[96:128] = False
+    got = rq.run(first=first, causal=False).cpu()
+    q64, ids = rq.q.double(), torch.tensor(rq.tables[0, :13].astype(np.int64)).clamp(min=0)
+    for h in (0, 63):
+        k, v = (x[ids, h].reshape(-1, 64)[:400][gone].double() for x in (rq.k, rq.v))
+        w = torch.softmax(q64[:200, h] @ k.t() * 0.125, -1)
+        # (bounds as in check(), with the largest sum |q||k| of all rows)
+        off = 2.0 ** -11 + 80 * F * (q64[:200, h].abs() @ k.abs().t()).max() * 0.125 + 8 * F + 400 * F / 4
+        assert ((got[:200, h].double() - w @ v).abs() <= 2.1 * off * (w @ v.abs()) + 2.0 ** -11 * (w @ v).abs() + 1e-7).all()
 
 
 @pytest.mark.parametrize("causal,window,sinks", [(False, 0, 0), (True, 0, 0), (True, 9, 2), (False, 9, 2)])
