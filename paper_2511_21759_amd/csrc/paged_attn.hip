@@ -44,7 +44,9 @@ template <> struct Num<__bf16> {
 // Probabilities are exp2(score - reference) with the reference kShift below the maximum that it was taken from: the binary16
 // form of a probability then keeps all its bits down to 2^-22 of the largest one.  The reference is raised when a score
 // passes it by more than kRaise, so a probability is at most 2^kRaise, which binary16 holds.
-constexpr float kShift = 8.0f, kRaise = 15.0f;
+// As long as a row has seen no key its reference is kNone, lower than any score: sums that are nought then stay so.
+constexpr float kShift = 8.0f, kRaise = 15.0f, kNone = -3.402823466e38f;
+struct Reference { float at = kNone, limit = kNone; };          // in units of log2; limit: the score beyond which it is raised
 
 // ---- which keys -------------------------------------------------------------------------------------------------------
 
@@ -218,28 +220,27 @@ __device__ __forceinline__ void store_out4(const PagedAttn &a, int row, int head
 // with V; the reference is raised, and sums and O rescaled, where a score passes it by too much.  It is common to the four lanes of
 // a row and only has to keep exp2 in range, so after the first blocks that is rare, and the common path has no exchange of lanes.
 template <class T, int CT>
-__device__ __forceinline__ frag_t probabilities(f32x4 (&z)[2], float sc, float &mref, f32x4 &lsum, f32x4 (&o)[CT]) {
+__device__ __forceinline__ frag_t probabilities(f32x4 (&z)[2], float sc, Reference &ref, f32x4 &lsum, f32x4 (&o)[CT]) {
     float top = -INFINITY;
 #pragma unroll
     for (int s = 0; s < 2; s++)
 #pragma unroll
         for (int e = 0; e < 4; e++) top = fmaxf(top, z[s][e]);
-    if (__any(top * sc > mref + kRaise)) {
+    if (__any(top > ref.limit)) {
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
-        const float up = fmaxf(mref, top * sc - kShift);
-        const float f = __builtin_amdgcn_exp2f(mref - (up == -INFINITY ? 0.f : up));
+        const float up = fmaxf(ref.at, top * sc - kShift), f = __builtin_amdgcn_exp2f(ref.at - up);
         lsum *= f;
 #pragma unroll
         for (int c = 0; c < CT; c++) o[c] *= f;
-        mref = up;
+        ref.at = up;
+        ref.limit = (up + kRaise) / sc;
     }
-    const float ref = mref == -INFINITY ? 0.f : mref;
     float p[2][4];
 #pragma unroll
     for (int s = 0; s < 2; s++)
 #pragma unroll
-        for (int e = 0; e < 4; e++) p[s][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[s][e], sc, -ref));
+        for (int e = 0; e < 4; e++) p[s][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[s][e], sc, -ref.at));
     // Probabilities are rounded to the type of V for the matrix cores; the sum that divides them at the end is that of the
     // rounded ones, so what equal rounding errors have in common drops out.
     return frag_t{{Num<T>::pack(p[0][0], p[0][1]), Num<T>::pack(p[0][2], p[0][3]), Num<T>::pack(p[1][0], p[1][1]), Num<T>::pack(p[1][2], p[1][3])}};
@@ -328,6 +329,15 @@ __device__ __forceinline__ Sight sight_of(const PagedAttn &a, int len, int pos) 
 __device__ __forceinline__ bool sees(const Sight &s, int key, int page) {
     return ((int)(page >= 0) & (((int)(key >= s.lo) & (int)(key < s.hi)) | (int)(key < s.stay))) != 0;
 }
+// scores of a 32-key block that a row does not see become -infinity
+__device__ __forceinline__ void hide_unseen(f32x4 (&z)[2], const Sight &sight, int key0, int g, int page0, int page1) {
+    int key = key0 + 4 * g;
+    asm volatile("" : "+v"(key));             // (hidden from the compiler, which else computes the eight keys outside this rare part)
+#pragma unroll
+    for (int s = 0; s < 2; s++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) z[s][e] = sees(sight, key + s * 16 + e, s ? page1 : page0) ? z[s][e] : -INFINITY;
+}
 // is every one of n keys from key0 on visible to every row at positions pmin .. pmax?
 __device__ __forceinline__ bool all_seen(const PagedAttn &a, int len, int key0, int n, int pmin, int pmax) {
     const int last = key0 + n - 1;
@@ -400,11 +410,10 @@ __global__ __launch_bounds__(256, DH == 256 || NT == 4 ? 1 : 2) void paged_attn_
         }
 
         f32x4 o[NT][CT], lsum[NT];
-        float mref[NT];
+        Reference ref[NT];
 #pragma unroll
         for (int t = 0; t < NT; t++) {
-            mref[t] = -INFINITY;
-            lsum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+                lsum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int c = 0; c < CT; c++) o[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
@@ -453,7 +462,6 @@ __global__ __launch_bounds__(256, DH == 256 || NT == 4 ? 1 : 2) void paged_attn_
                 base1 = tile_base(npg1, nkey + 16);
                 // is every key of the block visible to every row of the tile?
                 const bool plain = pg0 >= 0 && pg1 >= 0 && all_seen(a, rq.len, key0, 32, pmin, pmax);
-                auto visible = [&](int t, int key, int page) -> bool { return sees(sight[t], key, page); };
                 f32x4 st[2][2];                                       // scores of this row tile and the next
                 auto scores = [&](int t) {
 #pragma unroll
@@ -494,15 +502,10 @@ __global__ __launch_bounds__(256, DH == 256 || NT == 4 ? 1 : 2) void paged_attn_
                     if (t + 1 < NT) scores(t + 1);
                     if (NT > 1 && t + 2 == NT) load_k(base0, base1, k_next);
                     f32x4 (&z)[2] = st[t & 1];
-                    if (!plain) {
-#pragma unroll
-                        for (int s = 0; s < 2; s++)
-#pragma unroll
-                            for (int e = 0; e < 4; e++) z[s][e] = visible(t, key0 + s * 16 + 4 * g + e, s ? pg1 : pg0) ? z[s][e] : -INFINITY;
-                    }
-                    const frag_t pf = probabilities<T, CT>(z, a.sc, mref[t], lsum[t], o[t]);
+                    if (!plain) hide_unseen(z, sight[t], key0, g, pg0, pg1);
+                    const frag_t pf = probabilities<T, CT>(z, a.sc, ref[t], lsum[t], o[t]);
                     if (__builtin_expect(dirty, 0)) {
-                        add_odd<T, DH>(mine, lane, pf, [&](int key) { return visible(t, key0 + key, key & 16 ? pg1 : pg0); }, o[t]);
+                        add_odd<T, DH>(mine, lane, pf, [&](int key) { return sees(sight[t], key0 + key, key & 16 ? pg1 : pg0); }, o[t]);
                         if (NT == 1) {
                             int dl = lane;
                             asm volatile("" : "+v"(dl));
@@ -534,7 +537,7 @@ __global__ __launch_bounds__(256, DH == 256 || NT == 4 ? 1 : 2) void paged_attn_
         const int eg = (tid >> 4) & 3, el = tid & 15;
 #pragma unroll
         for (int t = 0; t < NT; t++)
-            if (eg == 0) stat[wave][t * 16 + el] = float2{mref[t], lsum[t][0]};
+            if (eg == 0) stat[wave][t * 16 + el] = float2{ref[t].at, lsum[t][0]};
         const long long place = (2ll * x + (b_lo == 0)) * kv + head;
         // parts of the pair: this piece, where it starts, to the one that holds its last block
         const int parts = whole ? 1 : (int)((piece * x + (min(piece, pl.total - piece * x) - left) - b_lo + nb - 1) / piece) - x + 1;
@@ -544,7 +547,7 @@ __global__ __launch_bounds__(256, DH == 256 || NT == 4 ? 1 : 2) void paged_attn_
             {
                 const float2 s0 = stat[0][t * 16 + el], s1 = stat[1][t * 16 + el], s2 = stat[2][t * 16 + el], s3 = stat[3][t * 16 + el];
                 const float top = fmaxf(fmaxf(s0.x, s1.x), fmaxf(s2.x, s3.x));
-                const float f = __builtin_amdgcn_exp2f(mref[t] - (top == -INFINITY ? 0.f : top));
+                const float f = __builtin_amdgcn_exp2f(ref[t].at - top);
                 float *dst = reinterpret_cast<float *>(mine) + el * OSTRIDE + 4 * eg;
 #pragma unroll
                 for (int c = 0; c < CT; c++) *reinterpret_cast<f32x4 *>(dst + c * 16) = o[t][c] * f;
@@ -559,7 +562,7 @@ __global__ __launch_bounds__(256, DH == 256 || NT == 4 ? 1 : 2) void paged_attn_
 #pragma unroll
                 for (int w = 0; w < 4; w++) {
                     const float2 s = stat[w][t * 16 + r];
-                    l += s.y * __builtin_amdgcn_exp2f(s.x - (top == -INFINITY ? 0.f : top));
+                    l += s.y * __builtin_amdgcn_exp2f(s.x - top);
                     const float *src = reinterpret_cast<const float *>(lds + w * WAVE_LDS) + r * OSTRIDE + c;
                     const f32x4 u = *reinterpret_cast<const f32x4 *>(src), v = *reinterpret_cast<const f32x4 *>(src + 4);
 #pragma unroll
@@ -653,10 +656,9 @@ __global__ __launch_bounds__(256, DH == 256 ? 1 : 2) void paged_rows_kernel(Page
         for (int k = 0; k < KS; k++) q[t][k] = ld_frag(src + 32 * k);
     }
     f32x4 o[NT][CT], lsum[NT];
-    float mref[NT];
+    Reference ref[NT];
 #pragma unroll
     for (int t = 0; t < NT; t++) {
-        mref[t] = -INFINITY;
         lsum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int c = 0; c < CT; c++) o[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -757,13 +759,8 @@ __global__ __launch_bounds__(256, DH == 256 ? 1 : 2) void paged_rows_kernel(Page
                     for (int c = 0; c < CT; c++) clear_odd<T>(vt[c]);
 #pragma unroll
                 for (int t = 0; t < NT; t++) {
-                    if (!all) {
-#pragma unroll
-                        for (int s = 0; s < 2; s++)
-#pragma unroll
-                            for (int e = 0; e < 4; e++) z[t][s][e] = sees(sight[t], key0 + s * 16 + 4 * g + e, s ? pg1 : pg0) ? z[t][s][e] : -INFINITY;
-                    }
-                    const frag_t pf = probabilities<T, CT>(z[t], a.sc, mref[t], lsum[t], o[t]);
+                    if (!all) hide_unseen(z[t], sight[t], key0, g, pg0, pg1);
+                    const frag_t pf = probabilities<T, CT>(z[t], a.sc, ref[t], lsum[t], o[t]);
                     if (__builtin_expect(dirty, 0))
                         add_odd<T, DH>(vb, lane, pf, [&](int key) { return sees(sight[t], key0 + key, key & 16 ? pg1 : pg0); }, o[t]);
                     lsum[t] = Num<T>::mfma(ones, pf, lsum[t]);
@@ -813,7 +810,6 @@ __global__ __launch_bounds__(WPR == 16 ? 1024 : 256) void paged_join_kernel(Page
         for (int p = lane; p < parts; p += 64) top = fmaxf(top, a.ml[place(p)].x);
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-        if (top == -INFINITY) top = 0.f;
         for (int p = lane; p < parts; p += 64) {
             const float2 s = a.ml[place(p)];
             total += s.y * __builtin_amdgcn_exp2f(s.x - top);
