@@ -109,6 +109,8 @@ __device__ __forceinline__ void tile_span(const Request &q, int group, int tile,
 
 // ---- which work: every workgroup works it out for itself from the lengths ---------------------------------------------
 
+constexpr int NW = 4;                    // waves of a workgroup
+
 struct Place { Request q; int r; long long at, total; };
 
 __device__ __forceinline__ long long uniform(long long x) {
@@ -123,6 +125,10 @@ __device__ __forceinline__ int tiles_of(const PagedAttn &a, const Request &q, in
 __device__ __forceinline__ int request_blocks(const PagedAttn &a, const Request &q) {
     return max(1, blocks_of(a, q.len, q.first, q.first + q.m - 1).count);
 }
+// A pair of request and row tile stands in the list with kPairCost places in front of those of its blocks: its queries, its first
+// loads and its sums at the end take about as long as that many blocks (64 single tokens of 17 to 16384 positions: 97 us with 6,
+// 98 with 8, 103 with 16, 107 without).
+constexpr int kPairCost = 6;
 
 // The requests' weights - row tiles, times blocks where keys are split - lie behind each other; finds the request that holds
 // item pick(total) and the item's offset inside it.  False if there is none.  Up to 64 requests every wave does it alone.
@@ -131,7 +137,7 @@ __device__ __forceinline__ bool find_place(const PagedAttn &a, int tile_rows, bo
     const int lane = threadIdx.x & 63;
     auto weigh = [&](const Request &q) -> long long {
         const int tiles = tiles_of(a, q, tile_rows);
-        return a.split && tiles ? (long long)tiles * request_blocks(a, q) : tiles;
+        return a.split && tiles ? (long long)tiles * (request_blocks(a, q) + kPairCost) : tiles;
     };
     auto scan64 = [&](long long v) -> long long {
 #pragma unroll
@@ -157,30 +163,32 @@ __device__ __forceinline__ bool find_place(const PagedAttn &a, int tile_rows, bo
         p.q.row0 = __builtin_amdgcn_readlane(q.row0, p.r);
         return true;
     }
-    __shared__ long long sums[4], found_at;
+    __shared__ long long sums[NW], found_at;
     __shared__ int found;
     const int t = threadIdx.x, wave = t >> 6;
     if (t == 0) found = -1;
     p.total = 0;
     if (need_total) {
         long long v = 0;
-        for (int r = t; r < a.n; r += 256) v += weigh(request_of(a, r));
+        for (int r = t; r < a.n; r += 64 * NW) v += weigh(request_of(a, r));
         v = scan64(v);
         if (lane == 63) sums[wave] = v;
         __syncthreads();
-        p.total = uniform(sums[0] + sums[1] + sums[2] + sums[3]);
+        v = 0;
+        for (int w = 0; w < NW; w++) v += sums[w];
+        p.total = uniform(v);
         __syncthreads();
         if (pick(p.total) >= p.total) return false;
     }
     const long long x = pick(p.total);
     long long carry = 0;
-    for (int r0 = 0; r0 < a.n && carry <= x; r0 += 256) {
+    for (int r0 = 0; r0 < a.n && carry <= x; r0 += 64 * NW) {
         const int r = r0 + t;
         const long long v = r < a.n ? weigh(request_of(a, r)) : 0, end0 = scan64(v);
         if (lane == 63) sums[wave] = end0;
         __syncthreads();
         long long end = carry + end0;
-        for (int w = 0; w < 4; w++) {
+        for (int w = 0; w < NW; w++) {
             if (w < wave) end += sums[w];
             carry += sums[w];
         }
@@ -348,24 +356,26 @@ __device__ __forceinline__ bool all_seen(const PagedAttn &a, int len, int key0, 
 
 // With keys split (a.split workgroups per K/V head), the blocks of all (request, row tile) pairs lie behind each other and every
 // workgroup takes an equal piece of that list, wherever it starts and ends: all finish together, however ragged the lengths are.
+// (A pair whose blocks all lie behind a piece's end is left to the next piece.)
 // A pair that lies inside one piece is finished there; of the others each piece leaves its sums (reference, sum, O), which
 // paged_join_kernel adds in order.  A piece has at most one pair that it does not start and one that it does not end, so two
 // places per workgroup hold them: 2 w + 1 for a pair that starts in it, 2 w for one that started before.
-constexpr int kLeastBlocks = 8;          // of a piece: two per wave; shorter ones cost more in sums than they save
+// Places of a piece at least: 32 single tokens of 20 to 4000 positions, 28 heads over 4, take 18 us with 12, 19 with 16, 21 with 10.
+constexpr int kLeastPiece = 12;
 
 template <class T, int DH, int NT>
-__global__ __launch_bounds__(256, DH == 256 || NT == 4 ? 1 : 2) void paged_attn_kernel(PagedAttn a) {
+__global__ __launch_bounds__(64 * NW, DH == 256 || NT == 4 ? 1 : 2) void paged_attn_kernel(PagedAttn a) {
     constexpr int KS = DH / 32, CT = DH / 16, VL = DH / 16;      // k-steps of S, channel tiles of O, V loads of a lane per block
     constexpr int KEYS = 1024 / DH * 8 / 16;                     // keys per V load of a wave: 64 lanes * 8 channels / DH
     constexpr int OSTRIDE = DH + 4, WAVE_LDS = 16 * OSTRIDE * 4; // a wave's 32 x DH block of V, later its 16 x DH tile of O in 32 bits
     constexpr int TILE_ROWS = NT * 16;
     static_assert(32 * DH * 2 <= WAVE_LDS && KEYS * VL == 32, "V block");
-    __shared__ __align__(16) unsigned char lds[4 * WAVE_LDS];
-    __shared__ float2 stat[4][TILE_ROWS];
+    __shared__ __align__(16) unsigned char lds[NW * WAVE_LDS];
+    __shared__ float2 stat[NW][TILE_ROWS];
 
     const int kv = a.pages.n_kv_heads, head = (int)(blockIdx.x % (unsigned)kv), x = (int)(blockIdx.x / (unsigned)kv);
     const bool split = a.split > 0;
-    auto piece_of = [&](long long total) { return max((long long)kLeastBlocks, (total + a.split - 1) / max(a.split, 1)); };
+    auto piece_of = [&](long long total) { return max((long long)kLeastPiece, (total + a.split - 1) / max(a.split, 1)); };
     Place pl;
     if (!find_place(a, TILE_ROWS, split, [&](long long total) { return split ? piece_of(total) * x : (long long)x; }, pl)) return;
 
@@ -380,220 +390,227 @@ __global__ __launch_bounds__(256, DH == 256 || NT == 4 ? 1 : 2) void paged_attn_
     const frag_t ones = {{Num<T>::kOnes, Num<T>::kOnes, Num<T>::kOnes, Num<T>::kOnes}};
     Request rq = pl.q;
     int request = pl.r, tiles = tiles_of(a, rq, TILE_ROWS), nb = split ? request_blocks(a, rq) : 1;
-    int tile = __builtin_amdgcn_readfirstlane((int)(pl.at / nb)), b_lo = __builtin_amdgcn_readfirstlane((int)(pl.at - (long long)tile * nb));
-    // blocks of this piece that are left
+    // place in the pair's part of the list where this piece starts
+    const int cost = split ? kPairCost : 0;
+    int tile = __builtin_amdgcn_readfirstlane((int)(pl.at / (nb + cost))), at = __builtin_amdgcn_readfirstlane((int)(pl.at - (long long)tile * (nb + cost)));
+    // places of this piece that are left
     const long long piece = piece_of(pl.total);
     long long left = split ? min(piece, pl.total - piece * x) : 1;
     if (!split) tile = tiles - 1 - tile;                          // the last rows of a causal request see the most: first
 
     for (;;) {
-        const int n_rows = rq.m * G, rho0 = tile * TILE_ROWS;
-        int ql = lane;
-        asm volatile("" : "+v"(ql));
-        int pmin, pmax;
-        tile_span(rq, G, tile, TILE_ROWS, pmin, pmax);
-        const Blocks bl = split ? blocks_of(a, rq.len, rq.first, rq.first + rq.m - 1) : blocks_of(a, rq.len, pmin, pmax);
-        const int b_end = split ? (int)min((long long)nb, b_lo + left) : 1;       // in units of the list
-        const int b_hi = split ? min(b_end, bl.count) : bl.count;
-        const bool whole = b_lo == 0 && b_end == nb;
+        const int end = split ? (int)min((long long)nb + cost, at + left) : 1;
+        const int b_lo = max(0, at - cost), b_end = max(0, end - cost);
+        if (b_end > b_lo) {
+            const int n_rows = rq.m * G, rho0 = tile * TILE_ROWS;
+            int ql = lane;
+            asm volatile("" : "+v"(ql));
+            int pmin, pmax;
+            tile_span(rq, G, tile, TILE_ROWS, pmin, pmax);
+            const Blocks bl = split ? blocks_of(a, rq.len, rq.first, rq.first + rq.m - 1) : blocks_of(a, rq.len, pmin, pmax);
+            const int b_hi = split ? min(b_end, bl.count) : bl.count;
+            const bool whole = b_lo == 0 && b_end == nb;
 
-        // queries of the tile, in operand order; rows behind the last repeat it and are not written
-        frag_t q[NT][KS];
-        Sight sight[NT];                                          // of the lane's row of each tile
+            // queries of the tile, in operand order; rows behind the last repeat it and are not written
+            frag_t q[NT][KS];
+            Sight sight[NT];                                          // of the lane's row of each tile
 #pragma unroll
-        for (int t = 0; t < NT; t++) {
-            const int rho = min(rho0 + t * 16 + (ql & 15), n_rows - 1), i = rho / G, hq = head * G + (rho - i * G);
-            sight[t] = sight_of(a, rq.len, rq.first + i);
-            const u16 *src = (const u16 *)a.q + (size_t)(rq.row0 + i) * a.q_row + (size_t)hq * DH + 8 * (ql >> 4);
+            for (int t = 0; t < NT; t++) {
+                const int rho = min(rho0 + t * 16 + (ql & 15), n_rows - 1), i = rho / G, hq = head * G + (rho - i * G);
+                sight[t] = sight_of(a, rq.len, rq.first + i);
+                const u16 *src = (const u16 *)a.q + (size_t)(rq.row0 + i) * a.q_row + (size_t)hq * DH + 8 * (ql >> 4);
 #pragma unroll
-            for (int k = 0; k < KS; k++) q[t][k] = ld_frag(src + 32 * k);
-        }
-
-        f32x4 o[NT][CT], lsum[NT];
-        Reference ref[NT];
-#pragma unroll
-        for (int t = 0; t < NT; t++) {
-                lsum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int c = 0; c < CT; c++) o[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
-        }
-
-        // page of each 16-key tile of a block: -1 where no key of the tile is visible or the table names no page of the pool
-        const int32_t *table = a.tables + (size_t)request * a.columns;
-        auto page_of = [&](int key) -> int {
-            const int id = key < rq.len ? ld_scalar(table, key >> a.page_shift) : -1;
-            return id >= 0 && id < a.pages.n_pages ? id : -1;
-        };
-        frag_t kf[2][KS], vf[VL];
-        auto tile_base = [&](int page, int key) -> size_t { return (size_t)max(page, 0) * page_stride + (size_t)(key & page_mask) * pos_stride; };
-        auto load_k = [&](size_t base0, size_t base1, unsigned off) {
-#pragma unroll
-            for (int k = 0; k < KS; k++) kf[0][k] = ld_at<NT == 1>(kp + base0 + 32 * k, off);     // (a request with one row tile reads its K/V once)
-#pragma unroll
-            for (int k = 0; k < KS; k++) kf[1][k] = ld_at<NT == 1>(kp + base1 + 32 * k, off);
-        };
-        auto load_v = [&](size_t base0, size_t base1, unsigned off) {
-#pragma unroll
-            for (int j = 0; j < VL; j++) vf[j] = ld_at<NT == 1>(vp + (j < VL / 2 ? base0 : base1) + (size_t)(j % (VL / 2) * KEYS) * pos_stride, off);
-        };
-
-        int b = b_lo + wave;
-        if (b < b_hi) {
-            int key0 = block_key(bl, b), pg0 = page_of(key0), pg1 = page_of(key0 + 16), nkey = 0, npg0 = -1, npg1 = -1;
-            size_t base0 = tile_base(pg0, key0), base1 = tile_base(pg1, key0 + 16);
-            load_k(base0, base1, k_off);
-            __builtin_amdgcn_sched_barrier(0);                    // K first here too, or the loop's first wait would be for both
-            load_v(base0, base1, v_off);
-#pragma unroll
-            for (int t = 0; t < NT; t++)
-#pragma unroll
-                for (int k = 0; k < KS; k++) asm volatile("" ::"v"(q[t][k].w[0]));     // waits for the queries here, not in the loop
-            if (b + 4 < b_hi) {
-                nkey = block_key(bl, b + 4);
-                npg0 = page_of(nkey);
-                npg1 = page_of(nkey + 16);
+                for (int k = 0; k < KS; k++) q[t][k] = ld_frag(src + 32 * k);
             }
-            for (; b < b_hi; b += 4) {
-                // Behind the last block the loads are made all the same, of 16 bytes for all lanes: with no branch around them
-                // the wait for K need not be one for V too.
-                const bool more = b + 4 < b_hi;
-                const unsigned k_next = more ? k_off : 0, v_next = more ? v_off : 0;
-                base0 = tile_base(npg0, nkey);
-                base1 = tile_base(npg1, nkey + 16);
-                // is every key of the block visible to every row of the tile?
-                const bool plain = pg0 >= 0 && pg1 >= 0 && all_seen(a, rq.len, key0, 32, pmin, pmax);
-                f32x4 st[2][2];                                       // scores of this row tile and the next
-                auto scores = [&](int t) {
-#pragma unroll
-                    for (int s = 0; s < 2; s++) {
-                        f32x4 z = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                        for (int k = 0; k < KS; k++) z = Num<T>::mfma(kf[s][k], q[t][k], z);
-                        st[t & 1][s] = z;
-                    }
-                };
-                scores(0);
-                if (NT == 1) load_k(base0, base1, k_next);            // the registers of K are free for the next block
-                bool dirty = false;
-                if (!plain) {
-                    int odd = 0;
-#pragma unroll
-                    for (int j = 0; j < VL; j++) odd |= has_odd<T>(vf[j]);
-                    dirty = __any(odd);
-                }
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-#pragma unroll
-                for (int j = 0; j < VL; j++)
-                    *reinterpret_cast<frag_t *>(mine + 16 * v_piece<DH>(v_key + j % (8 / KEYS) * KEYS, v_ch) + j / (8 / KEYS) * (8 * DH * 2)) = vf[j];
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                load_v(base0, base1, v_next);
-                frag_t vt[NT > 1 ? CT : 1];                           // held for several row tiles
-                if (NT > 1) {
-#pragma unroll
-                    for (int c = 0; c < CT; c++) vt[c] = v_operand<DH>(mine, lane, c);
-                    if (__builtin_expect(dirty, 0))
-#pragma unroll
-                        for (int c = 0; c < CT; c++) clear_odd<T>(vt[c]);
-                }
 
-                // row tiles one after the other, the next one's scores under way in the matrix cores while this one's probabilities are made
+            f32x4 o[NT][CT], lsum[NT];
+            Reference ref[NT];
 #pragma unroll
-                for (int t = 0; t < NT; t++) {
-                    if (t + 1 < NT) scores(t + 1);
-                    if (NT > 1 && t + 2 == NT) load_k(base0, base1, k_next);
-                    f32x4 (&z)[2] = st[t & 1];
-                    if (!plain) hide_unseen(z, sight[t], key0, g, pg0, pg1);
-                    const frag_t pf = probabilities<T, CT>(z, a.sc, ref[t], lsum[t], o[t]);
-                    if (__builtin_expect(dirty, 0)) {
-                        add_odd<T, DH>(mine, lane, pf, [&](int key) { return sees(sight[t], key0 + key, key & 16 ? pg1 : pg0); }, o[t]);
-                        if (NT == 1) {
-                            int dl = lane;
-                            asm volatile("" : "+v"(dl));
-                            for (int j = 0; j < VL; j++) {
-                                frag_t *at = reinterpret_cast<frag_t *>(mine + 16 * (dl + 64 * j)), v = *at;
-                                clear_odd<T>(v);
-                                *at = v;
-                            }
-                            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                        }
-                    }
-                    lsum[t] = Num<T>::mfma(ones, pf, lsum[t]);
+            for (int t = 0; t < NT; t++) {
+                    lsum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int c = 0; c < CT; c++) o[t][c] = Num<T>::mfma(NT > 1 ? vt[c] : v_operand<DH>(mine, lane, c), pf, o[t][c]);
-                }
-                key0 = nkey; pg0 = npg0; pg1 = npg1;
-                if (b + 8 < b_hi) {
-                    nkey = block_key(bl, b + 8);
+                for (int c = 0; c < CT; c++) o[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+            }
+
+            // page of each 16-key tile of a block: -1 where no key of the tile is visible or the table names no page of the pool
+            const int32_t *table = a.tables + (size_t)request * a.columns;
+            auto page_of = [&](int key) -> int {
+                const int id = key < rq.len ? ld_scalar(table, key >> a.page_shift) : -1;
+                return id >= 0 && id < a.pages.n_pages ? id : -1;
+            };
+            frag_t kf[2][KS], vf[VL];
+            auto tile_base = [&](int page, int key) -> size_t { return (size_t)max(page, 0) * page_stride + (size_t)(key & page_mask) * pos_stride; };
+            auto load_k = [&](size_t base0, size_t base1, unsigned off) {
+#pragma unroll
+                for (int k = 0; k < KS; k++) kf[0][k] = ld_at<NT == 1>(kp + base0 + 32 * k, off);     // (a request with one row tile reads its K/V once)
+#pragma unroll
+                for (int k = 0; k < KS; k++) kf[1][k] = ld_at<NT == 1>(kp + base1 + 32 * k, off);
+            };
+            auto load_v = [&](size_t base0, size_t base1, unsigned off) {
+#pragma unroll
+                for (int j = 0; j < VL; j++) vf[j] = ld_at<NT == 1>(vp + (j < VL / 2 ? base0 : base1) + (size_t)(j % (VL / 2) * KEYS) * pos_stride, off);
+            };
+
+            int b = b_lo + wave;
+            if (b < b_hi) {
+                int key0 = block_key(bl, b), pg0 = page_of(key0), pg1 = page_of(key0 + 16), nkey = 0, npg0 = -1, npg1 = -1;
+                size_t base0 = tile_base(pg0, key0), base1 = tile_base(pg1, key0 + 16);
+                load_k(base0, base1, k_off);
+                __builtin_amdgcn_sched_barrier(0);                    // K first here too, or the loop's first wait would be for both
+                load_v(base0, base1, v_off);
+#pragma unroll
+                for (int t = 0; t < NT; t++)
+#pragma unroll
+                    for (int k = 0; k < KS; k++) asm volatile("" ::"v"(q[t][k].w[0]));     // waits for the queries here, not in the loop
+                if (b + NW < b_hi) {
+                    nkey = block_key(bl, b + NW);
                     npg0 = page_of(nkey);
                     npg1 = page_of(nkey + 16);
                 }
-            }
-        }
-
-        // ---- the four waves' sums become one
-        // (the thread's number is hidden from the compiler, which else keeps addresses of this part in registers through the loop)
-        int tid = threadIdx.x;
-        asm volatile("" : "+v"(tid));
-        const int eg = (tid >> 4) & 3, el = tid & 15;
+                for (; b < b_hi; b += NW) {
+                    // Behind the last block the loads are made all the same, of 16 bytes for all lanes: with no branch around them
+                    // the wait for K need not be one for V too.
+                    const bool more = b + NW < b_hi;
+                    const unsigned k_next = more ? k_off : 0, v_next = more ? v_off : 0;
+                    base0 = tile_base(npg0, nkey);
+                    base1 = tile_base(npg1, nkey + 16);
+                    // is every key of the block visible to every row of the tile?
+                    const bool plain = pg0 >= 0 && pg1 >= 0 && all_seen(a, rq.len, key0, 32, pmin, pmax);
+                    f32x4 st[2][2];                                       // scores of this row tile and the next
+                    auto scores = [&](int t) {
 #pragma unroll
-        for (int t = 0; t < NT; t++)
-            if (eg == 0) stat[wave][t * 16 + el] = float2{ref[t].at, lsum[t][0]};
-        const long long place = (2ll * x + (b_lo == 0)) * kv + head;
-        // parts of the pair: this piece, where it starts, to the one that holds its last block
-        const int parts = whole ? 1 : (int)((piece * x + (min(piece, pl.total - piece * x) - left) - b_lo + nb - 1) / piece) - x + 1;
+                        for (int s = 0; s < 2; s++) {
+                            f32x4 z = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int t = 0; t < NT; t++) {
-            __syncthreads();
-            {
-                const float2 s0 = stat[0][t * 16 + el], s1 = stat[1][t * 16 + el], s2 = stat[2][t * 16 + el], s3 = stat[3][t * 16 + el];
-                const float top = fmaxf(fmaxf(s0.x, s1.x), fmaxf(s2.x, s3.x));
-                const float f = __builtin_amdgcn_exp2f(ref[t].at - top);
-                float *dst = reinterpret_cast<float *>(mine) + el * OSTRIDE + 4 * eg;
+                            for (int k = 0; k < KS; k++) z = Num<T>::mfma(kf[s][k], q[t][k], z);
+                            st[t & 1][s] = z;
+                        }
+                    };
+                    scores(0);
+                    if (NT == 1) load_k(base0, base1, k_next);            // the registers of K are free for the next block
+                    bool dirty = false;
+                    if (!plain) {
+                        int odd = 0;
 #pragma unroll
-                for (int c = 0; c < CT; c++) *reinterpret_cast<f32x4 *>(dst + c * 16) = o[t][c] * f;
-            }
-            __syncthreads();
-            for (int e = tid; e < 2 * DH; e += 256) {
-                const int r = e / (DH / 8), c = (e % (DH / 8)) * 8, rho = rho0 + t * 16 + r;
-                if (rho >= n_rows) continue;
-                float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, top = -INFINITY, l = 0.f;
-#pragma unroll
-                for (int w = 0; w < 4; w++) top = fmaxf(top, stat[w][t * 16 + r].x);
-#pragma unroll
-                for (int w = 0; w < 4; w++) {
-                    const float2 s = stat[w][t * 16 + r];
-                    l += s.y * __builtin_amdgcn_exp2f(s.x - top);
-                    const float *src = reinterpret_cast<const float *>(lds + w * WAVE_LDS) + r * OSTRIDE + c;
-                    const f32x4 u = *reinterpret_cast<const f32x4 *>(src), v = *reinterpret_cast<const f32x4 *>(src + 4);
-#pragma unroll
-                    for (int i = 0; i < 4; i++) { sum[i] += u[i]; sum[4 + i] += v[i]; }
-                }
-                const int i = rho / G, hq = head * G + (rho - i * G), row = rq.row0 + i;
-                if (!whole) {
-                    float *dst = a.partial + ((size_t)place * TILE_ROWS + t * 16 + r) * DH + c;
-                    *reinterpret_cast<f32x4 *>(dst) = f32x4{sum[0], sum[1], sum[2], sum[3]};
-                    *reinterpret_cast<f32x4 *>(dst + 4) = f32x4{sum[4], sum[5], sum[6], sum[7]};
-                    if (c == 0) {
-                        a.ml[place * TILE_ROWS + t * 16 + r] = float2{top, l};
-                        if (b_lo == 0) a.where[(size_t)row * a.heads + hq] = int2{x, parts * 64 + t * 16 + r};
+                        for (int j = 0; j < VL; j++) odd |= has_odd<T>(vf[j]);
+                        dirty = __any(odd);
                     }
-                } else {
-                    // a row that sees nothing is zero
-                    const float f = l > 0.f ? 1.0f / l : l == 0.f ? 0.f : l;
-                    uint4 v;
-                    v.x = Num<T>::pack(sum[0] * f, sum[1] * f);
-                    v.y = Num<T>::pack(sum[2] * f, sum[3] * f);
-                    v.z = Num<T>::pack(sum[4] * f, sum[5] * f);
-                    v.w = Num<T>::pack(sum[6] * f, sum[7] * f);
-                    store_out8(a, row, hq, DH, c, v);
-                    if (split && c == 0) a.where[(size_t)row * a.heads + hq] = int2{x, 0};
+                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+                    for (int j = 0; j < VL; j++)
+                        *reinterpret_cast<frag_t *>(mine + 16 * v_piece<DH>(v_key + j % (8 / KEYS) * KEYS, v_ch) + j / (8 / KEYS) * (8 * DH * 2)) = vf[j];
+                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                    load_v(base0, base1, v_next);
+                    frag_t vt[NT > 1 ? CT : 1];                           // held for several row tiles
+                    if (NT > 1) {
+#pragma unroll
+                        for (int c = 0; c < CT; c++) vt[c] = v_operand<DH>(mine, lane, c);
+                        if (__builtin_expect(dirty, 0))
+#pragma unroll
+                            for (int c = 0; c < CT; c++) clear_odd<T>(vt[c]);
+                    }
+
+                    // row tiles one after the other, the next one's scores under way in the matrix cores while this one's probabilities are made
+#pragma unroll
+                    for (int t = 0; t < NT; t++) {
+                        if (t + 1 < NT) scores(t + 1);
+                        if (NT > 1 && t + 2 == NT) load_k(base0, base1, k_next);
+                        f32x4 (&z)[2] = st[t & 1];
+                        if (!plain) hide_unseen(z, sight[t], key0, g, pg0, pg1);
+                        const frag_t pf = probabilities<T, CT>(z, a.sc, ref[t], lsum[t], o[t]);
+                        if (__builtin_expect(dirty, 0)) {
+                            add_odd<T, DH>(mine, lane, pf, [&](int key) { return sees(sight[t], key0 + key, key & 16 ? pg1 : pg0); }, o[t]);
+                            if (NT == 1) {
+                                int dl = lane;
+                                asm volatile("" : "+v"(dl));
+                                for (int j = 0; j < VL; j++) {
+                                    frag_t *at = reinterpret_cast<frag_t *>(mine + 16 * (dl + 64 * j)), v = *at;
+                                    clear_odd<T>(v);
+                                    *at = v;
+                                }
+                                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                            }
+                        }
+                        lsum[t] = Num<T>::mfma(ones, pf, lsum[t]);
+#pragma unroll
+                        for (int c = 0; c < CT; c++) o[t][c] = Num<T>::mfma(NT > 1 ? vt[c] : v_operand<DH>(mine, lane, c), pf, o[t][c]);
+                    }
+                    key0 = nkey; pg0 = npg0; pg1 = npg1;
+                    if (b + 2 * NW < b_hi) {
+                        nkey = block_key(bl, b + 2 * NW);
+                        npg0 = page_of(nkey);
+                        npg1 = page_of(nkey + 16);
+                    }
                 }
             }
+
+            // ---- the waves' sums become one
+            // (the thread's number is hidden from the compiler, which else keeps addresses of this part in registers through the loop)
+            int tid = threadIdx.x;
+            asm volatile("" : "+v"(tid));
+            const int eg = (tid >> 4) & 3, el = tid & 15;
+#pragma unroll
+            for (int t = 0; t < NT; t++)
+                if (eg == 0) stat[wave][t * 16 + el] = float2{ref[t].at, lsum[t][0]};
+            const long long place = (2ll * x + (b_lo == 0)) * kv + head;
+            // parts of the pair: this piece, where it starts, to the one that holds its last block
+            const int parts = whole ? 1 : (int)((piece * x + (min(piece, pl.total - piece * x) - left) - at + cost + nb - 1) / piece) - x + 1;
+#pragma unroll
+            for (int t = 0; t < NT; t++) {
+                __syncthreads();
+                {
+                    float top = kNone;
+#pragma unroll
+                    for (int w = 0; w < NW; w++) top = fmaxf(top, stat[w][t * 16 + el].x);
+                    const float f = __builtin_amdgcn_exp2f(ref[t].at - top);
+                    float *dst = reinterpret_cast<float *>(mine) + el * OSTRIDE + 4 * eg;
+#pragma unroll
+                    for (int c = 0; c < CT; c++) *reinterpret_cast<f32x4 *>(dst + c * 16) = o[t][c] * f;
+                }
+                __syncthreads();
+                for (int e = tid; e < 2 * DH; e += 64 * NW) {
+                    const int r = e / (DH / 8), c = (e % (DH / 8)) * 8, rho = rho0 + t * 16 + r;
+                    if (rho >= n_rows) continue;
+                    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, top = -INFINITY, l = 0.f;
+#pragma unroll
+                    for (int w = 0; w < NW; w++) top = fmaxf(top, stat[w][t * 16 + r].x);
+#pragma unroll
+                    for (int w = 0; w < NW; w++) {
+                        const float2 s = stat[w][t * 16 + r];
+                        l += s.y * __builtin_amdgcn_exp2f(s.x - top);
+                        const float *src = reinterpret_cast<const float *>(lds + w * WAVE_LDS) + r * OSTRIDE + c;
+                        const f32x4 u = *reinterpret_cast<const f32x4 *>(src), v = *reinterpret_cast<const f32x4 *>(src + 4);
+#pragma unroll
+                        for (int i = 0; i < 4; i++) { sum[i] += u[i]; sum[4 + i] += v[i]; }
+                    }
+                    const int i = rho / G, hq = head * G + (rho - i * G), row = rq.row0 + i;
+                    if (!whole) {
+                        float *dst = a.partial + ((size_t)place * TILE_ROWS + t * 16 + r) * DH + c;
+                        *reinterpret_cast<f32x4 *>(dst) = f32x4{sum[0], sum[1], sum[2], sum[3]};
+                        *reinterpret_cast<f32x4 *>(dst + 4) = f32x4{sum[4], sum[5], sum[6], sum[7]};
+                        if (c == 0) {
+                            a.ml[place * TILE_ROWS + t * 16 + r] = float2{top, l};
+                            if (b_lo == 0) a.where[(size_t)row * a.heads + hq] = int2{x, parts * 64 + t * 16 + r};
+                        }
+                    } else {
+                        // a row that sees nothing is zero
+                        const float f = l > 0.f ? 1.0f / l : l == 0.f ? 0.f : l;
+                        uint4 v;
+                        v.x = Num<T>::pack(sum[0] * f, sum[1] * f);
+                        v.y = Num<T>::pack(sum[2] * f, sum[3] * f);
+                        v.z = Num<T>::pack(sum[4] * f, sum[5] * f);
+                        v.w = Num<T>::pack(sum[6] * f, sum[7] * f);
+                        store_out8(a, row, hq, DH, c, v);
+                        if (split && c == 0) a.where[(size_t)row * a.heads + hq] = int2{x, 0};
+                    }
+                }
+            }
+            __syncthreads();
         }
         if (!split) return;
-        left -= b_end - b_lo;
+        left -= end - at;
         if (left <= 0) return;
-        b_lo = 0;
+        at = 0;
         if (++tile == tiles) {
             do {
                 if (++request >= a.n) return;
@@ -603,7 +620,6 @@ __global__ __launch_bounds__(256, DH == 256 || NT == 4 ? 1 : 2) void paged_attn_
             tile = 0;
             nb = request_blocks(a, rq);
         }
-        __syncthreads();
     }
 }
 
@@ -787,8 +803,7 @@ __global__ __launch_bounds__(256, DH == 256 ? 1 : 2) void paged_rows_kernel(Page
     }
 }
 
-// Adds the parts of a row in order.  WPR waves per (row, head) - one where there are many rows, which have few parts each, 16
-// where there are few, which have many: the parts' references and sums first, a part per lane, then their O, a part per wave in turn.
+// Adds the parts of a row in order, WPR waves per (row, head) with a part each in turn.  Rows that belong to no request are left alone.
 template <class T, int DH, int WPR>
 __global__ __launch_bounds__(WPR == 16 ? 1024 : 256) void paged_join_kernel(PagedAttn a) {
     constexpr int V = DH / 64, ROWS = WPR == 16 ? 1 : 4 / WPR;          // channels of a lane, rows of a workgroup
@@ -796,10 +811,12 @@ __global__ __launch_bounds__(WPR == 16 ? 1024 : 256) void paged_join_kernel(Page
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = wave / WPR, w = wave % WPR;
     const long long unit = (long long)blockIdx.x * ROWS + sub;
     const int row = (int)(unit / a.heads), hq = (int)(unit % a.heads);
-    // rows that belong to no request are left alone
-    bool mine = row < a.rows && (!a.cu_rows || (row >= a.cu_rows[0] && row < a.cu_rows[a.n]));
     int2 at{0, 0};
-    if (mine) at = a.where[(size_t)row * a.heads + hq];
+    bool mine = row < a.rows;
+    if (mine) {
+        at = a.where[(size_t)row * a.heads + hq];
+        mine = !a.cu_rows || (row >= a.cu_rows[0] && row < a.cu_rows[a.n]);
+    }
     const int parts = at.y >> 6, r = at.y & 63, kv = a.pages.n_kv_heads, head = hq / a.group;
     mine = mine && parts > 1 && r < a.tile_rows && at.x >= 0 && (long long)at.x + parts <= a.split;
     auto place = [&](int p) { return ((size_t)(2ll * (at.x + p) + (p == 0)) * kv + head) * a.tile_rows + r; };
@@ -807,17 +824,38 @@ __global__ __launch_bounds__(WPR == 16 ? 1024 : 256) void paged_join_kernel(Page
 #pragma unroll
     for (int i = 0; i < V; i++) acc[i] = 0.f;
     if (mine) {
-        for (int p = lane; p < parts; p += 64) top = fmaxf(top, a.ml[place(p)].x);
+        // the first parts' O are on their way while the references and sums are looked at, a part per lane
+        constexpr int AHEAD = 4;
+        float first[AHEAD][V];
+#pragma unroll
+        for (int j = 0; j < AHEAD; j++) {
+            const float *src = a.partial + place(min(w + j * WPR, parts - 1)) * DH + lane * V;
+#pragma unroll
+            for (int i = 0; i < V; i++) first[j][i] = src[i];
+        }
+        const float2 s0 = a.ml[place(min(lane, parts - 1))];
+        top = s0.x;
+        for (int p = lane + 64; p < parts; p += 64) top = fmaxf(top, a.ml[place(p)].x);
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-        for (int p = lane; p < parts; p += 64) {
+        const float f0 = __builtin_amdgcn_exp2f(s0.x - top);
+        if (lane < parts) total = s0.y * f0;
+        for (int p = lane + 64; p < parts; p += 64) {
             const float2 s = a.ml[place(p)];
             total += s.y * __builtin_amdgcn_exp2f(s.x - top);
         }
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o);
-#pragma unroll 8
-        for (int p = w; p < parts; p += WPR) {
+#pragma unroll
+        for (int j = 0; j < AHEAD; j++) {
+            const int p = w + j * WPR;
+            const float f = __shfl(f0, p);                             // (p < 64)
+            if (p < parts)
+#pragma unroll
+                for (int i = 0; i < V; i++) acc[i] += first[j][i] * f;
+        }
+#pragma unroll 4
+        for (int p = w + AHEAD * WPR; p < parts; p += WPR) {
             const size_t e = place(p);
             const float f = __builtin_amdgcn_exp2f(a.ml[e].x - top);
             const float *src = a.partial + e * DH + lane * V;
@@ -831,7 +869,7 @@ __global__ __launch_bounds__(WPR == 16 ? 1024 : 256) void paged_join_kernel(Page
     const int c = (w * 64 + lane) * 8;
     if (!mine || c >= DH) return;
     float out[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll
+#pragma unroll 4
     for (int k = 0; k < WPR; k++)
 #pragma unroll
         for (int i = 0; i < 8; i++) out[i] += sums[sub][k][c + i];
@@ -848,8 +886,10 @@ template <class T, int DH, int NT>
 void launch_nt(const PagedAttn &a, hipStream_t s) {
     paged_attn_kernel<T, DH, NT><<<dim3((unsigned)(a.items * a.pages.n_kv_heads)), 256, 0, s>>>(a);
     if (!a.split) return;
-    const long long units = (long long)a.rows * a.heads;
-    if (units <= 512) paged_join_kernel<T, DH, 16><<<dim3((unsigned)units), 1024, 0, s>>>(a);
+    // parts of a row, where the lengths are equal
+    const long long units = (long long)a.rows * a.heads, parts = a.split / max(1ll, min((long long)a.n, (long long)a.rows));
+    if (parts > 16) paged_join_kernel<T, DH, 16><<<dim3((unsigned)units), 1024, 0, s>>>(a);
+    else if (parts > 4) paged_join_kernel<T, DH, 4><<<dim3((unsigned)units), 256, 0, s>>>(a);
     else paged_join_kernel<T, DH, 1><<<dim3((unsigned)((units + 3) / 4)), 256, 0, s>>>(a);
 }
 
@@ -898,7 +938,7 @@ void paged_attn_plan(const odb_pages &p, int n, int rows, int group, int max_row
     // 59 us, two 62, four 68).
     const int aim = (256 * (*nt == 1 && p.head_dim != 256 ? 2 : 1) + p.n_kv_heads - 1) / p.n_kv_heads;
     // With four row tiles for every workgroup the lengths even out by themselves, and a tile then reads only the keys it sees.
-    *split = tiles(16 * *nt) >= 4 * aim || (max_len + 31) / 32 <= 2 * kLeastBlocks ? 0 : aim;
+    *split = tiles(16 * *nt) >= 4 * aim || (max_len + 31) / 32 <= 16 ? 0 : aim;
     *items = *split ? *split : tiles(16 * *nt);
 }
 
