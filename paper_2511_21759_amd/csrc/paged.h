@@ -16,8 +16,9 @@ struct PageTables {
     int32_t *tables, *free_pages;
     const int32_t *n_free;
     int32_t *len, *cu_rows, *slots, *positions, *state;
+    int row_groups, page_groups;        // workgroups for the rows, and for each of pages given back and pages taken
 };
-void launch_page_tables(const PageTables &a, hipStream_t s);
+void launch_page_tables(PageTables a, hipStream_t s);
 
 // Angle per position of every pair, in turns: hi + lo (two doubles, so that far positions keep their fraction)
 constexpr int kMaxRotPairs = 128;

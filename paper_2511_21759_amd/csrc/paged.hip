@@ -1,5 +1,6 @@
 // Operators around a paged K/V cache: page tables and slot maps, the table of rotary angles, and the pass that norms and
 // turns queries and keys and stores keys and values in their pages.  Attention over the pages is in paged_attn.hip.
+#include "launch.h"
 #include "paged.h"
 
 namespace odb {
@@ -9,25 +10,6 @@ namespace odb {
 // Sums of these kernels saturate at 2^30 (more than any pool or row buffer has), so that lengths of any size cannot wrap them.
 constexpr unsigned kSat = 1u << 30;
 __device__ __forceinline__ unsigned sat_add(unsigned a, unsigned b) { return min(a + b, kSat); }
-
-// Inclusive scan of one value per thread over the 256 threads of a workgroup, on top of `carry`; `carry` becomes the total.
-__device__ __forceinline__ unsigned scan256(unsigned v, unsigned &carry, unsigned *wave_sums) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const unsigned up = __shfl_up(v, o);
-        if (lane >= o) v = sat_add(v, up);
-    }
-    if (lane == 63) wave_sums[wave] = v;
-    __syncthreads();
-    unsigned before = carry;
-    for (int w = 0; w < 4; w++) {
-        if (w < wave) before = sat_add(before, wave_sums[w]);
-        carry = sat_add(carry, wave_sums[w]);
-    }
-    __syncthreads();
-    return sat_add(before, v);
-}
 
 // index of the request whose part of the inclusive sums holds item i (sums[n - 1] > i)
 __device__ __forceinline__ int owner(const unsigned *sums, int n, unsigned i) {
@@ -41,12 +23,11 @@ __device__ __forceinline__ int owner(const unsigned *sums, int n, unsigned i) {
 
 // Pages that a request holds, needs, and whether its wanted length can be named by its table at all.
 struct PageNeed { unsigned had, need; int held, wanted; bool fits; };
-__device__ __forceinline__ PageNeed page_need(const PageTables &a, int r) {
+__device__ __forceinline__ PageNeed page_need(const PageTables &a, int held, int wanted) {
     PageNeed p;
-    const long long most = (long long)a.columns << a.page_shift;
-    const int top = (int)min(most, 0x7fffffffll), mask = (1 << a.page_shift) - 1;
-    p.held = min(max(a.held[r], 0), top);
-    p.wanted = a.wanted[r];
+    const int top = a.columns << a.page_shift, mask = (1 << a.page_shift) - 1;      // (at most 2^30)
+    p.held = min(max(held, 0), top);
+    p.wanted = wanted;
     p.fits = p.wanted >= 0 && p.wanted <= top;
     p.had = ((unsigned)p.held + mask) >> a.page_shift;
     p.need = p.fits ? ((unsigned)p.wanted + mask) >> a.page_shift : p.had;
@@ -54,32 +35,81 @@ __device__ __forceinline__ PageNeed page_need(const PageTables &a, int r) {
 }
 
 // One launch, no exchange between workgroups: each of them computes the three running sums over the requests (pages taken,
-// pages given back, rows) for itself - at most 4096 requests, so at most 16 per thread - and then does its share of
-// the items: rows, pages given back, pages taken.  What one workgroup writes no other reads: entries behind a request's held
-// pages are not looked up in the table but derived from the stack, and the stack's new top from the tables of those that gave back.
-// A second call with the same inputs therefore writes the same values again. 
+// pages given back, rows) for itself - a thread takes up to 16 neighbouring requests, then one scan over the threads - and keeps
+// them in LDS with what else the items need; then it does its share of one kind of items: rows, pages given back, pages taken.  What one
+// workgroup writes no other reads: entries behind a request's held pages are not looked up in the table but derived from the
+// stack, and the stack's new top from the tables of those that gave back.  A second call with the same inputs therefore writes the
+// same values again.
 __global__ __launch_bounds__(256) void page_tables_kernel(PageTables a) {
     extern __shared__ unsigned lds[];
-    __shared__ unsigned wave_sums[4], granted_top[4];
-    unsigned *taken = lds, *given = lds + a.n, *rows = lds + 2 * a.n;
-    const int t = threadIdx.x;
-    unsigned c_take = 0, c_give = 0, c_rows = 0;
-    for (int r0 = 0; r0 < a.n; r0 += 256) {
-        const int r = r0 + t;
-        unsigned take = 0, give = 0, count = 0;
-        if (r < a.n) {
-            const PageNeed p = page_need(a, r);
-            take = p.need > p.had ? p.need - p.had : 0;
-            give = p.had > p.need ? p.had - p.need : 0;
-            const int c = a.count ? a.count[r] : p.fits ? p.wanted - p.held : 0;
-            count = min((unsigned)max(c, 0), (unsigned)a.rows_cap);
-        }
-        const unsigned st = scan256(take, c_take, wave_sums), sg = scan256(give, c_give, wave_sums), sr = scan256(count, c_rows, wave_sums);
-        if (r < a.n) { taken[r] = st; given[r] = sg; rows[r] = sr; }
+    __shared__ unsigned wave_sums[4][3], tops[4], misses[4];
+    unsigned *taken = lds, *given = lds + a.n, *rows = lds + 2 * a.n, *had = lds + 3 * a.n, *need = lds + 4 * a.n;
+    int *first = (int *)(lds + 5 * a.n), *length = (int *)(lds + 6 * a.n);
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    const int per = (a.n + 255) / 256, r0 = t * per, r1 = min(a.n, r0 + per);
+    const unsigned n_free = (unsigned)min(max(*a.n_free, 0), a.n_pages);
+
+    // the inputs first, neighbouring threads reading neighbouring requests: one latency for all of them
+    int *in_held = (int *)had, *in_wanted = (int *)need, *in_count = (int *)rows;
+#pragma unroll 4
+    for (int r = t; r < a.n; r += 256) {
+        const int h = a.held[r], w = a.wanted[r], c = a.count ? a.count[r] : 0, f = a.first ? a.first[r] : 0;
+        in_held[r] = h;
+        in_wanted[r] = w;
+        in_count[r] = c;
+        first[r] = f;
     }
     __syncthreads();
-    const unsigned n_free = (unsigned)min(max(*a.n_free, 0), a.n_pages), have = n_free + c_give;
-    const unsigned n_rows = min(c_rows, (unsigned)a.rows_cap);
+    unsigned sum[3] = {0, 0, 0};
+    for (int r = r0; r < r1; r++) {
+        const PageNeed p = page_need(a, in_held[r], in_wanted[r]);
+        const int c = a.count ? in_count[r] : p.fits ? p.wanted - p.held : 0;
+        taken[r] = sum[0] = sat_add(sum[0], p.need > p.had ? p.need - p.had : 0);
+        given[r] = sum[1] = sat_add(sum[1], p.had > p.need ? p.had - p.need : 0);
+        rows[r] = sum[2] = sat_add(sum[2], min((unsigned)max(c, 0), (unsigned)a.rows_cap));
+        had[r] = p.had;
+        need[r] = p.need;
+        if (!a.first) first[r] = p.held;
+        length[r] = p.fits ? p.wanted : ~p.held;                   // (a length that cannot be: the request is refused)
+    }
+    unsigned before[3], total[3] = {0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 3; i++) {
+        unsigned v = sum[i];
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const unsigned up = __shfl_up(v, o);
+            if (lane >= o) v = sat_add(v, up);
+        }
+        if (lane == 63) wave_sums[wave][i] = v;
+        before[i] = __shfl_up(v, 1);
+        if (lane == 0) before[i] = 0;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 3; i++)
+        for (int w = 0; w < 4; w++) {
+            if (w < wave) before[i] = sat_add(before[i], wave_sums[w][i]);
+            total[i] = sat_add(total[i], wave_sums[w][i]);
+        }
+    const unsigned have = n_free + total[1], n_rows = min(total[2], (unsigned)a.rows_cap);
+    unsigned refused = 0, most = 0;
+    for (int r = r0; r < r1; r++) {
+        taken[r] = sat_add(taken[r], before[0]);
+        given[r] = sat_add(given[r], before[1]);
+        rows[r] = sat_add(rows[r], before[2]);
+        // pages of a request behind the first refused one are not granted either: the sums only rise
+        const bool takes = need[r] > had[r], ok = length[r] >= 0 && (!takes || taken[r] <= have);
+        const int held = length[r] < 0 ? ~length[r] : ok ? 0 : page_need(a, a.held[r], 0).held;
+        length[r] = ok ? length[r] : held;
+        refused += !ok;
+        if (ok && takes) most = max(most, taken[r]);
+        if (blockIdx.x == 0) {
+            a.len[r] = length[r];
+            a.cu_rows[r + 1] = (int)min(rows[r], (unsigned)a.rows_cap);
+        }
+    }
+    __syncthreads();
 
     // The page that takes number i off the stack: those given back in this call lie on top.
     auto taken_page = [&](unsigned i) -> int {
@@ -87,74 +117,70 @@ __global__ __launch_bounds__(256) void page_tables_kernel(PageTables a) {
         if (at < n_free) return a.free_pages[at];
         const unsigned g = at - n_free;
         const int r = owner(given, a.n, g);
-        const unsigned mine = g - (r ? given[r - 1] : 0);
-        return a.tables[(size_t)r * a.columns + page_need(a, r).need + mine];
+        return a.tables[(size_t)r * a.columns + need[r] + (g - (r ? given[r - 1] : 0))];
     };
-    auto granted = [&](int r, const PageNeed &p) { return p.fits && (p.need <= p.had || taken[r] <= have); };
-
-    // rows: position and slot
-    const unsigned step = gridDim.x * 256, first = blockIdx.x * 256 + t;
-    for (unsigned i = first; i < n_rows; i += step) {
-        const int r = owner(rows, a.n, i);
-        const PageNeed p = page_need(a, r);
-        const bool ok = granted(r, p);
-        const int len = ok ? p.wanted : p.held;
-        const long long pos = (long long)(a.first ? a.first[r] : p.held) + (i - (r ? rows[r - 1] : 0));
-        int slot = -1;
-        if (pos >= 0 && pos < len) {
-            const unsigned j = (unsigned)pos >> a.page_shift;
-            const int page = j < p.had ? a.tables[(size_t)r * a.columns + j] : taken_page((r ? taken[r - 1] : 0) + (j - p.had));
-            if (page >= 0 && page < a.n_pages) slot = (page << a.page_shift) + ((int)pos & ((1 << a.page_shift) - 1));
+    // rows: position and slot, four neighbouring ones per thread, which mostly share their request and often their page
+    const int role = (int)blockIdx.x < a.row_groups ? 0 : (int)blockIdx.x < a.row_groups + a.page_groups ? 1 : 2;
+    const unsigned step = (role ? a.page_groups : a.row_groups) * 256, item0 = (blockIdx.x - (role ? a.row_groups + (role - 1) * a.page_groups : 0)) * 256 + t;
+    for (unsigned i0 = role == 0 ? item0 * 4 : n_rows; i0 < n_rows; i0 += step * 4) {
+        int r = owner(rows, a.n, i0), page = -1;
+        long long page_at = -1;                                    // r and page number that `page` was looked up for
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            const unsigned i = i0 + k;
+            if (i >= n_rows) break;
+            while (rows[r] <= i) r++;
+            const long long pos = (long long)first[r] + (i - (r ? rows[r - 1] : 0));
+            int slot = -1;
+            if (pos >= 0 && pos < length[r]) {
+                const unsigned j = (unsigned)pos >> a.page_shift;
+                const long long key = (long long)r << 32 | j;
+                if (key != page_at) {
+                    page = j < had[r] ? a.tables[(size_t)r * a.columns + j] : taken_page((r ? taken[r - 1] : 0) + (j - had[r]));
+                    page_at = key;
+                }
+                if (page >= 0 && page < a.n_pages) slot = (page << a.page_shift) + ((int)pos & ((1 << a.page_shift) - 1));
+            }
+            a.slots[i] = slot;
+            a.positions[i] = (int)min(pos, 0x7fffffffll);
         }
-        a.slots[i] = slot;
-        a.positions[i] = (int)min(pos, 0x7fffffffll);
     }
     // pages given back go on the stack
-    for (unsigned g = first; g < c_give; g += step) {
+    for (unsigned g = role == 1 ? item0 : total[1]; g < total[1]; g += step) {
         const int r = owner(given, a.n, g);
-        const unsigned mine = g - (r ? given[r - 1] : 0);
-        if (n_free + g < (unsigned)a.n_pages) a.free_pages[n_free + g] = a.tables[(size_t)r * a.columns + page_need(a, r).need + mine];
+        if (n_free + g < (unsigned)a.n_pages) a.free_pages[n_free + g] = a.tables[(size_t)r * a.columns + need[r] + (g - (r ? given[r - 1] : 0))];
     }
-    // pages taken go into the tables (those of requests behind the first refused one are not granted: the sums only rise)
-    for (unsigned i = first; i < min(c_take, have); i += step) {
+    // pages taken go into the tables
+    for (unsigned i = role == 2 ? item0 : total[0]; i < min(total[0], have); i += step) {
         const int r = owner(taken, a.n, i);
         if (taken[r] > have) break;
-        const unsigned mine = i - (r ? taken[r - 1] : 0);
-        a.tables[(size_t)r * a.columns + page_need(a, r).had + mine] = taken_page(i);
+        a.tables[(size_t)r * a.columns + had[r] + (i - (r ? taken[r - 1] : 0))] = taken_page(i);
     }
     if (blockIdx.x) return;
-    unsigned refused = 0, most = 0;
-    for (int r = t; r < a.n; r += 256) {
-        const PageNeed p = page_need(a, r);
-        const bool ok = granted(r, p);
-        a.len[r] = ok ? p.wanted : p.held;
-        a.cu_rows[r + 1] = (int)min(rows[r], (unsigned)a.rows_cap);
-        if (!ok) refused++;
-        else if (p.need > p.had) most = max(most, taken[r]);
-    }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) {
         refused += __shfl_xor(refused, o);
         most = max(most, __shfl_xor(most, o));
     }
-    if ((t & 63) == 0) { wave_sums[t >> 6] = refused; granted_top[t >> 6] = most; }
+    if (lane == 0) { misses[wave] = refused; tops[wave] = most; }
     __syncthreads();
     if (t == 0) {
-        refused = wave_sums[0] + wave_sums[1] + wave_sums[2] + wave_sums[3];
-        most = max(max(granted_top[0], granted_top[1]), max(granted_top[2], granted_top[3]));
+        most = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
         a.cu_rows[0] = 0;
         a.state[0] = (int)min(have - most, (unsigned)a.n_pages);
         a.state[1] = (int)most;
-        a.state[2] = (int)c_give;
-        a.state[3] = (int)refused;
+        a.state[2] = (int)total[1];
+        a.state[3] = (int)(misses[0] + misses[1] + misses[2] + misses[3]);
     }
 }
 
-void launch_page_tables(const PageTables &a, hipStream_t s) {
-    // a workgroup per 256 rows up to two per CU; more would only repeat the sums
-    const int wanted = a.rows_cap / 256 + 1;
-    const int grid = wanted < 512 ? wanted : 512;
-    page_tables_kernel<<<dim3(grid), 256, (size_t)a.n * 12, s>>>(a);
+void launch_page_tables(PageTables a, hipStream_t s) {
+    // four rows per thread up to two workgroups per CU (more would only repeat the sums), and one thread for every eight requests'
+    // pages; the kinds of items are done beside each other, since each is a chain of dependent reads
+    a.row_groups = a.rows_cap / 1024 + 1 < 512 ? a.rows_cap / 1024 + 1 : 512;
+    a.page_groups = a.n / 32 + 1;
+    allow_lds<page_tables_kernel>(kMaxRequests * 28);
+    page_tables_kernel<<<dim3(a.row_groups + 2 * a.page_groups), 256, a.n * 28, s>>>(a);
 }
 
 // ---- rotary angles --------------------------------------------------------------------------------------------------
@@ -179,19 +205,32 @@ __device__ __forceinline__ void turn_sincos(double r, double &c, double &s) {
 }
 
 // The angle is counted in turns, p * (hi + lo), and its whole turns are dropped before anything is rounded to fewer bits, so a
-// position of 2^22 has the same error as the first.  One pair per thread, pairs of a position beside each other: stores of 512
-// contiguous bytes per wave.
+// position of 2^22 has the same error as the first.  A thread computes one pair at every eighth position that way and turns on
+// from there by the pair's own angle, seven times in 64 bits (an error of 7 * 2^-52 at most): 14 operations of 64 bits for an entry
+// and not 36.  Pairs of a position lie beside each other: stores of 512 contiguous bytes per wave.
+constexpr int kAngleRun = 8;
 __global__ __launch_bounds__(256) void rope_angles_kernel(RopeTable a) {
-    const unsigned i = blockIdx.x * 256u + threadIdx.x, pos = i / (unsigned)a.pairs, j = i - pos * a.pairs;
-    if (pos >= (unsigned)a.n_pos) return;
-    const double p = (double)pos, hi = a.hi[j], r = fma(p, hi, -rint(p * hi)) + p * a.lo[j];
-    double c, s;
+    const unsigned i = blockIdx.x * 256u + threadIdx.x, run = i / (unsigned)a.pairs, j = i - run * a.pairs;
+    const int p0 = (int)run * kAngleRun;
+    if (p0 >= a.n_pos) return;
+    const double p = (double)p0, hi = a.hi[j], lo = a.lo[j], r = fma(p, hi, -rint(p * hi)) + p * lo, one = (hi - rint(hi)) + lo;
+    double c, s, dc, ds;
     turn_sincos(r - rint(r), c, s);
-    *reinterpret_cast<float2 *>(a.table + 2 * (size_t)i) = float2{(float)(c * a.magnitude), (float)(s * a.magnitude)};
+    turn_sincos(one, dc, ds);
+    c *= a.magnitude;
+    s *= a.magnitude;
+    float *out = a.table + 2 * ((size_t)p0 * a.pairs + j);
+    const int n = min(kAngleRun, a.n_pos - p0);
+    for (int k = 0; k < n; k++) {
+        *reinterpret_cast<float2 *>(out + 2 * (size_t)k * a.pairs) = float2{(float)c, (float)s};
+        const double u = fma(c, dc, -(s * ds)), w = fma(s, dc, c * ds);
+        c = u;
+        s = w;
+    }
 }
 
 void launch_rope_angles(const RopeTable &a, hipStream_t s) {
-    const long long total = (long long)a.n_pos * a.pairs;          // at most 2^22 * 2^7
+    const long long total = ((long long)a.n_pos + kAngleRun - 1) / kAngleRun * a.pairs;          // at most 2^19 * 2^7
     rope_angles_kernel<<<dim3((unsigned)((total + 255) / 256)), 256, 0, s>>>(a);
 }
 

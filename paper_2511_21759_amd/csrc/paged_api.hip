@@ -112,7 +112,7 @@ int odb_page_tables(const int32_t *held, const int32_t *wanted, int n, int page_
             if (overlap(writes[i], writes[j])) return fail(ODB_E_INVALID_ARG, "%s: two buffers that are written overlap", who);
     }
     launch_page_tables(PageTables{held, wanted, row_first, row_count, n, page_shift(page_size), columns, n_pages, rows_cap, tables, free_pages, n_free, len,
-                                  cu_rows, slots, positions, state}, (hipStream_t)stream);
+                                  cu_rows, slots, positions, state, 0, 0}, (hipStream_t)stream);
     HIP_TRY(hipGetLastError());
     return ODB_OK;
 }
