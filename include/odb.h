@@ -521,6 +521,41 @@ int odb_paged_attention(const odb_attention *a, const odb_pages *pages, void *st
 /* Bytes of workspace that the call needs (fields that are device buffers are not read, workspace is ignored), or a negative error code. */
 long long odb_paged_attention_workspace(const odb_attention *a, const odb_pages *pages);
 
+/* The model's forward over paged K/V: n requests of different lengths, b rows each, in one pass.  Row i of request r is the token
+ * tokens[r][i] at position positions[r * b + i]; its K and V go to the pages (slots, as odb_qk_norm_rope stores them), and it attends
+ * in both directions to positions 0 .. kv_len[r] - 1 of its request as the pages then hold them: the rows' own and those that
+ * earlier calls stored.  With b the whole sequence it is the cache refresh of one or more requests (odb_prefill), with a block's
+ * rows at first_pos[r] a decode step (odb_block_step with one draft) whose requests need neither the same length nor the same
+ * block; the block's K/V in the pages are then those of this step.  odb_page_tables makes slots and positions from row_first =
+ * first_pos and row_count = b; rows that pad a request have position and slot -1 and mean nothing in the outputs.
+ * Inside the pages a head's K has the channel order of an interleaved rotation (channel j of the model at 2j, j + head_dim / 2 at
+ * 2j + 1).
+ *   tokens      dev int32 [n, b]; first_pos, kv_len dev int32 [n]; tables dev int32 [n, columns]; positions, slots dev int32 [n * b]
+ *   table       dev float [n_pos, head_dim / 2, 2] as odb_rope_table writes it (base: the model's rope_base)
+ *   layer0      the first layer's pool, binary16, n_heads heads; those of the next layers lie layer_stride elements further each
+ *   skip        rows of each request in front of those that conf and argmax are written for (a prompt's)
+ *   conf, argmax   dev float / int32 [n, b - skip]; both NULL: only K/V are wanted
+ *   unmask      dev uint8 [n, b] or NULL: the acceptance of odb_block_step with threshold tau, for b <= 256 and skip 0
+ *   max_len     upper bound of kv_len as for odb_paged_attention
+ * Uses the model's scratch (see the conventions above).  Asynchronous on `stream`.  Errors: ODB_E_INVALID_ARG for NULL inputs,
+ * n * b outside [1, 65536], pools that do not fit the model, and what odb_paged_attention refuses. */
+typedef struct {
+    const int32_t *tokens;
+    int n, b;
+    const int32_t *first_pos, *kv_len, *tables;
+    int columns;
+    const int32_t *positions, *slots;
+    const float *table;
+    int n_pos;
+    long long layer_stride;
+    int skip, max_len;
+    float tau;
+    float *conf;
+    int32_t *argmax;
+    uint8_t *unmask;
+} odb_paged_rows;
+int odb_step_paged(odb_model *m, const odb_paged_rows *rows, const odb_pages *layer0, void *stream);
+
 /* Copies cached K (kv = 0, post-RoPE, logical channel order) or V (kv = 1) of
  * positions pos0 .. pos0+n-1 of one sequence and layer to host memory as
  * float [n, n_heads, head_dim].  Synchronous (device-wide). */

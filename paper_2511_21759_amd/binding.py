@@ -26,7 +26,7 @@ SYMBOLS = (
     "odb_predict_length", "odb_accept_jump", "odb_block_step_shared", "odb_block_step_static",
     "odb_block_step_shared_rows", "odb_block_step_shared_logits", "odb_cache_truncate", "odb_generate",
     "odb_speculative_jump", "odb_page_tables", "odb_rope_table", "odb_qk_norm_rope", "odb_paged_attention",
-    "odb_paged_attention_workspace",
+    "odb_paged_attention_workspace", "odb_step_paged",
 )
 
 KERNEL_CLASSES = ("gemm_qkv", "attention", "gemm_o", "gemm_gate_up", "gemm_down", "gemm_lm_head", "rmsnorm")
@@ -101,6 +101,14 @@ class odb_attention(ctypes.Structure):
                 ("workspace_bytes", ctypes.c_size_t)]
 
 
+class odb_paged_rows(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_void_p), ("n", ctypes.c_int), ("b", ctypes.c_int), ("first_pos", ctypes.c_void_p),
+                ("kv_len", ctypes.c_void_p), ("tables", ctypes.c_void_p), ("columns", ctypes.c_int), ("positions", ctypes.c_void_p),
+                ("slots", ctypes.c_void_p), ("table", ctypes.c_void_p), ("n_pos", ctypes.c_int), ("layer_stride", ctypes.c_longlong),
+                ("skip", ctypes.c_int), ("max_len", ctypes.c_int), ("tau", ctypes.c_float), ("conf", ctypes.c_void_p),
+                ("argmax", ctypes.c_void_p), ("unmask", ctypes.c_void_p)]
+
+
 EVENT_KINDS = ("refresh", "step", "shared")
 
 _lib = None
@@ -153,6 +161,7 @@ def lib() -> ctypes.CDLL:
     L.odb_paged_attention.argtypes = [vp, vp, vp]
     L.odb_paged_attention_workspace.argtypes = [vp, vp]
     L.odb_paged_attention_workspace.restype = ctypes.c_longlong
+    L.odb_step_paged.argtypes = [vp, vp, vp, vp]
     L.odb_strerror.argtypes = [ci]
     L.odb_strerror.restype = ctypes.c_char_p
     L.odb_last_error.restype = ctypes.c_char_p
@@ -611,6 +620,32 @@ def odb_paged_attention(q, k_pages, v_pages, tables, kv_len, *, causal: bool, cu
         a = _PACK_ATTENTION(*fields, workspace.data_ptr(), workspace.numel())
     _on(index, lib().odb_paged_attention, a, pages)
     return out
+
+
+def odb_step_paged(model: int, tokens, k_pages, v_pages, tables, first_pos, kv_len, positions, slots, table, tau: Optional[float] = None,
+                   skip: int = 0, head: bool = True, max_len: int = 0):
+    """tokens int32 [n, b]; k_pages, v_pages float16 [n_layers, n_pages, n_heads, page_size, head_dim]; tables int32 [n, columns];
+    first_pos, kv_len int32 [n]; positions, slots int32 [n * b]; table float32 [n_pos, head_dim / 2, 2] -> (conf f32, argmax int32,
+    each [n, b - skip], unmask uint8 [n, b] or None): unmask with a threshold tau only; all None with head=False."""
+    torch = _torch or _load_torch()
+    index, i32 = tokens.get_device(), torch.int32
+    n, b = tokens.shape
+    if k_pages.dim() != 5 or k_pages.shape != v_pages.shape or k_pages.stride() != v_pages.stride() or k_pages.get_device() != index:
+        raise TypeError("k_pages and v_pages must be [n_layers, n_pages, n_heads, page_size, head_dim] with the same strides, on the device of the others")
+    if table.dtype is not torch.float32 or table.dim() != 3 or tuple(table.shape[1:]) != (k_pages.shape[4] // 2, 2) or table.get_device() != index or not table.is_contiguous():
+        raise TypeError("table must be a contiguous float32 tensor [n_pos, head_dim / 2, 2] on the device of the others")
+    if tables.dim() != 2:
+        _not_ints("tables", "[n, columns]")
+    conf = argmax = unmask = None
+    if head:
+        conf, argmax = tokens.new_empty((n, b - skip), dtype=torch.float32), tokens.new_empty((n, b - skip))
+        unmask = None if tau is None else tokens.new_empty((n, b), dtype=torch.uint8)
+    r = odb_paged_rows(_ints("tokens", tokens, (n, b), index, i32), n, b, _ints("first_pos", first_pos, (n,), index, i32),
+                       _ints("kv_len", kv_len, (n,), index, i32), _ints("tables", tables, (n, tables.shape[1]), index, i32), tables.shape[1],
+                       _ints("positions", positions, (n * b,), index, i32), _ints("slots", slots, (n * b,), index, i32), table.data_ptr(), table.shape[0],
+                       k_pages.stride(0), skip, max_len, 0.0 if tau is None else tau, *(None if t is None else t.data_ptr() for t in (conf, argmax, unmask)))
+    _on(index, lib().odb_step_paged, model, ctypes.byref(r), _pages(k_pages[0], v_pages[0]))
+    return conf, argmax, unmask
 
 
 def odb_set_option(model: int, option: int, value: int) -> None:

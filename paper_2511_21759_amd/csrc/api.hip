@@ -1,5 +1,6 @@
 // C ABI of the library (include/odb.h): argument validation, memory, and the
 // sequence of kernel launches that make up the prefill and the block step.
+#include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
 #include <string.h>
@@ -11,6 +12,7 @@
 #include "choose.h"
 #include "errors.h"
 #include "model.h"
+#include "paged.h"
 
 using namespace odb;
 
@@ -1070,6 +1072,97 @@ int odb_block_step_static(odb_model *m, const odb_cache *c, const int32_t *draft
     int rc = static_scratch_ptr(m->m.device, &base);      // a table look-up after model creation
     if (rc) return rc;
     return step_impl(m, c, drafts_dev, block_off, b, S, tau, conf_dev, argmax_dev, unmask_dev, nullptr, stream, base);
+}
+
+// The stack over paged K/V: rows of requests of different lengths, dense.  QKV leaves 32-bit rows, which are turned and stored in the
+// pages in one pass (Q and K in the interleaved channel order of the projection's weights, whose scores are the same); attention
+// over the pages hands its rows to O in operand order.
+int odb_step_paged(odb_model *mh, const odb_paged_rows *args, const odb_pages *layer0, void *stream) {
+    const char *who = "step_paged";
+    if (!mh || !args || !layer0) return fail(ODB_E_INVALID_ARG, "%s: NULL argument", who);
+    Model &m = mh->m;
+    const odb_config &cfg = m.cfg;
+    const odb_paged_rows &r = *args;
+    const int d = cfg.d_model, H = cfg.n_heads, dh = cfg.head_dim, F = cfg.d_ff;
+    if (!r.tokens || !r.first_pos || !r.kv_len || !r.tables || !r.positions || !r.slots || !r.table) return fail(ODB_E_INVALID_ARG, "%s: NULL input", who);
+    if (r.n < 1 || r.n > kMaxRequests || r.b < 1 || r.b > 65536 || (long long)r.n * r.b > 65536)
+        return fail(ODB_E_INVALID_ARG, "%s: %d requests of %d rows (at most 65536 rows)", who, r.n, r.b);
+    if (r.skip < 0 || r.skip >= r.b) return fail(ODB_E_INVALID_ARG, "%s: skip=%d outside [0, %d)", who, r.skip, r.b);
+    if (r.unmask && (r.b > 256 || r.skip || !r.conf)) return fail(ODB_E_INVALID_ARG, "%s: unmask needs conf, blocks of at most 256 rows and no skip", who);
+    if ((r.conf == nullptr) != (r.argmax == nullptr)) return fail(ODB_E_INVALID_ARG, "%s: conf and argmax are given together", who);
+    if (layer0->dtype != ODB_F16 || layer0->n_kv_heads != H || layer0->head_dim != dh)
+        return fail(ODB_E_INVALID_ARG, "%s: pages of %d heads of %d, dtype %d; the model has %d of %d in binary16", who, layer0->n_kv_heads, layer0->head_dim,
+                    layer0->dtype, H, dh);
+    if (cfg.n_layers > 1 && (r.layer_stride < 8 || r.layer_stride & 7)) return fail(ODB_E_INVALID_ARG, "%s: layer_stride=%lld", who, r.layer_stride);
+    const int rows = r.n * r.b, rows_pad = ru(rows, 16), mt = rows_pad / 16;
+    const bool head = r.conf != nullptr, fused_head = r.unmask != nullptr;
+
+    odb_attention at{};
+    at.q_row = at.out_row = d;
+    at.columns = r.columns; at.n = r.n; at.rows = rows; at.n_heads = H;
+    at.scale = 1.0f / sqrtf((float)dh);
+    at.max_rows = r.b; at.max_len = r.max_len;
+    PagedAttn pa;
+    int nt;
+    int rc = plan_paged_attention(&at, layer0, true, pa, nt);
+    if (rc) return rc;
+    const size_t qkv_bytes = align_up((size_t)rows_pad * 3 * d * 4, 256), at_bytes = paged_attn_workspace(*layer0, rows, H, nt, pa.split);
+    if (r.n_pos < 1 || r.n_pos > 1 << 22 || (uintptr_t)r.table & 15) return fail(ODB_E_INVALID_ARG, "%s: table of %d positions, or not aligned to 16 bytes", who, r.n_pos);
+
+    hipStream_t s = (hipStream_t)stream;
+    HIP_TRY(hipSetDevice(m.device));
+    Plan pl;
+    rc = plan_scratch(m, [&](size_t room) {
+        return make_plan(cfg, rows_pad, rows_pad, 0, fused_head ? rows_pad : ru(r.n * (r.b - r.skip), 16), head, qkv_bytes + at_bytes, room);
+    }, pl, s);
+    if (rc) return rc;
+    char *base = (char *)m.scratch;
+    float *h = (float *)(base + pl.h), *qkv = (float *)(base + pl.extra);
+    u16 *xa = (u16 *)(base + pl.xa), *q = (u16 *)(base + pl.q), *ao = (u16 *)(base + pl.ao), *act = (u16 *)(base + pl.act);
+    const RowMap rm{1, rows_pad, rows};
+    const Workspace ws = workspace(m, base, pl);
+    const NormIn ni = norm_in(m, base, pl, mt);
+    // (the last row tile of the attention's output is padded with zeros: the projection works on them and reports what is out of range)
+    launch_embed(m, r.tokens, rm, h, norm_out(m, base, pl, m.g1, mt), ao, rows % 16 ? (size_t)rows_pad * d * 2 : 0, s);
+
+    QkNormRope qk{qkv, qkv + d, qkv + 2 * (size_t)d, ODB_F32, 3ll * d, 3ll * d, 3ll * d, rows, H, nullptr, nullptr, 0.f, r.table, r.n_pos, dh, 1, r.positions,
+                  r.slots, q, d, *layer0};
+    pa.q = q; pa.out = ao; pa.q_row = pa.out_row = d; pa.out_mt = mt;
+    pa.rows_per_request = r.b;
+    pa.first = r.first_pos; pa.kv_len = r.kv_len; pa.tables = r.tables;
+    pa.sc = at.scale * 1.44269504088896340736f;
+    for (int l = 0; l < cfg.n_layers; l++) {
+        LayerPtrs w = layer_ptrs(m, l);
+        qk.pages.k = (u16 *)layer0->k + (size_t)l * r.layer_stride;
+        qk.pages.v = (u16 *)layer0->v + (size_t)l * r.layer_stride;
+        pa.pages = qk.pages;
+        {
+            ProfScope ps(m, ODB_K_GEMM_QKV, s);
+            launch_gemm_store(xa, w.qkv, GemmShape{mt, 3 * d / 16, d / 32}, ni, qkv, 1, rows_pad, rows, 3 * d, ws, s);
+        }
+        launch_qk_norm_rope(qk, s);
+        {
+            ProfScope ps(m, ODB_K_ATTENTION, s);
+            launch_paged_attention(pa, nt, base + pl.extra + qkv_bytes, s);
+        }
+        const float *g_after_mlp = l + 1 < cfg.n_layers ? m.g1 + (size_t)(l + 1) * d : m.gf;
+        {
+            ProfScope ps(m, ODB_K_GEMM_O, s);
+            launch_gemm_resid(ao, w.o, GemmShape{mt, d / 16, d / 32}, h, d, norm_out(m, base, pl, w.g2, mt), ws, s);
+        }
+        {
+            ProfScope ps(m, ODB_K_GEMM_GATE_UP, s);
+            launch_gemm_swiglu(xa, w.gu, GemmShape{mt, 2 * F / 16, d / 32}, ni, act, m.counters, ws, s);
+        }
+        {
+            ProfScope ps(m, ODB_K_GEMM_DOWN, s);
+            launch_gemm_resid(act, w.dn, GemmShape{mt, d / 16, F / 32}, h, d, norm_out(m, base, pl, g_after_mlp, mt), ws, s);
+        }
+    }
+    HIP_TRY(hipGetLastError());
+    if (!head) return ODB_OK;
+    if (fused_head) return run_head(m, base, pl, rm, 0, true, r.tokens, r.b, r.tau, r.conf, r.argmax, r.unmask, nullptr, s);
+    return run_head(m, base, pl, RowMap{r.n, r.b, r.b}, r.skip, false, nullptr, 64, 0.f, r.conf, r.argmax, nullptr, nullptr, s);
 }
 
 }  // extern "C"

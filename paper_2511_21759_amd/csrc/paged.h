@@ -51,7 +51,9 @@ struct PagedAttn {
     void *out;
     long long q_row, out_row;
     int out_mt;                         // > 0: out is in operand tiles [heads * head_dim / 32][out_mt][512] (see common.h)
-    const int32_t *cu_rows, *first, *kv_len, *tables;   // cu_rows null: request r is row r; first null: the rows are the last positions
+    // cu_rows null: every request has rows_per_request rows; first null: the rows are the last positions
+    const int32_t *cu_rows, *first, *kv_len, *tables;
+    int rows_per_request;
     int columns, n, rows, heads, group;
     float sc;                           // scale * log2(e)
     int causal, window, sinks;
@@ -72,6 +74,8 @@ struct PagedAttn {
 constexpr int kManyRows = 0;
 void paged_attn_plan(const odb_pages &p, int n, int rows, int group, int max_rows, long long max_len, int *nt, int *split, long long *items);
 size_t paged_attn_workspace(const odb_pages &p, int rows, int heads, int nt, int split);
+// Checks a call's sizes and fills the fields that follow from them (paged_api.hip); buffers: the pools' addresses are checked too
+int plan_paged_attention(const odb_attention *a, const odb_pages *pages, bool buffers, PagedAttn &p, int &nt);
 void launch_paged_attention(PagedAttn a, int nt, void *workspace, hipStream_t s);
 
 }  // namespace odb

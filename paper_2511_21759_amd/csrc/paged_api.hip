@@ -59,8 +59,10 @@ size_t span(int rows, long long stride, int heads, int dim, int bytes) {
     return rows < 1 ? 0 : ((size_t)(rows - 1) * (size_t)stride + (size_t)heads * dim) * bytes;
 }
 
+}  // namespace
+
 // checks what does not need buffers, and fills the launch's fields that follow from it
-int plan_attention(const odb_attention *a, const odb_pages *pages, bool buffers, PagedAttn &p, int &nt) {
+int odb::plan_paged_attention(const odb_attention *a, const odb_pages *pages, bool buffers, PagedAttn &p, int &nt) {
     const char *who = "paged_attention";
     if (!a) return fail(ODB_E_INVALID_ARG, "%s: NULL argument", who);
     int rc = check_pages(who, pages, buffers);
@@ -73,20 +75,18 @@ int plan_attention(const odb_attention *a, const odb_pages *pages, bool buffers,
     if (!(a->scale > 0.f) || !isfinite(a->scale)) return fail(ODB_E_INVALID_ARG, "%s: scale=%g", who, (double)a->scale);
     if (a->window < 0 || a->window > 1 << 30 || a->sinks < 0 || a->sinks > 1 << 30) return fail(ODB_E_INVALID_ARG, "%s: window=%d, sinks=%d", who, a->window, a->sinks);
     if (a->max_rows < 0 || a->max_len < 0) return fail(ODB_E_INVALID_ARG, "%s: max_rows=%d, max_len=%d", who, a->max_rows, a->max_len);
-    if (!a->cu_rows && buffers && a->rows != a->n) return fail(ODB_E_INVALID_ARG, "%s: without cu_rows every request has one row (%d rows, %d requests)", who, a->rows, a->n);
     const long long most = (long long)a->columns * pages->page_size;
     p = PagedAttn{};
     p.columns = a->columns; p.n = a->n; p.rows = a->rows; p.heads = a->n_heads; p.group = a->n_heads / pages->n_kv_heads;
     p.pages = *pages;
     p.page_shift = page_shift(pages->page_size);
+    p.rows_per_request = 1;
     const int max_rows = a->max_rows > 0 && a->max_rows < a->rows ? a->max_rows : a->rows;
     paged_attn_plan(*pages, a->n, a->rows, p.group, max_rows, a->max_len > 0 && a->max_len < most ? a->max_len : most, &nt, &p.split, &p.items);
     if (p.items * pages->n_kv_heads > 0x7fffffffll || (long long)a->rows * a->n_heads > 0x7fffffffll)
         return fail(ODB_E_INVALID_ARG, "%s: %d rows of %d heads are too many for one launch", who, a->rows, a->n_heads);
     return ODB_OK;
 }
-
-}  // namespace
 
 extern "C" {
 
@@ -195,7 +195,7 @@ int odb_qk_norm_rope(const odb_qk_rows *rows, const odb_pages *pages, void *stre
 long long odb_paged_attention_workspace(const odb_attention *a, const odb_pages *pages) {
     PagedAttn p;
     int nt;
-    const int rc = plan_attention(a, pages, false, p, nt);
+    const int rc = plan_paged_attention(a, pages, false, p, nt);
     return rc ? rc : (long long)paged_attn_workspace(*pages, p.rows, p.heads, nt, p.split);
 }
 
@@ -203,8 +203,9 @@ int odb_paged_attention(const odb_attention *a, const odb_pages *pages, void *st
     const char *who = "paged_attention";
     PagedAttn p;
     int nt;
-    int rc = plan_attention(a, pages, true, p, nt);
+    int rc = plan_paged_attention(a, pages, true, p, nt);
     if (rc) return rc;
+    if (!a->cu_rows && a->rows != a->n) return fail(ODB_E_INVALID_ARG, "%s: without cu_rows every request has one row (%d rows, %d requests)", who, a->rows, a->n);
     const int dim = pages->head_dim;
     if ((rc = check_rows(who, "q", a->q, a->q_row, a->n_heads, dim)) || (rc = check_rows(who, "out", a->out, a->out_row, a->n_heads, dim))) return rc;
     if (!a->kv_len || !a->tables) return fail(ODB_E_INVALID_ARG, "%s: NULL kv_len or tables", who);

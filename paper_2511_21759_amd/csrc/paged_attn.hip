@@ -60,7 +60,7 @@ __device__ __forceinline__ int ld_scalar(const int32_t *p, int i) { return ((sca
 
 __device__ __forceinline__ Request request_of(const PagedAttn &a, int r) {
     Request q;
-    int lo = r, hi = r + 1;
+    int lo = r * a.rows_per_request, hi = lo + a.rows_per_request;
     if (a.cu_rows) { lo = ld_scalar(a.cu_rows, r); hi = ld_scalar(a.cu_rows, r + 1); }
     lo = min(max(lo, 0), a.rows);
     hi = min(max(hi, 0), a.rows);

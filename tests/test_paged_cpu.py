@@ -110,6 +110,7 @@ def test_null_structures(lib):
     assert lib.odb_qk_norm_rope(None, ctypes.byref(pages()), None) == INVALID
     assert lib.odb_qk_norm_rope(ctypes.byref(qk_rows()), None, None) == INVALID
     assert lib.odb_paged_attention_workspace(None, None) == INVALID
+    assert lib.odb_step_paged(None, None, ctypes.byref(pages()), None) == INVALID
 
 
 def test_workspace_grows_with_rows_and_is_none_for_short_keys(lib):
