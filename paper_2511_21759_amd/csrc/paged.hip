@@ -256,8 +256,10 @@ __device__ __forceinline__ void store8(T *p, f32x8 x) {
 
 // A head is held by DH / 16 lanes with 16 channels each: in the half layout channel pair (j, j + rot / 2) sits in one lane as
 // elements of its first and its second eight, in the interleaved layout (2j, 2j + 1) inside each eight.  Lanes behind the rotated
-// part hold two neighbouring eights that pass through.  A wave does `per` groups of heads of one row, so the row's cosines and
-// sines are loaded once into registers; its groups of lanes do different heads.  Bound by the memory: every element is read and written once.
+// part hold two neighbouring eights that pass through.  A wave does as many heads of one row as it has groups of lanes, and nothing
+// else: with loops over more heads, which would load the row's angles once for all of them, the large call is slower.  Bound by the
+// memory, every element read and written once: 16411 rows of 48 heads of 128 bfloat16, 408 MB, take 81 us (5.0 TB/s; a copy reaches
+// 4.9), with two or three times as many heads per wave 84 to 89; loads past the caches take 100.
 template <class TI, class TO, int DH, bool INTER>
 __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkNormRope a, int waves_per_row) {
     constexpr int LANES = DH / 16, HEADS = 64 / LANES;          // lanes per head, heads per wave
@@ -288,66 +290,62 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkNormRope a, int wav
         }
     }
     const int kv = pg.n_kv_heads, total = a.heads + 2 * kv;
-    for (int h = part * HEADS + slice; h < total; h += waves_per_row * HEADS) {
-        const bool is_q = h < a.heads, is_k = !is_q && h < a.heads + kv;
-        const int head = is_q ? h : is_k ? h - a.heads : h - a.heads - kv;
-        const TI *src = is_q ? (const TI *)a.q + (size_t)row * a.q_row : is_k ? (const TI *)a.k + (size_t)row * a.k_row
-                                                                              : (const TI *)a.v + (size_t)row * a.v_row;
-        src += (size_t)head * DH;
-        f32x8 x = load8(src + c0), y = load8(src + c1);
-        if (is_q || is_k) {
-            const float *gain = is_q ? a.q_gain : a.k_gain;
-            if (gain) {
-                float ss = 0.f;
+    const int h = part * HEADS + slice;
+    if (h >= total) return;
+    const bool is_q = h < a.heads, is_k = !is_q && h < a.heads + kv;
+    const int head = is_q ? h : is_k ? h - a.heads : h - a.heads - kv;
+    const TI *src = is_q ? (const TI *)a.q + (size_t)row * a.q_row : is_k ? (const TI *)a.k + (size_t)row * a.k_row
+                                                                          : (const TI *)a.v + (size_t)row * a.v_row;
+    src += (size_t)head * DH;
+    f32x8 x = load8(src + c0), y = load8(src + c1);
+    if (is_q || is_k) {
+        const float *gain = is_q ? a.q_gain : a.k_gain;
+        if (gain) {
+            float ss = 0.f;
 #pragma unroll
-                for (int i = 0; i < 8; i++) ss += x[i] * x[i] + y[i] * y[i];
+            for (int i = 0; i < 8; i++) ss += x[i] * x[i] + y[i] * y[i];
 #pragma unroll
-                for (int o = LANES / 2; o > 0; o >>= 1) ss += __shfl_xor(ss, o);
-                const float r = 1.0f / sqrtf(ss / (float)DH + a.eps);
-                const f32x8 g0 = load8(gain + c0), g1 = load8(gain + c1);
-                x = x * r * g0;
-                y = y * r * g1;
-            }
-            if (turns) {
-                if (INTER) {
+            for (int o = LANES / 2; o > 0; o >>= 1) ss += __shfl_xor(ss, o);
+            const float r = 1.0f / sqrtf(ss / (float)DH + a.eps);
+            const f32x8 g0 = load8(gain + c0), g1 = load8(gain + c1);
+            x = x * r * g0;
+            y = y * r * g1;
+        }
+        if (turns) {
+            if (INTER) {
 #pragma unroll
-                    for (int i = 0; i < 4; i++) {
-                        const float u = x[2 * i], v = x[2 * i + 1], p = y[2 * i], q = y[2 * i + 1];
-                        x[2 * i] = u * cs[i] - v * sn[i];
-                        x[2 * i + 1] = v * cs[i] + u * sn[i];
-                        y[2 * i] = p * cs[4 + i] - q * sn[4 + i];
-                        y[2 * i + 1] = q * cs[4 + i] + p * sn[4 + i];
-                    }
-                } else {
+                for (int i = 0; i < 4; i++) {
+                    const float u = x[2 * i], v = x[2 * i + 1], p = y[2 * i], q = y[2 * i + 1];
+                    x[2 * i] = u * cs[i] - v * sn[i];
+                    x[2 * i + 1] = v * cs[i] + u * sn[i];
+                    y[2 * i] = p * cs[4 + i] - q * sn[4 + i];
+                    y[2 * i + 1] = q * cs[4 + i] + p * sn[4 + i];
+                }
+            } else {
 #pragma unroll
-                    for (int i = 0; i < 8; i++) {
-                        const float u = x[i], v = y[i];
-                        x[i] = u * cs[i] - v * sn[i];
-                        y[i] = v * cs[i] + u * sn[i];
-                    }
+                for (int i = 0; i < 8; i++) {
+                    const float u = x[i], v = y[i];
+                    x[i] = u * cs[i] - v * sn[i];
+                    y[i] = v * cs[i] + u * sn[i];
                 }
             }
         }
-        TO *dst;
-        if (is_q) {
-            dst = (TO *)a.q_out + (size_t)row * a.q_out_row + (size_t)head * DH;
-            if (!live) x = y = f32x8{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        } else {
-            if (!stored) continue;
-            dst = (TO *)(is_k ? pg.k : pg.v) + at + (size_t)head * pg.head_stride;
-        }
-        store8(dst + c0, x);
-        store8(dst + c1, y);
     }
+    TO *dst;
+    if (is_q) {
+        dst = (TO *)a.q_out + (size_t)row * a.q_out_row + (size_t)head * DH;
+        if (!live) x = y = f32x8{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    } else {
+        if (!stored) return;
+        dst = (TO *)(is_k ? pg.k : pg.v) + at + (size_t)head * pg.head_stride;
+    }
+    store8(dst + c0, x);
+    store8(dst + c1, y);
 }
 
 template <class TI, class TO, int DH>
 static void launch_rope_dim(const QkNormRope &a, hipStream_t s) {
-    // A wave that does all heads of its row loads the angles once; with few rows the heads are spread over more waves, up to
-    // four per SIMD of the chip, which shortens the chain of loads that bounds a small call.
-    const int per_wave = 64 / (DH / 16), total = a.heads + 2 * a.pages.n_kv_heads, most = (total + per_wave - 1) / per_wave;
-    int wpr = 1;
-    while (wpr < most && (long long)a.rows * wpr < 4096) wpr++;
+    const int per_wave = 64 / (DH / 16), wpr = (a.heads + 2 * a.pages.n_kv_heads + per_wave - 1) / per_wave;
     const unsigned grid = (unsigned)(((long long)a.rows * wpr + 3) / 4);
     if (a.interleaved) qk_norm_rope_kernel<TI, TO, DH, true><<<dim3(grid), 256, 0, s>>>(a, wpr);
     else qk_norm_rope_kernel<TI, TO, DH, false><<<dim3(grid), 256, 0, s>>>(a, wpr);

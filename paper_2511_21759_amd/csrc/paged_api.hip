@@ -168,6 +168,7 @@ int odb_qk_norm_rope(const odb_qk_rows *rows, const odb_pages *pages, void *stre
     const int dim = pages->head_dim, kv = pages->n_kv_heads;
     if (r.rows < 0 || r.rows > 1 << 24) return fail(ODB_E_INVALID_ARG, "%s: rows=%d outside [0, 2^24]", who, r.rows);
     if (r.n_heads < 1 || r.n_heads > 65536) return fail(ODB_E_INVALID_ARG, "%s: n_heads=%d", who, r.n_heads);
+    if ((long long)r.rows * (r.n_heads + 2ll * kv) > 0x7fffffffll) return fail(ODB_E_INVALID_ARG, "%s: %d rows of %d heads are too many for one launch", who, r.rows, r.n_heads);
     if (r.in_dtype != ODB_F32 && r.in_dtype != pages->dtype) return fail(ODB_E_INVALID_ARG, "%s: rows of dtype %d into pages of dtype %d", who, r.in_dtype, pages->dtype);
     if (!(rc = check_rows(who, "q", r.q, r.q_row, r.n_heads, dim)) && !(rc = check_rows(who, "k", r.k, r.k_row, kv, dim)) &&
         !(rc = check_rows(who, "v", r.v, r.v_row, kv, dim)))

@@ -68,7 +68,7 @@ def qk_rows(**kw):
 
 
 @pytest.mark.parametrize("kw", [dict(q=None), dict(k=None), dict(v=(3 << 30) + 2), dict(q_out=None), dict(in_dtype=1), dict(in_dtype=3), dict(rows=-1),
-                                dict(rows=(1 << 24) + 1), dict(n_heads=0), dict(q_row=248), dict(k_row=132), dict(v_row=120), dict(q_out_row=-256),
+                                dict(rows=(1 << 24) + 1), dict(rows=1 << 24, n_heads=200), dict(n_heads=0), dict(q_row=248), dict(k_row=132), dict(v_row=120), dict(q_out_row=-256),
                                 dict(q_gain=None), dict(k_gain=A[3] + 4), dict(eps=-1.0), dict(eps=float("nan")), dict(table=None), dict(n_pos=0),
                                 dict(rot_dim=8), dict(rot_dim=72), dict(rot_dim=24), dict(positions=None), dict(slots=None), dict(q_out=(1 << 30) + 256),
                                 dict(q_out=2 << 30), dict(q_out=(3 << 30) - 2048), dict(q_out=1 << 30, in_dtype=2), dict(q_out=1 << 30, q_out_row=264)])
