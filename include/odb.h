@@ -425,6 +425,8 @@ typedef struct {
  *   slots, positions   dev int32 [rows_cap]: for every row its position and its slot, page * page_size + position inside the
  *                  page; -1 where the position lies outside [0, len[r]) or its page outside the pool.  Entries behind the last row stay.
  *   state          dev int32 [4]: free pages afterwards (the next call's n_free), pages taken, given back, requests refused
+ * Pages are not counted: one that several tables name (a prefix that requests share) is given back as often as requests that
+ * hold it get shorter, so shared pages are kept out of what is given back.
  * The same call with the same inputs writes the same values again.  Buffers must not overlap.  Asynchronous on `stream`.
  * Errors: ODB_E_INVALID_ARG for NULL buffers, n outside [1, 4096], columns < 1, columns * page_size > 2^30, rows_cap outside
  * [1, 2^24], n_pages < 1, a page size or a pool outside the requirements above, or buffers that overlap. */
@@ -503,8 +505,8 @@ int odb_qk_norm_rope(const odb_qk_rows *rows, const odb_pages *pages, void *stre
  * Scores and sums are 32-bit; probabilities are rounded to the pages' dtype for the product with V.  The order of all
  * additions follows from the arguments and the lengths alone, so the same call gives the same bits.
  * Asynchronous on `stream`.  Errors: ODB_E_INVALID_ARG for NULL buffers, n outside [1, 4096], rows outside [0, 2^24] (0: nothing is
- * launched), n_heads no multiple of n_kv_heads, columns < 1, columns * page_size > 2^30, a scale that is not positive and
- * finite, window or sinks negative or above 2^30, a workspace that is too small, buffers not aligned to 16 bytes, row
+ * launched), n_heads no multiple of n_kv_heads, columns < 1, columns * page_size > 2^30, a scale that is not positive or, times
+ * log2(e), not finite, window or sinks negative or above 2^30, a workspace that is too small, buffers not aligned to 16 bytes, row
  * strides that are no multiples of 8, out overlapping q, pools outside the requirements above. */
 typedef struct {
     const void *q;

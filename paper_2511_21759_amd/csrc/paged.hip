@@ -179,7 +179,7 @@ void launch_page_tables(PageTables a, hipStream_t s) {
     // pages; the kinds of items are done beside each other, since each is a chain of dependent reads
     a.row_groups = a.rows_cap / 1024 + 1 < 512 ? a.rows_cap / 1024 + 1 : 512;
     a.page_groups = a.n / 32 + 1;
-    allow_lds<page_tables_kernel>(kMaxRequests * 28);
+    if (a.n * 28 > 65536) allow_lds<page_tables_kernel>(kMaxRequests * 28);
     page_tables_kernel<<<dim3(a.row_groups + 2 * a.page_groups), 256, a.n * 28, s>>>(a);
 }
 

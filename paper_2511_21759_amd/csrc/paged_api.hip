@@ -72,7 +72,7 @@ int odb::plan_paged_attention(const odb_attention *a, const odb_pages *pages, bo
     if (a->n_heads < 1 || a->n_heads % pages->n_kv_heads) return fail(ODB_E_INVALID_ARG, "%s: %d query heads over %d K/V heads", who, a->n_heads, pages->n_kv_heads);
     rc = check_columns(who, a->columns, pages->page_size);
     if (rc) return rc;
-    if (!(a->scale > 0.f) || !isfinite(a->scale)) return fail(ODB_E_INVALID_ARG, "%s: scale=%g", who, (double)a->scale);
+    if (!(a->scale > 0.f) || !isfinite(a->scale * 1.44269504088896340736f)) return fail(ODB_E_INVALID_ARG, "%s: scale=%g", who, (double)a->scale);
     if (a->window < 0 || a->window > 1 << 30 || a->sinks < 0 || a->sinks > 1 << 30) return fail(ODB_E_INVALID_ARG, "%s: window=%d, sinks=%d", who, a->window, a->sinks);
     if (a->max_rows < 0 || a->max_len < 0) return fail(ODB_E_INVALID_ARG, "%s: max_rows=%d, max_len=%d", who, a->max_rows, a->max_len);
     const long long most = (long long)a->columns * pages->page_size;

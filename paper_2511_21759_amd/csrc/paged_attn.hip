@@ -81,7 +81,7 @@ __device__ __forceinline__ Blocks blocks_of(const PagedAttn &a, int len, int pmi
     if (a.causal) hi = min(hi, pmax + 1);
     if (a.window) {
         lo = max(0, pmin - a.window + 1);
-        hi = min(hi, pmax < 0 ? 0 : pmax > kFar - a.window ? kFar : pmax + a.window);
+        hi = min(hi, pmax > kFar - a.window ? kFar : pmax + a.window);
     }
     Blocks b;
     constexpr int M = (1 << SHIFT) - 1;

@@ -263,7 +263,7 @@ def test_long_keys_split_over_workgroups(page, max_len):
     rq.check(rq.run(causal=True, cu=False, max_len=max_len), causal=True)
 
 
-@pytest.mark.parametrize("n,kv", [(64, 1), (65, 1), (300, 1), (300, 2), (700, 4)])
+@pytest.mark.parametrize("n,kv", [(64, 1), (65, 1), (300, 1), (300, 2), (700, 4), (4096, 1)])
 @pytest.mark.parametrize("max_len", [0, 64])
 def test_many_requests(n, kv, max_len):
     """Lists of requests longer than a wave, with and without split keys; most of them short, some without rows or keys."""
@@ -329,6 +329,16 @@ def test_rows_at_given_positions(causal, window, sinks):
     rq = Requests(3, rows, lens, 4, 4, 128, "f16", 16)
     got = rq.run(first=first, causal=causal, window=window, sinks=sinks)
     rq.check(got, first=first, causal=causal, window=window, sinks=sinks)
+
+
+def test_windows_that_reach_over_the_ends():
+    """Rows before the first position and behind the last whose window reaches back to it, with sinks and without."""
+    rows, lens, first = [4, 3, 5, 1], [50, 300, 40, 700], [-7, -300, 45, 705]
+    for max_len in (0, 5000):
+        for sinks in (0, 3):
+            rq = Requests(5 + sinks, rows, lens, 2, 1, 64, "f16", 16, extra_columns=100 if max_len else 1)
+            rq.check(rq.run(first=first, causal=False, window=9, sinks=sinks), first=first, window=9, sinks=sinks)
+            rq.check(rq.run(first=first, causal=True, window=9, sinks=sinks), first=first, causal=True, window=9, sinks=sinks)
 
 
 def test_no_number_at_hidden_places_of_a_visible_block():

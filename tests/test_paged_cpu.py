@@ -86,7 +86,7 @@ def attention(**kw):
 
 @pytest.mark.parametrize("kw", [dict(q=None), dict(out=None), dict(kv_len=None), dict(tables=None), dict(q=(1 << 30) + 4), dict(q_row=8), dict(out_row=260),
                                 dict(n=0), dict(n=4097), dict(rows=-1), dict(rows=(1 << 24) + 1), dict(n_heads=3), dict(n_heads=0), dict(columns=0),
-                                dict(columns=1 << 28), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")),
+                                dict(columns=1 << 28), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=3e38),
                                 dict(window=-1), dict(sinks=-1), dict(window=(1 << 30) + 1), dict(max_rows=-1), dict(max_len=-1), dict(out=(1 << 30) + 512),
                                 dict(cu_rows=None), dict(columns=4000), dict(columns=4000, workspace=A[5] + 16, workspace_bytes=1 << 30),
                                 dict(columns=4000, workspace=A[5], workspace_bytes=100)])
