@@ -68,11 +68,14 @@ struct PagedAttn {
     float *partial;
     float2 *ml;
     int2 *where;
+    int4 *plan;                         // kManyRows: where each of `split` pieces starts (request, tile, place), then the pieces' size and sum
+    int tiles;                          // upper bound of the row tiles
 };
 // The way of a call: nt 16-row tiles per workgroup whose waves split the keys (1, 2 or 4), or kManyRows, where they split the rows;
 // workgroups per K/V head that share the keys (0: no split), and the grid's items per K/V head.
 constexpr int kManyRows = 0;
-void paged_attn_plan(const odb_pages &p, int n, int rows, int group, int max_rows, long long max_len, int *nt, int *split, long long *items);
+void paged_attn_plan(const odb_pages &p, int n, int rows, int group, int max_rows, long long max_len, long long columns, int *nt, int *split,
+                     long long *items);
 size_t paged_attn_workspace(const odb_pages &p, int rows, int heads, int nt, int split);
 // Checks a call's sizes and fills the fields that follow from them (paged_api.hip); buffers: the pools' addresses are checked too
 int plan_paged_attention(const odb_attention *a, const odb_pages *pages, bool buffers, PagedAttn &p, int &nt);

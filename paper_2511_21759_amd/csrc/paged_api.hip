@@ -82,7 +82,7 @@ int odb::plan_paged_attention(const odb_attention *a, const odb_pages *pages, bo
     p.page_shift = page_shift(pages->page_size);
     p.rows_per_request = 1;
     const int max_rows = a->max_rows > 0 && a->max_rows < a->rows ? a->max_rows : a->rows;
-    paged_attn_plan(*pages, a->n, a->rows, p.group, max_rows, a->max_len > 0 && a->max_len < most ? a->max_len : most, &nt, &p.split, &p.items);
+    paged_attn_plan(*pages, a->n, a->rows, p.group, max_rows, a->max_len > 0 && a->max_len < most ? a->max_len : most, a->columns, &nt, &p.split, &p.items);
     if (p.items * pages->n_kv_heads > 0x7fffffffll || (long long)a->rows * a->n_heads > 0x7fffffffll)
         return fail(ODB_E_INVALID_ARG, "%s: %d rows of %d heads are too many for one launch", who, a->rows, a->n_heads);
     return ODB_OK;

@@ -362,6 +362,7 @@ __device__ __forceinline__ bool all_seen(const PagedAttn &a, int len, int key0, 
 // places per workgroup hold them: 2 w + 1 for a pair that starts in it, 2 w for one that started before.
 // Places of a piece at least: 32 single tokens of 20 to 4000 positions, 28 heads over 4, take 18 us with 12, 19 with 16, 21 with 10.
 constexpr int kLeastPiece = 12;
+constexpr int kRowsPlace = 256;          // `where` holds parts * kRowsPlace + row of the tile
 
 template <class T, int DH, int NT>
 __global__ __launch_bounds__(64 * NW, DH == 256 || NT == 4 ? 1 : 2) void paged_attn_kernel(PagedAttn a) {
@@ -590,7 +591,7 @@ __global__ __launch_bounds__(64 * NW, DH == 256 || NT == 4 ? 1 : 2) void paged_a
                         *reinterpret_cast<f32x4 *>(dst + 4) = f32x4{sum[4], sum[5], sum[6], sum[7]};
                         if (c == 0) {
                             a.ml[place * TILE_ROWS + t * 16 + r] = float2{top, l};
-                            if (b_lo == 0) a.where[(size_t)row * a.heads + hq] = int2{x, parts * 64 + t * 16 + r};
+                            if (b_lo == 0) a.where[(size_t)row * a.heads + hq] = int2{x, parts * kRowsPlace + t * 16 + r};
                         }
                     } else {
                         // a row that sees nothing is zero
@@ -638,6 +639,69 @@ __device__ __forceinline__ int k_piece(int key, int c) {
     return key * (DH / 8) + (DH == 64 ? c ^ ((key >> 1) & 7) : c ^ (key & 15));
 }
 
+// Where row tiles are too few to fill the chip, pieces of the list of their stages are given out as in paged_attn_kernel.  The stages
+// that a tile sees differ from tile to tile, so a launch in front works out where each piece starts: a thread per tile.
+constexpr int kTileCost = 3, kLeastStages = 4, kPlanTiles = 512;
+template <int DH>
+__global__ __launch_bounds__(kPlanTiles) void paged_plan_kernel(PagedAttn a) {
+    typedef RowsShape<DH> Shape;
+    __shared__ int request_end[kMaxRequests], tile_end[kPlanTiles], sums[kPlanTiles / 64];
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    auto scan = [&](int v, int &carry) {
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int up = __shfl_up(v, o);
+            if (lane >= o) v += up;
+        }
+        if (lane == 63) sums[wave] = v;
+        __syncthreads();
+        v += carry;
+        for (int w = 0; w < kPlanTiles / 64; w++) {
+            if (w < wave) v += sums[w];
+            carry += sums[w];
+        }
+        __syncthreads();
+        return v;
+    };
+    auto first_behind = [](const int *ends, int n, int x) {            // first entry above x
+        int lo = 0, hi = n - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (ends[mid] > x) hi = mid; else lo = mid + 1;
+        }
+        return lo;
+    };
+    int n_tiles = 0;
+    for (int r0 = 0; r0 < a.n; r0 += kPlanTiles) {
+        const int r = r0 + t, tiles = r < a.n ? min(tiles_of(a, request_of(a, r), Shape::TILE_ROWS), kPlanTiles) : 0, end = scan(tiles, n_tiles);
+        if (r < a.n) request_end[r] = end;
+    }
+    __syncthreads();
+    n_tiles = min(n_tiles, kPlanTiles);                                     // (more only if cu_rows does not rise)
+    int places = 0, total = 0;
+    if (t < n_tiles) {
+        const int r = first_behind(request_end, a.n, t);
+        const Request q = request_of(a, r);
+        int pmin, pmax;
+        tile_span(q, a.group, t - (r ? request_end[r - 1] : 0), Shape::TILE_ROWS, pmin, pmax);
+        places = max(1, blocks_of<Shape::SHIFT>(a, q.len, pmin, pmax).count) + kTileCost;
+    }
+    const int end = scan(places, total);
+    tile_end[t] = end;
+    __syncthreads();
+    const int piece = max(kLeastStages + kTileCost, (total + a.split - 1) / a.split);
+    for (int x = t; x < a.split; x += kPlanTiles) {
+        const long long start = (long long)x * piece;
+        int4 p{-1, 0, 0, 0};
+        if (start < total) {
+            const int y = first_behind(tile_end, n_tiles, (int)start), r = first_behind(request_end, a.n, y);
+            p = int4{r, y - (r ? request_end[r - 1] : 0), (int)start - (y ? tile_end[y - 1] : 0), 0};
+        }
+        a.plan[x] = p;
+    }
+    if (t == 0) a.plan[a.split] = int4{piece, total, 0, 0};
+}
+
 template <class T, int DH>
 __global__ __launch_bounds__(256, DH == 256 ? 1 : 2) void paged_rows_kernel(PagedAttn a) {
     typedef RowsShape<DH> Shape;
@@ -648,158 +712,214 @@ __global__ __launch_bounds__(256, DH == 256 ? 1 : 2) void paged_rows_kernel(Page
     __shared__ int odd_flag[2][4];
 
     const int kv = a.pages.n_kv_heads, head = (int)(blockIdx.x % (unsigned)kv), x = (int)(blockIdx.x / (unsigned)kv);
-    Place pl;
-    if (!find_place(a, Shape::TILE_ROWS, false, [&](long long) { return (long long)x; }, pl)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, li = lane & 15;
-    const Request rq = pl.q;
-    const int G = a.group, n_rows = rq.m * G;
-    const int tile = tiles_of(a, rq, Shape::TILE_ROWS) - 1 - __builtin_amdgcn_readfirstlane((int)pl.at);    // those that see the most first
-    int pmin, pmax, wmin, wmax;                                             // positions of the tile's rows and of this wave's
-    tile_span(rq, G, tile, Shape::TILE_ROWS, pmin, pmax);
-    tile_span(rq, G, tile * 4 + wave, 16 * NT, wmin, wmax);
-    const Blocks bl = blocks_of<SHIFT>(a, rq.len, pmin, pmax);
-    const int rho0 = (tile * 4 + wave) * 16 * NT;
-    const bool idle = rho0 >= n_rows;                                       // (a wave without rows helps to load)
-
-    frag_t q[NT][KS];
-    Sight sight[NT];
-#pragma unroll
-    for (int t = 0; t < NT; t++) {
-        const int rho = min(rho0 + t * 16 + li, n_rows - 1), i = rho / G, hq = head * G + (rho - i * G);
-        sight[t] = sight_of(a, rq.len, rq.first + i);
-        const u16 *src = (const u16 *)a.q + (size_t)(rq.row0 + i) * a.q_row + (size_t)hq * DH + 8 * g;
-#pragma unroll
-        for (int k = 0; k < KS; k++) q[t][k] = ld_frag(src + 32 * k);
+    const bool split = a.split > 0;
+    const int cost = split ? kTileCost : 0;
+    // request and tile, the place in the tile's part of the list where this piece starts, and the places that are left
+    Request rq;
+    int request, tiles, tile, at, left, piece = 1, total = 0;
+    if (split) {
+        const int32_t *plan = reinterpret_cast<const int32_t *>(a.plan);
+        request = ld_scalar(plan, 4 * x);
+        if (request < 0) return;
+        tile = ld_scalar(plan, 4 * x + 1);
+        at = ld_scalar(plan, 4 * x + 2);
+        piece = ld_scalar(plan, 4 * a.split);
+        total = ld_scalar(plan, 4 * a.split + 1);
+        left = min(piece, total - piece * x);
+        rq = request_of(a, request);
+        tiles = tiles_of(a, rq, Shape::TILE_ROWS);
+    } else {
+        Place pl;
+        if (!find_place(a, Shape::TILE_ROWS, false, [&](long long) { return (long long)x; }, pl)) return;
+        request = pl.r;
+        rq = pl.q;
+        tiles = tiles_of(a, rq, Shape::TILE_ROWS);
+        tile = tiles - 1 - __builtin_amdgcn_readfirstlane((int)pl.at);      // those that see the most first
+        at = 0;
+        left = 1;
     }
-    f32x4 o[NT][CT], lsum[NT];
-    Reference ref[NT];
-#pragma unroll
-    for (int t = 0; t < NT; t++) {
-        lsum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int c = 0; c < CT; c++) o[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
+    const int G = a.group;
     const frag_t ones = {{Num<T>::kOnes, Num<T>::kOnes, Num<T>::kOnes, Num<T>::kOnes}};
 
     const u16 *kp = (const u16 *)a.pages.k + (size_t)head * a.pages.head_stride, *vp = (const u16 *)a.pages.v + (size_t)head * a.pages.head_stride;
-    const int32_t *table = a.tables + (size_t)pl.r * a.columns;
     const int page_mask = (1 << a.page_shift) - 1;
     const size_t pos_stride = a.pages.pos_stride, page_stride = a.pages.page_stride;
     const int s_key = lane / (DH / 8), s_ch = lane % (DH / 8);
     const unsigned s_off = 2u * (s_key * (unsigned)pos_stride + s_ch * 8);
-    auto page_of = [&](int key) -> int {
-        const int id = key < rq.len ? ld_scalar(table, key >> a.page_shift) : -1;
-        return id >= 0 && id < a.pages.n_pages ? id : -1;
-    };
-    // pages of the 16-key tiles of a stage, and the one that holds the keys which this wave stages
-    struct Stage { int key0, page[SK / 16], mine; };
-    auto stage_of = [&](int b) {
-        Stage s;
-        s.key0 = block_key<SHIFT>(bl, b);
+    for (;;) {
+        const int n_rows = rq.m * G, rho0 = (tile * 4 + wave) * 16 * NT;
+        int pmin, pmax, wmin, wmax;                                             // positions of the tile's rows and of this wave's
+        tile_span(rq, G, tile, Shape::TILE_ROWS, pmin, pmax);
+        tile_span(rq, G, tile * 4 + wave, 16 * NT, wmin, wmax);
+        const Blocks bl = blocks_of<SHIFT>(a, rq.len, pmin, pmax);
+        const int nb = max(1, bl.count), end = split ? min(nb + cost, at + left) : nb;
+        const int b_lo = max(0, at - cost), b_hi = min(bl.count, end - cost);
+        if (end - cost > b_lo) {
+            const bool whole = b_lo == 0 && end - cost == nb;
+            const bool idle = rho0 >= n_rows;                                       // (a wave without rows helps to load)
+            const int32_t *table = a.tables + (size_t)request * a.columns;
+            frag_t q[NT][KS];
+            Sight sight[NT];
 #pragma unroll
-        for (int i = 0; i < SK / 16; i++) s.page[i] = page_of(s.key0 + 16 * i);
-        s.mine = page_of(s.key0 + WK * wave);
-        return s;
-    };
-    frag_t kr[LD], vr[LD];
-    auto load = [&](const Stage &s) {
-        const size_t base = (size_t)max(s.mine, 0) * page_stride + (size_t)((s.key0 + WK * wave) & page_mask) * pos_stride;
+            for (int t = 0; t < NT; t++) {
+                const int rho = min(rho0 + t * 16 + li, n_rows - 1), i = rho / G, hq = head * G + (rho - i * G);
+                sight[t] = sight_of(a, rq.len, rq.first + i);
+                const u16 *src = (const u16 *)a.q + (size_t)(rq.row0 + i) * a.q_row + (size_t)hq * DH + 8 * g;
 #pragma unroll
-        for (int j = 0; j < LD; j++) kr[j] = ld_at<false>(kp + base + (size_t)(j * KEYS) * pos_stride, s_off);
+                for (int k = 0; k < KS; k++) q[t][k] = ld_frag(src + 32 * k);
+            }
+            f32x4 o[NT][CT], lsum[NT];
+            Reference ref[NT];
 #pragma unroll
-        for (int j = 0; j < LD; j++) vr[j] = ld_at<false>(vp + base + (size_t)(j * KEYS) * pos_stride, s_off);
-    };
-    auto store = [&](int buf, bool look) {
-        unsigned char *k0 = stages + buf * BUF, *v0 = k0 + SK * DH * 2;
-        int odd = 0;
+            for (int t = 0; t < NT; t++) {
+                lsum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int j = 0; j < LD; j++) {
-            const int key = WK * wave + s_key + j * KEYS;
-            *reinterpret_cast<frag_t *>(k0 + 16 * k_piece<DH>(key, s_ch)) = kr[j];
-            *reinterpret_cast<frag_t *>(v0 + 16 * v_piece<DH>(key, s_ch)) = vr[j];
-            if (look) odd |= has_odd<T>(vr[j]);
-        }
-        if (look) {
-            odd = __any(odd);
-            if (lane == 0) odd_flag[buf][wave] = odd;
-        }
-    };
-    // does every row of the tile see every key of the stage?
-    auto plain_stage = [&](const Stage &s) {
-        bool there = true;
+                for (int c = 0; c < CT; c++) o[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+            }
+            auto page_of = [&](int key) -> int {
+                const int id = key < rq.len ? ld_scalar(table, key >> a.page_shift) : -1;
+                return id >= 0 && id < a.pages.n_pages ? id : -1;
+            };
+            // pages of the 16-key tiles of a stage, and the one that holds the keys which this wave stages
+            struct Stage { int key0, page[SK / 16], mine; };
+            auto stage_of = [&](int b) {
+                Stage s;
+                s.key0 = block_key<SHIFT>(bl, b);
 #pragma unroll
-        for (int i = 0; i < SK / 16; i++) there = there && s.page[i] >= 0;
-        return there && all_seen(a, rq.len, s.key0, SK, pmin, pmax);
-    };
+                for (int i = 0; i < SK / 16; i++) s.page[i] = page_of(s.key0 + 16 * i);
+                s.mine = page_of(s.key0 + WK * wave);
+                return s;
+            };
+            frag_t kr[LD], vr[LD];
+            auto load = [&](const Stage &s) {
+                const size_t base = (size_t)max(s.mine, 0) * page_stride + (size_t)((s.key0 + WK * wave) & page_mask) * pos_stride;
+#pragma unroll
+                for (int j = 0; j < LD; j++) kr[j] = ld_at<false>(kp + base + (size_t)(j * KEYS) * pos_stride, s_off);
+#pragma unroll
+                for (int j = 0; j < LD; j++) vr[j] = ld_at<false>(vp + base + (size_t)(j * KEYS) * pos_stride, s_off);
+            };
+            auto store = [&](int buf, bool look) {
+                unsigned char *k0 = stages + buf * BUF, *v0 = k0 + SK * DH * 2;
+                int odd = 0;
+#pragma unroll
+                for (int j = 0; j < LD; j++) {
+                    const int key = WK * wave + s_key + j * KEYS;
+                    *reinterpret_cast<frag_t *>(k0 + 16 * k_piece<DH>(key, s_ch)) = kr[j];
+                    *reinterpret_cast<frag_t *>(v0 + 16 * v_piece<DH>(key, s_ch)) = vr[j];
+                    if (look) odd |= has_odd<T>(vr[j]);
+                }
+                if (look) {
+                    odd = __any(odd);
+                    if (lane == 0) odd_flag[buf][wave] = odd;
+                }
+            };
+            // does every row of the tile see every key of the stage?
+            auto plain_stage = [&](const Stage &s) {
+                bool there = true;
+#pragma unroll
+                for (int i = 0; i < SK / 16; i++) there = there && s.page[i] >= 0;
+                return there && all_seen(a, rq.len, s.key0, SK, pmin, pmax);
+            };
 
-    if (bl.count > 0) {
-        Stage cur = stage_of(0), next = bl.count > 1 ? stage_of(1) : cur;
-        load(cur);
-        bool plain = plain_stage(cur);
-        store(0, !plain);
-        __syncthreads();
-        for (int b = 0; b < bl.count; b++) {
-            const int buf = b & 1;
-            const Stage after = b + 2 < bl.count ? stage_of(b + 2) : next;
-            load(next);                                                     // (behind the last stage once more the same one)
-            const unsigned char *k0 = stages + buf * BUF, *v0 = k0 + SK * DH * 2;
-            const bool dirty = !plain && (odd_flag[buf][0] | odd_flag[buf][1] | odd_flag[buf][2] | odd_flag[buf][3]) != 0;
+            if (b_hi > b_lo) {
+                Stage cur = stage_of(b_lo), next = b_lo + 1 < b_hi ? stage_of(b_lo + 1) : cur;
+                load(cur);
+                bool plain = plain_stage(cur);
+                store(0, !plain);
+                __syncthreads();
+                for (int b = b_lo; b < b_hi; b++) {
+                    const int buf = (b - b_lo) & 1;
+                    const Stage after = b + 2 < b_hi ? stage_of(b + 2) : next;
+                    load(next);                                                     // (behind the last stage once more the same one)
+                    const unsigned char *k0 = stages + buf * BUF, *v0 = k0 + SK * DH * 2;
+                    const bool dirty = !plain && (odd_flag[buf][0] | odd_flag[buf][1] | odd_flag[buf][2] | odd_flag[buf][3]) != 0;
 #pragma unroll
-            for (int h = 0; h < SK / 32; h++) {
-                const int key0 = cur.key0 + 32 * h, pg0 = cur.page[2 * h], pg1 = cur.page[2 * h + 1];
-                // keys that none of this wave's rows sees
-                const bool none = idle || key0 >= rq.len || (a.causal && key0 > wmax) ||
-                                  (a.window && key0 >= a.sinks && (key0 + 31 <= wmin - a.window || key0 - wmax >= a.window));
-                if (none) continue;
-                const bool all = plain || (pg0 >= 0 && pg1 >= 0 && all_seen(a, rq.len, key0, 32, wmin, wmax));
-                const unsigned char *kb = k0 + 32 * h * DH * 2, *vb = v0 + 32 * h * DH * 2;
-                frag_t kf[2][KS];
+                    for (int h = 0; h < SK / 32; h++) {
+                        const int key0 = cur.key0 + 32 * h, pg0 = cur.page[2 * h], pg1 = cur.page[2 * h + 1];
+                        // keys that none of this wave's rows sees
+                        const bool none = idle || key0 >= rq.len || (a.causal && key0 > wmax) ||
+                                          (a.window && key0 >= a.sinks && (key0 + 31 <= wmin - a.window || key0 - wmax >= a.window));
+                        if (none) continue;
+                        const bool all = plain || (pg0 >= 0 && pg1 >= 0 && all_seen(a, rq.len, key0, 32, wmin, wmax));
+                        const unsigned char *kb = k0 + 32 * h * DH * 2, *vb = v0 + 32 * h * DH * 2;
+                        frag_t kf[2][KS];
 #pragma unroll
-                for (int s = 0; s < 2; s++)
+                        for (int s = 0; s < 2; s++)
 #pragma unroll
-                    for (int k = 0; k < KS; k++) kf[s][k] = *reinterpret_cast<const frag_t *>(kb + 16 * k_piece<DH>(16 * s + li, 4 * k + g));
-                f32x4 z[NT][2];
+                            for (int k = 0; k < KS; k++) kf[s][k] = *reinterpret_cast<const frag_t *>(kb + 16 * k_piece<DH>(16 * s + li, 4 * k + g));
+                        f32x4 z[NT][2];
 #pragma unroll
-                for (int t = 0; t < NT; t++)
+                        for (int t = 0; t < NT; t++)
 #pragma unroll
-                    for (int s = 0; s < 2; s++) {
-                        z[t][s] = f32x4{0.f, 0.f, 0.f, 0.f};
+                            for (int s = 0; s < 2; s++) {
+                                z[t][s] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                        for (int k = 0; k < KS; k++) z[t][s] = Num<T>::mfma(kf[s][k], q[t][k], z[t][s]);
+                                for (int k = 0; k < KS; k++) z[t][s] = Num<T>::mfma(kf[s][k], q[t][k], z[t][s]);
+                            }
+                        frag_t vt[CT];
+#pragma unroll
+                        for (int c = 0; c < CT; c++) vt[c] = v_operand<DH>(vb, lane, c);
+                        if (__builtin_expect(dirty, 0))
+#pragma unroll
+                            for (int c = 0; c < CT; c++) clear_odd<T>(vt[c]);
+#pragma unroll
+                        for (int t = 0; t < NT; t++) {
+                            if (!all) hide_unseen(z[t], sight[t], key0, g, pg0, pg1);
+                            const frag_t pf = probabilities<T, CT>(z[t], a.sc, ref[t], lsum[t], o[t]);
+                            if (__builtin_expect(dirty, 0))
+                                add_odd<T, DH>(vb, lane, pf, [&](int key) { return sees(sight[t], key0 + key, key & 16 ? pg1 : pg0); }, o[t]);
+                            lsum[t] = Num<T>::mfma(ones, pf, lsum[t]);
+#pragma unroll
+                            for (int c = 0; c < CT; c++) o[t][c] = Num<T>::mfma(vt[c], pf, o[t][c]);
+                        }
                     }
-                frag_t vt[CT];
-#pragma unroll
-                for (int c = 0; c < CT; c++) vt[c] = v_operand<DH>(vb, lane, c);
-                if (__builtin_expect(dirty, 0))
-#pragma unroll
-                    for (int c = 0; c < CT; c++) clear_odd<T>(vt[c]);
-#pragma unroll
-                for (int t = 0; t < NT; t++) {
-                    if (!all) hide_unseen(z[t], sight[t], key0, g, pg0, pg1);
-                    const frag_t pf = probabilities<T, CT>(z[t], a.sc, ref[t], lsum[t], o[t]);
-                    if (__builtin_expect(dirty, 0))
-                        add_odd<T, DH>(vb, lane, pf, [&](int key) { return sees(sight[t], key0 + key, key & 16 ? pg1 : pg0); }, o[t]);
-                    lsum[t] = Num<T>::mfma(ones, pf, lsum[t]);
-#pragma unroll
-                    for (int c = 0; c < CT; c++) o[t][c] = Num<T>::mfma(vt[c], pf, o[t][c]);
+                    plain = plain_stage(next);
+                    store(buf ^ 1, !plain);
+                    __syncthreads();
+                    cur = next;
+                    next = after;
                 }
             }
-            plain = plain_stage(next);
-            store(buf ^ 1, !plain);
-            __syncthreads();
-            cur = next;
-            next = after;
+            // ---- results, or sums for the joining kernel
+            int tid = threadIdx.x;                                                  // (hidden, as above)
+            asm volatile("" : "+v"(tid));
+            const int parts = whole ? 1 : (piece * x + (min(piece, total - piece * x) - left) - at + cost + nb - 1) / piece - x + 1;
+#pragma unroll
+            for (int t = 0; t < NT; t++) {
+                const int in_tile = wave * 16 * NT + t * 16 + (tid & 15), rho = tile * Shape::TILE_ROWS + in_tile, eg = (tid >> 4) & 3;
+                if (rho >= n_rows) continue;
+                const int i = rho / G, hq = head * G + (rho - i * G);
+                const float l = lsum[t][0];
+                if (!whole) {
+                    const long long place = ((2ll * x + (b_lo == 0)) * kv + head) * Shape::TILE_ROWS + in_tile;
+#pragma unroll
+                    for (int c = 0; c < CT; c++) *reinterpret_cast<f32x4 *>(a.partial + place * DH + c * 16 + 4 * eg) = o[t][c];
+                    if (eg == 0) {
+                        a.ml[place] = float2{ref[t].at, l};
+                        if (b_lo == 0) a.where[(size_t)(rq.row0 + i) * a.heads + hq] = int2{x, parts * kRowsPlace + in_tile};
+                    }
+                    continue;
+                }
+                const float f = l > 0.f ? 1.0f / l : l == 0.f ? 0.f : l;          // a row that sees nothing is zero
+#pragma unroll
+                for (int c = 0; c < CT; c++)
+                    store_out4(a, rq.row0 + i, hq, DH, c * 16 + 4 * eg, uint2{Num<T>::pack(o[t][c][0] * f, o[t][c][1] * f), Num<T>::pack(o[t][c][2] * f, o[t][c][3] * f)});
+                if (split && eg == 0) a.where[(size_t)(rq.row0 + i) * a.heads + hq] = int2{x, 0};
+            }
         }
-    }
-#pragma unroll
-    for (int t = 0; t < NT; t++) {
-        const int rho = rho0 + t * 16 + li;
-        if (rho >= n_rows) continue;
-        const int i = rho / G, hq = head * G + (rho - i * G);
-        const float l = lsum[t][0], f = l > 0.f ? 1.0f / l : l == 0.f ? 0.f : l;          // a row that sees nothing is zero
-#pragma unroll
-        for (int c = 0; c < CT; c++)
-            store_out4(a, rq.row0 + i, hq, DH, c * 16 + 4 * g, uint2{Num<T>::pack(o[t][c][0] * f, o[t][c][1] * f), Num<T>::pack(o[t][c][2] * f, o[t][c][3] * f)});
+        if (!split) return;
+        left -= end - at;
+        if (left <= 0) return;
+        at = 0;
+        if (++tile == tiles) {
+            do {
+                if (++request >= a.n) return;
+                rq = request_of(a, request);
+                tiles = tiles_of(a, rq, Shape::TILE_ROWS);
+            } while (tiles == 0);
+            tile = 0;
+        }
     }
 }
 
@@ -817,7 +937,7 @@ __global__ __launch_bounds__(WPR == 16 ? 1024 : 256) void paged_join_kernel(Page
         at = a.where[(size_t)row * a.heads + hq];
         mine = !a.cu_rows || (row >= a.cu_rows[0] && row < a.cu_rows[a.n]);
     }
-    const int parts = at.y >> 6, r = at.y & 63, kv = a.pages.n_kv_heads, head = hq / a.group;
+    const int parts = at.y / kRowsPlace, r = at.y % kRowsPlace, kv = a.pages.n_kv_heads, head = hq / a.group;
     mine = mine && parts > 1 && r < a.tile_rows && at.x >= 0 && (long long)at.x + parts <= a.split;
     auto place = [&](int p) { return ((size_t)(2ll * (at.x + p) + (p == 0)) * kv + head) * a.tile_rows + r; };
     float top = -INFINITY, total = 0.f, acc[V];
@@ -882,22 +1002,29 @@ __global__ __launch_bounds__(WPR == 16 ? 1024 : 256) void paged_join_kernel(Page
     store_out8(a, row, hq, DH, c, v);
 }
 
+template <class T, int DH>
+void launch_join(const PagedAttn &a, hipStream_t s) {
+    // parts of a row, where the lengths are equal
+    const long long units = (long long)a.rows * a.heads, parts = a.split / a.tiles;
+    if (parts > 16) paged_join_kernel<T, DH, 16><<<dim3((unsigned)units), 1024, 0, s>>>(a);
+    else if (parts > 4) paged_join_kernel<T, DH, 4><<<dim3((unsigned)units), 256, 0, s>>>(a);
+    else paged_join_kernel<T, DH, 1><<<dim3((unsigned)((units + 3) / 4)), 256, 0, s>>>(a);
+}
+
 template <class T, int DH, int NT>
 void launch_nt(const PagedAttn &a, hipStream_t s) {
     paged_attn_kernel<T, DH, NT><<<dim3((unsigned)(a.items * a.pages.n_kv_heads)), 256, 0, s>>>(a);
     if (!a.split) return;
-    // parts of a row, where the lengths are equal
-    const long long units = (long long)a.rows * a.heads, parts = a.split / max(1ll, min((long long)a.n, (long long)a.rows));
-    if (parts > 16) paged_join_kernel<T, DH, 16><<<dim3((unsigned)units), 1024, 0, s>>>(a);
-    else if (parts > 4) paged_join_kernel<T, DH, 4><<<dim3((unsigned)units), 256, 0, s>>>(a);
-    else paged_join_kernel<T, DH, 1><<<dim3((unsigned)((units + 3) / 4)), 256, 0, s>>>(a);
+    launch_join<T, DH>(a, s);
 }
 
 template <class T, int DH>
 void launch_rows(const PagedAttn &a, hipStream_t s) {
     constexpr int bytes = 2 * 2 * RowsShape<DH>::SK * DH * 2;
     allow_lds<paged_rows_kernel<T, DH>>(bytes);
+    if (a.split) paged_plan_kernel<DH><<<dim3(1), kPlanTiles, 0, s>>>(a);
     paged_rows_kernel<T, DH><<<dim3((unsigned)(a.items * a.pages.n_kv_heads)), 256, bytes, s>>>(a);
+    if (a.split) launch_join<T, DH>(a, s);
 }
 
 template <class T, int DH>
@@ -918,19 +1045,32 @@ void launch_type(const PagedAttn &a, int nt, hipStream_t s) {
 }
 
 inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
+inline int many_rows(const odb_pages &p) { return p.head_dim == 256 ? RowsShape<256>::TILE_ROWS : RowsShape<128>::TILE_ROWS; }
 
 }  // namespace
 
-void paged_attn_plan(const odb_pages &p, int n, int rows, int group, int max_rows, long long max_len, int *nt, int *split, long long *items) {
+void paged_attn_plan(const odb_pages &p, int n, int rows, int group, int max_rows, long long max_len, long long columns, int *nt, int *split,
+                     long long *items) {
     const long long most = (long long)max_rows * group;
     // Every request has at most one row tile that is not full.
     auto tiles = [&](int tile_rows) { return (long long)(n < rows ? n : rows) + (long long)rows * group / tile_rows; };
-    const int many = p.head_dim == 256 ? 64 : 128;
-    if (most >= many && tiles(many) * p.n_kv_heads >= 256) {
-        *nt = kManyRows;
-        *split = 0;
-        *items = tiles(many);
-        return;
+    // Full tiles of many rows: whole where there is one for every CU, or half as many that each see few keys; in pieces where fewer
+    // see long keys, 24 stages a piece at least.  Else the waves split the keys of smaller tiles.  Whole / pieces / keys split by waves, 32
+    // query heads over 8: 600 rows of 600 positions 28 / 37 / 47 us, 512 of 8192 272 / 115 / 134, 900 of 32000 1032 / 643 / 983, 256 of 2048
+    // 73 / 54 / 36, 128 of 8192 269 / 52 / 53; 32 heads over 32, 1024 of 1024 43 / 60 / 52.
+    const int many = many_rows(p), keys = p.head_dim == 256 ? RowsShape<256>::SK : RowsShape<128>::SK;
+    const long long groups = tiles(many) * p.n_kv_heads, stages = (max_len + keys - 1) / keys;
+    if (most >= many) {
+        const bool whole = groups >= 256 || (groups >= 128 && stages <= 12);
+        const int pieces = (256 * (p.head_dim == 256 ? 1 : 2) + p.n_kv_heads - 1) / p.n_kv_heads;
+        // (the plan's sums are 32-bit, by the tables' columns: max_len may not hold)
+        const bool fits = tiles(many) <= kPlanTiles && tiles(many) * (columns * p.page_size / keys + 8) < 1 << 30;
+        if (whole || (fits && tiles(many) * stages >= 24ll * pieces)) {
+            *nt = kManyRows;
+            *split = whole ? 0 : pieces;
+            *items = whole ? tiles(many) : pieces;
+            return;
+        }
     }
     *nt = most <= 16 ? 1 : most <= 32 || p.head_dim == 256 ? 2 : 4;
     // One round of workgroups.  Two per CU hide each other's starts and ends where a tile is 16 rows (64 single tokens over 555 MB:
@@ -944,19 +1084,22 @@ void paged_attn_plan(const odb_pages &p, int n, int rows, int group, int max_row
 
 size_t paged_attn_workspace(const odb_pages &p, int rows, int heads, int nt, int split) {
     if (!split) return 0;
-    const size_t tile_rows = 2 * (size_t)split * p.n_kv_heads * nt * 16;
-    return up256(tile_rows * p.head_dim * 4) + up256(tile_rows * 8) + up256((size_t)rows * heads * 8);
+    const size_t tile_rows = 2 * (size_t)split * p.n_kv_heads * (nt == kManyRows ? many_rows(p) : nt * 16);
+    return up256(tile_rows * p.head_dim * 4) + up256(tile_rows * 8) + up256((size_t)rows * heads * 8) + up256(((size_t)split + 1) * 16);
 }
 
 void launch_paged_attention(PagedAttn a, int nt, void *workspace, hipStream_t s) {
     if (a.rows < 1) return;
-    a.tile_rows = nt * 16;              // (of the kernel that can split keys)
+    a.tile_rows = nt == kManyRows ? many_rows(a.pages) : nt * 16;
+    a.tiles = (int)max(1ll, (long long)min(a.n, a.rows) + (long long)a.rows * a.group / a.tile_rows);
     if (a.split > 0) {
-        const size_t tile_rows = 2 * (size_t)a.split * a.pages.n_kv_heads * nt * 16;
+        const size_t tile_rows = 2 * (size_t)a.split * a.pages.n_kv_heads * a.tile_rows;
         char *w = (char *)workspace;
-        a.partial = (float *)w;
-        a.ml = (float2 *)(w + up256(tile_rows * a.pages.head_dim * 4));
-        a.where = (int2 *)((char *)a.ml + up256(tile_rows * 8));
+        auto take = [&](size_t bytes) { char *p = w; w += up256(bytes); return p; };
+        a.partial = (float *)take(tile_rows * a.pages.head_dim * 4);
+        a.ml = (float2 *)take(tile_rows * 8);
+        a.where = (int2 *)take((size_t)a.rows * a.heads * 8);
+        a.plan = (int4 *)take(((size_t)a.split + 1) * 16);
     }
     if (a.pages.dtype == ODB_F16) launch_type<_Float16>(a, nt, s);
     else launch_type<__bf16>(a, nt, s);

@@ -294,6 +294,32 @@ def test_many_rows(cache, dim, heads, kv, causal, window, sinks):
     rq.check(rq.run(causal=causal, window=window, sinks=sinks), causal=causal, window=window, sinks=sinks, oracle=plain.attention_many)
 
 
+@pytest.mark.parametrize("cache,dim,heads,kv", [("f16", 64, 16, 16), ("bf16", 128, 32, 32), ("f16", 256, 16, 16)])
+@pytest.mark.parametrize("causal,window,sinks", [(False, 0, 0), (True, 0, 0), (True, 900, 5), (False, 300, 70)])
+def test_many_rows_whose_keys_are_split_over_workgroups(cache, dim, heads, kv, causal, window, sinks):
+    """Few row tiles and long keys: pieces that begin and end inside tiles, tiles that see much less than others."""
+    rows, lens = [150, 0, 1, 129], [3500, 20, 1, 9000]
+    rq = Requests(dim + window + heads, rows, lens, heads, kv, dim, cache, 16)
+    cu = ints([0, 150, 150, 151, 280])                                     # rows that belong to no request stay
+    q = torch.cat([rq.q, rq.q[:20]]).cuda()
+    out = torch.full_like(q, 3.0)
+    B.odb_paged_attention(q, rq.k.cuda(), rq.v.cuda(), ints(rq.tables), ints(rq.lens), causal=causal, window=window, sinks=sinks, cu_rows=cu, out=out)
+    rq.check(out[:280], causal=causal, window=window, sinks=sinks, oracle=plain.attention_many)
+    assert (out[280:] == 3.0).all()
+
+
+@pytest.mark.parametrize("n", [250, 600])
+def test_split_rows_over_many_requests(n):
+    """Many requests, one or two of many rows, most of one or none; their tables are wide, which is what the way of computing goes by."""
+    rng = random.Random(8)
+    lens = [rng.choice([1, 5, 33, 70]) for _ in range(n)]
+    rows = [int(rng.random() < 20 / n) for _ in lens]
+    for r in (3, 177) if n == 250 else (599,):
+        lens[r], rows[r] = 1800 + r, 150
+    rq = Requests(77, rows, lens, 1, 1, 64, "f16", 16, extra_columns=900)
+    rq.check(rq.run(causal=True, max_rows=150), causal=True, oracle=plain.attention_many)
+
+
 def test_many_rows_at_given_positions_and_with_hidden_numbers():
     rows, lens, first = [200, 200, 130], [400, 250, 130], [150, -20, 100]
     rq = Requests(71, rows, lens, 64, 64, 64, "f16", 32)
