@@ -255,8 +255,9 @@ __device__ __forceinline__ frag_t probabilities(f32x4 (&z)[2], float sc, Referen
 }
 
 // Values of V that are infinite or no number must not reach a row that does not see their key, not even times zero.  In blocks
-// that not all rows see in full they are looked for; where there are any, they are added one by one to the rows that see them
-// (add_odd) and the product has zeros in their place (clear_odd).
+// that not all rows see in full, keys that no row sees (whatever lies behind the last position, or in no page of the pool) become
+// zero as they are loaded, and the others are looked at; where there are such values, they are added one by one to the rows that
+// see them (add_odd) and the product has zeros in their place (clear_odd).
 template <class T>
 __device__ __forceinline__ int has_odd(const frag_t &v) {
     int odd = 0;
@@ -493,7 +494,11 @@ __global__ __launch_bounds__(64 * NW, DH == 256 || NT == 4 ? 1 : 2) void paged_a
                     if (!plain) {
                         int odd = 0;
 #pragma unroll
-                        for (int j = 0; j < VL; j++) odd |= has_odd<T>(vf[j]);
+                        for (int j = 0; j < VL; j++) {
+                            const int key = key0 + (j < VL / 2 ? 0 : 16) + v_key + j % (VL / 2) * KEYS;
+                            if (!((int)(key < rq.len) & (int)((j < VL / 2 ? pg0 : pg1) >= 0))) vf[j] = frag_t{{0, 0, 0, 0}};
+                            odd |= has_odd<T>(vf[j]);
+                        }
                         dirty = __any(odd);
                     }
                     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -799,15 +804,18 @@ __global__ __launch_bounds__(256, DH == 256 ? 1 : 2) void paged_rows_kernel(Page
 #pragma unroll
                 for (int j = 0; j < LD; j++) vr[j] = ld_at<false>(vp + base + (size_t)(j * KEYS) * pos_stride, s_off);
             };
-            auto store = [&](int buf, bool look) {
+            auto store = [&](int buf, const Stage &s, bool look) {
                 unsigned char *k0 = stages + buf * BUF, *v0 = k0 + SK * DH * 2;
                 int odd = 0;
 #pragma unroll
                 for (int j = 0; j < LD; j++) {
                     const int key = WK * wave + s_key + j * KEYS;
+                    if (look) {
+                        if (!((int)(s.key0 + key < rq.len) & (int)(s.mine >= 0))) vr[j] = frag_t{{0, 0, 0, 0}};
+                        odd |= has_odd<T>(vr[j]);
+                    }
                     *reinterpret_cast<frag_t *>(k0 + 16 * k_piece<DH>(key, s_ch)) = kr[j];
                     *reinterpret_cast<frag_t *>(v0 + 16 * v_piece<DH>(key, s_ch)) = vr[j];
-                    if (look) odd |= has_odd<T>(vr[j]);
                 }
                 if (look) {
                     odd = __any(odd);
@@ -826,7 +834,7 @@ __global__ __launch_bounds__(256, DH == 256 ? 1 : 2) void paged_rows_kernel(Page
                 Stage cur = stage_of(b_lo), next = b_lo + 1 < b_hi ? stage_of(b_lo + 1) : cur;
                 load(cur);
                 bool plain = plain_stage(cur);
-                store(0, !plain);
+                store(0, cur, !plain);
                 __syncthreads();
                 for (int b = b_lo; b < b_hi; b++) {
                     const int buf = (b - b_lo) & 1;
@@ -875,7 +883,7 @@ __global__ __launch_bounds__(256, DH == 256 ? 1 : 2) void paged_rows_kernel(Page
                         }
                     }
                     plain = plain_stage(next);
-                    store(buf ^ 1, !plain);
+                    store(buf ^ 1, next, !plain);
                     __syncthreads();
                     cur = next;
                     next = after;
