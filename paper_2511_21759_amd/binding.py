@@ -523,13 +523,19 @@ def odb_page_tables(held, wanted, tables, free_pages, n_free, page_size: int, n_
         positions = held.new_empty((cap,))
     per = (n,)
     p_held = _ints("held", held, per, index, i32)
-    length, cu_rows, state = held.new_empty((2 * n + 5,)).split((n, n + 1, 4)) if out is None else out
+    if out is None:
+        own = held.new_empty((2 * n + 5,))
+        length, cu_rows, state = torch.split_with_sizes(own, (n, n + 1, 4))
+        p_len = own.data_ptr()
+        p_rows, p_state = p_len + 4 * n, p_len + 4 * (2 * n + 1)
+    else:
+        length, cu_rows, state = out
+        p_len, p_rows, p_state = _ints("len", length, per, index, i32), _ints("cu_rows", cu_rows, (n + 1,), index, i32), _ints("state", state, (4,), index, i32)
     _on(index, lib().odb_page_tables, p_held, _ints("wanted", wanted, per, index, i32), n, page_size, _ints("tables", tables, (n, columns), index, i32),
         columns, _ints("free_pages", free_pages, (n_pages,), index, i32), n_pages, _ints("n_free", n_free, (1,), index, i32),
         None if row_first is None else _ints("row_first", row_first, per, index, i32),
-        None if row_count is None else _ints("row_count", row_count, per, index, i32), _ints("len", length, per, index, i32),
-        _ints("cu_rows", cu_rows, (n + 1,), index, i32), _ints("slots", slots, (cap,), index, i32),
-        _ints("positions", positions, (cap,), index, i32), cap, _ints("state", state, (4,), index, i32))
+        None if row_count is None else _ints("row_count", row_count, per, index, i32), p_len, p_rows, _ints("slots", slots, (cap,), index, i32),
+        _ints("positions", positions, (cap,), index, i32), cap, p_state)
     return length, cu_rows, slots, positions, state
 
 
@@ -562,7 +568,9 @@ def odb_qk_norm_rope(q, k, v, k_pages, v_pages, table, positions, slots, q_gain=
     if k_pages.get_device() != index or dim != k_pages.shape[3] or dtype not in _DTYPES:
         raise TypeError("q and the pools must lie on one device and have heads of the same size, of float16, bfloat16 or float32")
     if out is None:
-        out = q.new_empty(shape, dtype=k_pages.dtype)
+        out, out_row = q.new_empty(shape, dtype=k_pages.dtype), heads * dim
+    else:
+        out_row = _head_rows("out", out, index, k_pages.dtype, shape)
     if table.dtype is not f32 or table.dim() != 3 or table.shape[2] != 2 or table.get_device() != index or not table.is_contiguous():
         raise TypeError("table must be a contiguous float32 tensor [n_pos, rot_dim / 2, 2] on the device of the others")
     for gain in (q_gain, k_gain):
@@ -572,7 +580,7 @@ def odb_qk_norm_rope(q, k, v, k_pages, v_pages, table, positions, slots, q_gain=
                       _head_rows("k", k, index, dtype, kv), _head_rows("v", v, index, dtype, kv), 0 if q_gain is None else q_gain.data_ptr(),
                       0 if k_gain is None else k_gain.data_ptr(), eps, table.data_ptr(), table.shape[0], 2 * table.shape[1], bool(interleaved),
                       _ints("positions", positions, (rows,), index, i32), _ints("slots", slots, (rows,), index, i32), out.data_ptr(),
-                      _head_rows("out", out, index, k_pages.dtype, shape))
+                      out_row)
     if rows:
         _on(index, lib().odb_qk_norm_rope, r, pages)
     return out
@@ -601,9 +609,12 @@ def odb_paged_attention(q, k_pages, v_pages, tables, kv_len, *, causal: bool, cu
     n, columns = tables.shape
     if cu_rows is None and rows != n:
         raise ValueError("without cu_rows every request has one row (%d rows, %d requests)" % (rows, n))
+    q_row = _head_rows("q", q, index, k_pages.dtype, shape)
     if out is None:
-        out = q.new_empty(shape)
-    fields = (q.data_ptr(), out.data_ptr(), _head_rows("q", q, index, k_pages.dtype, shape), _head_rows("out", out, index, q.dtype, shape),
+        out, out_row = q.new_empty(shape), heads * dim
+    else:
+        out_row = _head_rows("out", out, index, q.dtype, shape)
+    fields = (q.data_ptr(), out.data_ptr(), q_row, out_row,
               0 if cu_rows is None else _ints("cu_rows", cu_rows, (n + 1,), index, i32),
               0 if first_pos is None else _ints("first_pos", first_pos, (n,), index, i32), _ints("kv_len", kv_len, (n,), index, i32),
               _ints("tables", tables, (n, columns), index, i32), columns, n, rows, heads, dim ** -0.5 if scale is None else scale, bool(causal),
@@ -636,6 +647,8 @@ def odb_step_paged(model: int, tokens, k_pages, v_pages, tables, first_pos, kv_l
         raise TypeError("table must be a contiguous float32 tensor [n_pos, head_dim / 2, 2] on the device of the others")
     if tables.dim() != 2:
         _not_ints("tables", "[n, columns]")
+    if not 0 <= skip < b:
+        raise ValueError("skip=%d outside [0, %d)" % (skip, b))
     conf = argmax = unmask = None
     if head:
         conf, argmax = tokens.new_empty((n, b - skip), dtype=torch.float32), tokens.new_empty((n, b - skip))

@@ -432,7 +432,7 @@ __global__ __launch_bounds__(64 * NW, DH == 256 || NT == 4 ? 1 : 2) void paged_a
             Reference ref[NT];
 #pragma unroll
             for (int t = 0; t < NT; t++) {
-                    lsum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+                lsum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int c = 0; c < CT; c++) o[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
             }

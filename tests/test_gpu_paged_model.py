@@ -156,13 +156,15 @@ def test_refusals_and_a_batch_with_padding():
         assert torch.equal(before.nan_to_num(7.0), pg.k.nan_to_num(7.0))
         args = dict(tokens=ints(tokens), k_pages=pg.k, v_pages=pg.v, tables=tables, first_pos=ints([20, 0]), kv_len=ints([64, 0]), positions=positions,
                     slots=slots, table=pg.table)
-        for bad in (dict(k_pages=pg.k.bfloat16(), v_pages=pg.v.bfloat16()), dict(skip=16), dict(skip=3, tau=0.5), dict(max_len=-1),
+        for bad in (dict(k_pages=pg.k.bfloat16(), v_pages=pg.v.bfloat16()), dict(skip=3, tau=0.5), dict(max_len=-1),
                     dict(k_pages=pg.k[:, :, :2], v_pages=pg.v[:, :, :2])):
             with pytest.raises(B.OdbError):
                 B.odb_step_paged(model, **dict(args, **bad))
         for bad in (dict(tokens=ints(tokens[:1])), dict(k_pages=pg.k[0], v_pages=pg.v[0]), dict(table=pg.table[:, :8]), dict(slots=slots[:16])):
             with pytest.raises(TypeError):
                 B.odb_step_paged(model, **dict(args, **bad))
+        with pytest.raises(ValueError):
+            B.odb_step_paged(model, **dict(args, skip=16))
         assert B.lib().odb_step_paged(None, None, None, None) == -1
         B.odb_model_status(model)
     finally:
