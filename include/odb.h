@@ -471,7 +471,8 @@ int odb_rope_table(float *table_dev, int n_pos, int rot_dim, const odb_rope *rop
  *   q_out       dev [rows, n_heads, head_dim] of the pages' dtype, rows q_out_row elements apart; may be q itself
  *               (same dtype and stride), otherwise it must not overlap q, k or v
  * Requirements: buffers aligned to 16 bytes, row strides multiples of 8, rot_dim a multiple of 16 in [16, head_dim].
- * Asynchronous on `stream`.  rows = 0 launches nothing.  Errors: ODB_E_INVALID_ARG. */
+ * Asynchronous on `stream`.  rows = 0 launches nothing.  Errors: ODB_E_INVALID_ARG, also where rows * ceil((n_heads + 2 n_kv_heads)
+ * * head_dim / 1024) reaches 2^26. */
 typedef struct {
     const void *q, *k, *v;
     int in_dtype, rows, n_heads;
@@ -507,7 +508,8 @@ int odb_qk_norm_rope(const odb_qk_rows *rows, const odb_pages *pages, void *stre
  * Asynchronous on `stream`.  Errors: ODB_E_INVALID_ARG for NULL buffers, n outside [1, 4096], rows outside [0, 2^24] (0: nothing is
  * launched), n_heads no multiple of n_kv_heads, columns < 1, columns * page_size > 2^30, a scale that is not positive or, times
  * log2(e), not finite, window or sinks negative or above 2^30, a workspace that is too small, buffers not aligned to 16 bytes, row
- * strides that are no multiples of 8, out overlapping q, pools outside the requirements above. */
+ * strides that are no multiples of 8, out overlapping q, rows * n_heads above 2^30, pools
+ * outside the requirements above. */
 typedef struct {
     const void *q;
     void *out;

@@ -44,6 +44,11 @@ struct QkNormRope {
     long long q_out_row;
     odb_pages pages;
 };
+// head_dim / 16 lanes a head; rows times this, 64 threads each, is below 2^32
+inline int qk_waves_per_row(int heads, const odb_pages &p) {
+    const int per_wave = 64 / (p.head_dim / 16);
+    return (heads + 2 * p.n_kv_heads + per_wave - 1) / per_wave;
+}
 void launch_qk_norm_rope(const QkNormRope &a, hipStream_t s);
 
 struct PagedAttn {

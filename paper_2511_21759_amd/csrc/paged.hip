@@ -347,7 +347,7 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkNormRope a, int wav
 
 template <class TI, class TO, int DH>
 static void launch_rope_dim(const QkNormRope &a, hipStream_t s) {
-    const int per_wave = 64 / (DH / 16), wpr = (a.heads + 2 * a.pages.n_kv_heads + per_wave - 1) / per_wave;
+    const int wpr = qk_waves_per_row(a.heads, a.pages);
     const unsigned grid = (unsigned)(((long long)a.rows * wpr + 3) / 4);
     if (a.interleaved) qk_norm_rope_kernel<TI, TO, DH, true><<<dim3(grid), 256, 0, s>>>(a, wpr);
     else qk_norm_rope_kernel<TI, TO, DH, false><<<dim3(grid), 256, 0, s>>>(a, wpr);

@@ -83,7 +83,9 @@ int odb::plan_paged_attention(const odb_attention *a, const odb_pages *pages, bo
     p.rows_per_request = 1;
     const int max_rows = a->max_rows > 0 && a->max_rows < a->rows ? a->max_rows : a->rows;
     paged_attn_plan(*pages, a->n, a->rows, p.group, max_rows, a->max_len > 0 && a->max_len < most ? a->max_len : most, a->columns, &nt, &p.split, &p.items);
-    if (p.items * pages->n_kv_heads > 0x7fffffffll || (long long)a->rows * a->n_heads > 0x7fffffffll)
+    if (a->rows == 0) p.split = 0;                                     // nothing is launched, no workspace
+    // (a launch has fewer than 2^32 threads, 256 a workgroup; rows of a tile are counted in 32 bits, with room for a tile behind the last)
+    if (p.items * pages->n_kv_heads >= 1 << 24 || (long long)a->rows * a->n_heads > 1 << 30)
         return fail(ODB_E_INVALID_ARG, "%s: %d rows of %d heads are too many for one launch", who, a->rows, a->n_heads);
     return ODB_OK;
 }
@@ -168,7 +170,7 @@ int odb_qk_norm_rope(const odb_qk_rows *rows, const odb_pages *pages, void *stre
     const int dim = pages->head_dim, kv = pages->n_kv_heads;
     if (r.rows < 0 || r.rows > 1 << 24) return fail(ODB_E_INVALID_ARG, "%s: rows=%d outside [0, 2^24]", who, r.rows);
     if (r.n_heads < 1 || r.n_heads > 65536) return fail(ODB_E_INVALID_ARG, "%s: n_heads=%d", who, r.n_heads);
-    if ((long long)r.rows * (r.n_heads + 2ll * kv) > 0x7fffffffll) return fail(ODB_E_INVALID_ARG, "%s: %d rows of %d heads are too many for one launch", who, r.rows, r.n_heads);
+    if ((long long)r.rows * qk_waves_per_row(r.n_heads, *pages) >= 1 << 26) return fail(ODB_E_INVALID_ARG, "%s: %d rows of %d heads are too many for one launch", who, r.rows, r.n_heads);
     if (r.in_dtype != ODB_F32 && r.in_dtype != pages->dtype) return fail(ODB_E_INVALID_ARG, "%s: rows of dtype %d into pages of dtype %d", who, r.in_dtype, pages->dtype);
     if (!(rc = check_rows(who, "q", r.q, r.q_row, r.n_heads, dim)) && !(rc = check_rows(who, "k", r.k, r.k_row, kv, dim)) &&
         !(rc = check_rows(who, "v", r.v, r.v_row, kv, dim)))

@@ -113,6 +113,24 @@ def test_null_structures(lib):
     assert lib.odb_step_paged(None, None, ctypes.byref(pages()), None) == INVALID
 
 
+def test_launches_of_too_many_threads_are_refused(lib):
+    # a launch has fewer than 2^32 threads
+    size = lambda **kw: lib.odb_paged_attention_workspace(ctypes.byref(attention(rows=1 << 24, **kw)), ctypes.byref(pages()))        # noqa: E731
+    assert size(n_heads=64) == 0
+    for kw in (dict(n_heads=66), dict(n_heads=100), dict(n_heads=60, max_rows=1)):
+        assert size(**kw) == INVALID
+        assert b"too many for one launch" in lib.odb_last_error()
+    wide = dict(rows=1 << 24, n_heads=60, q_row=3840, q_out=1 << 30, q_out_row=3840)          # four waves a row
+    assert lib.odb_qk_norm_rope(ctypes.byref(qk_rows(**wide)), ctypes.byref(pages()), None) == INVALID
+    assert b"too many for one launch" in lib.odb_last_error()
+
+
+def test_no_rows_need_no_workspace(lib):
+    assert lib.odb_paged_attention_workspace(ctypes.byref(attention(columns=4000, rows=0)), ctypes.byref(pages())) == 0
+    assert lib.odb_paged_attention(ctypes.byref(attention(columns=4000, rows=0)), ctypes.byref(pages()), None) == 0
+    assert lib.odb_qk_norm_rope(ctypes.byref(qk_rows(rows=0)), ctypes.byref(pages()), None) == 0
+
+
 def test_workspace_grows_with_rows_and_is_none_for_short_keys(lib):
     size = lambda **kw: lib.odb_paged_attention_workspace(ctypes.byref(attention(**kw)), ctypes.byref(pages()))        # noqa: E731
     assert size(columns=8) == 0 and size(columns=4000, max_len=100) == 0
