@@ -279,7 +279,7 @@ __device__ __forceinline__ void clear_odd(frag_t &v) {
 // Where the 16-byte piece `c` of key row `key` lies in a block of V: pieces are exchanged inside 256 bytes so that the
 // 8-byte reads of eight neighbouring keys, 32 bytes of each, fall on all 64 banks.
 template <int DH>
-__device__ __forceinline__ int v_piece(int key, int c) {
+__host__ __device__ constexpr int v_piece(int key, int c) {
     return key * (DH / 8) + (DH == 64 ? c ^ (((key >> 1) & 3) << 1) : c ^ ((key & 7) << 1));
 }
 
@@ -307,14 +307,20 @@ __device__ __forceinline__ void add_odd(const unsigned char *v_block, int lane, 
 }
 
 // V^T of a 32-key block in operand order: a lane's channel is (lane & 15) of tile c, its keys 4 (lane >> 4) + 0..3 of each 16
+__device__ __forceinline__ frag_t v_operand_at(const unsigned char *p0, int keys16) {
+    typedef __attribute__((address_space(3))) s16x4 *lds_ptr;
+    const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)p0));
+    const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p0 + keys16)));
+    return frag_t{{lo.x, lo.y, hi.x, hi.y}};
+}
+template <int DH>
+__device__ __forceinline__ unsigned v_lane(int lane, int c) {             // bytes
+    const int li = lane & 15, row = 4 * (lane >> 4) + (li >> 2), at = 2 * c + ((li >> 1) & 1);
+    return 16 * v_piece<DH>(row, at) + 8 * (li & 1);
+}
 template <int DH>
 __device__ __forceinline__ frag_t v_operand(const unsigned char *v_block, int lane, int c) {
-    typedef const __attribute__((address_space(3))) s16x4 *lds_ptr;
-    const int li = lane & 15, row = 4 * (lane >> 4) + (li >> 2), at = 2 * c + ((li >> 1) & 1);
-    const unsigned char *p0 = v_block + 16 * v_piece<DH>(row, at) + 8 * (li & 1), *p1 = p0 + 16 * DH * 2;
-    const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(lds_ptr)p0));
-    const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(lds_ptr)p1));
-    return frag_t{{lo.x, lo.y, hi.x, hi.y}};
+    return v_operand_at(v_block + v_lane<DH>(lane, c), 16 * DH * 2);
 }
 
 // Load of 16 bytes at a scalar address plus a lane's offset.  STREAM: data that is read once, past the caches' replacement.
@@ -327,6 +333,16 @@ __device__ __forceinline__ frag_t ld_at(const u16 *uniform, unsigned lane_bytes)
     asm("" : "+s"(base));                                         // (keeps the sum of a scalar base and a 32-bit offset apart)
     const global_ptr p = (global_ptr)(base + lane_bytes);
     return __builtin_bit_cast(frag_t, STREAM ? __builtin_nontemporal_load(p) : *p);
+}
+
+// The same with the base in a buffer's description and one more scalar offset: no sums of addresses beside the load itself.  (The
+// offsets of a lane and of the wave together are below 2^30, and the description has no other bound.)
+typedef __amdgpu_buffer_rsrc_t rsrc_t;
+__device__ __forceinline__ rsrc_t rsrc_of(const u16 *base) {
+    return __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, 0x7fffffff, 0x00027000);
+}
+__device__ __forceinline__ frag_t ld_buffer(rsrc_t r, unsigned lane_bytes, unsigned wave_bytes) {
+    return __builtin_bit_cast(frag_t, __builtin_amdgcn_raw_buffer_load_b128(r, (int)lane_bytes, (int)wave_bytes, 0));
 }
 
 // the keys that a row at position p sees: lo .. hi - 1 and 0 .. stay - 1
@@ -353,6 +369,18 @@ __device__ __forceinline__ bool all_seen(const PagedAttn &a, int len, int key0, 
     const int last = key0 + n - 1;
     return last < len && (!a.causal || last <= pmin) && (!a.window || last < a.sinks || (key0 > pmax - a.window && last - pmin < a.window));
 }
+
+// Keys that some, or that all rows at positions pmin .. pmax see, as a Sight: is any, or every one, of n keys from key0 on among them?
+__device__ __forceinline__ Sight sight_of_some(const PagedAttn &a, int len, int pmin, int pmax) {
+    const Sight s = sight_of(a, len, pmin), e = sight_of(a, len, pmax);
+    return Sight{s.lo, e.hi, e.stay};
+}
+__device__ __forceinline__ Sight sight_of_all(const PagedAttn &a, int len, int pmin, int pmax) {
+    const Sight s = sight_of(a, len, pmin), e = sight_of(a, len, pmax);
+    return Sight{e.lo, s.hi, s.stay};
+}
+__device__ __forceinline__ bool any_of(const Sight &s, int key0, int n) { return (key0 < s.hi && key0 + n > s.lo) || key0 < s.stay; }
+__device__ __forceinline__ bool all_of(const Sight &s, int key0, int n) { return (key0 >= s.lo && key0 + n <= s.hi) || key0 + n <= s.stay; }
 
 // ---- few rows: the waves of a workgroup split the keys -----------------------------------------------------------------
 
@@ -644,7 +672,7 @@ struct RowsShape {
 };
 // Where piece c of a key of K lies: the 16 keys that one operand load reads fall on different banks.
 template <int DH>
-__device__ __forceinline__ int k_piece(int key, int c) {
+__host__ __device__ constexpr int k_piece(int key, int c) {
     return key * (DH / 8) + (DH == 64 ? c ^ ((key >> 1) & 7) : c ^ (key & 15));
 }
 
@@ -718,7 +746,7 @@ __global__ __launch_bounds__(256, DH == 256 ? 1 : 2) void paged_rows_kernel(Page
     constexpr int WK = SK / 4, KEYS = 512 / DH, LD = WK / KEYS;              // keys that a wave stages; per load; loads each of K and V
     constexpr int BUF = 2 * SK * DH * 2;                                    // bytes of a stage
     extern __shared__ __align__(16) unsigned char stages[];
-    __shared__ int odd_flag[2][4];
+    __shared__ __align__(4) unsigned char flags[2][4];                        // of a wave's part of a stage: 1 odd values, 2 in no page
 
     const int kv = a.pages.n_kv_heads, head = (int)(blockIdx.x % (unsigned)kv), x = (int)(blockIdx.x / (unsigned)kv);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, li = lane & 15;
@@ -755,7 +783,11 @@ __global__ __launch_bounds__(256, DH == 256 ? 1 : 2) void paged_rows_kernel(Page
     const int page_mask = (1 << a.page_shift) - 1;
     const size_t pos_stride = a.pages.pos_stride, page_stride = a.pages.page_stride;
     const int s_key = lane / (DH / 8), s_ch = lane % (DH / 8);
-    const unsigned s_off = 2u * (s_key * (unsigned)pos_stride + s_ch * 8);
+    const unsigned s_off = 2u * (s_key * (unsigned)pos_stride + s_ch * 8), s_step = 2u * KEYS * (unsigned)pos_stride;      // bytes
+    // Bytes of a stage where a lane writes and reads its pieces.  Those of other keys and channels differ from these by an exclusive or,
+    // which takes no register of its own, and a constant.
+    const unsigned k_put = 16 * k_piece<DH>(WK * wave + s_key, s_ch), v_put = SK * DH * 2 + 16 * v_piece<DH>(WK * wave + s_key, s_ch);
+    const unsigned k_get = 16 * k_piece<DH>(li, g), v_get = SK * DH * 2 + v_lane<DH>(lane, 0);
     for (;;) {
         const int n_rows = rq.m * G, rho0 = (tile * 4 + wave) * 16 * NT;
         int pmin, pmax, wmin, wmax;                                             // positions of the tile's rows and of this wave's
@@ -786,80 +818,74 @@ __global__ __launch_bounds__(256, DH == 256 ? 1 : 2) void paged_rows_kernel(Page
 #pragma unroll
                 for (int c = 0; c < CT; c++) o[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
             }
-            auto page_of = [&](int key) -> int {
-                const int id = key < rq.len ? ld_scalar(table, key >> a.page_shift) : -1;
-                return id >= 0 && id < a.pages.n_pages ? id : -1;
-            };
-            // pages of the 16-key tiles of a stage, and the one that holds the keys which this wave stages
-            struct Stage { int key0, page[SK / 16], mine; };
-            auto stage_of = [&](int b) {
-                Stage s;
-                s.key0 = block_key<SHIFT>(bl, b);
-#pragma unroll
-                for (int i = 0; i < SK / 16; i++) s.page[i] = page_of(s.key0 + 16 * i);
-                s.mine = page_of(s.key0 + WK * wave);
-                return s;
+            // Where the keys that this wave stages lie, of 64 stages from `base` on, a stage per lane: elements from the head's part of
+            // the pool on, -1 for keys of no page.
+            long long places;
+            auto find_places = [&](int base) {
+                const int b = base + lane, key = block_key<SHIFT>(bl, b) + WK * wave;
+                int id = -1;
+                if (b < b_hi && key < rq.len) id = table[key >> a.page_shift];
+                places = id >= 0 && id < a.pages.n_pages ? id * (long long)page_stride + (key & page_mask) * (long long)pos_stride : -1;
+                asm volatile("" : "+v"(places));                                // (the wait for the table is here, not in every stage)
             };
             frag_t kr[LD], vr[LD];
-            auto load = [&](const Stage &s) {
-                const size_t base = (size_t)max(s.mine, 0) * page_stride + (size_t)((s.key0 + WK * wave) & page_mask) * pos_stride;
+            auto load = [&](int b) -> bool {
+                const int i = (b - b_lo) & 63, hi = __builtin_amdgcn_readlane((int)(places >> 32), i);
+                const unsigned lo = (unsigned)__builtin_amdgcn_readlane((int)places, i);
+                const size_t at = hi < 0 ? 0 : (size_t)hi << 32 | lo;
+                const rsrc_t k_src = rsrc_of(kp + at), v_src = rsrc_of(vp + at);
 #pragma unroll
-                for (int j = 0; j < LD; j++) kr[j] = ld_at<false>(kp + base + (size_t)(j * KEYS) * pos_stride, s_off);
+                for (int j = 0; j < LD; j++) kr[j] = ld_buffer(k_src, s_off, j * s_step);
 #pragma unroll
-                for (int j = 0; j < LD; j++) vr[j] = ld_at<false>(vp + base + (size_t)(j * KEYS) * pos_stride, s_off);
+                for (int j = 0; j < LD; j++) vr[j] = ld_buffer(v_src, s_off, j * s_step);
+                return hi >= 0;
             };
-            auto store = [&](int buf, const Stage &s, bool look) {
-                unsigned char *k0 = stages + buf * BUF, *v0 = k0 + SK * DH * 2;
+            // `plain`: every row of the tile sees every key of the stage, as far as there is a page
+            auto store = [&](int buf, int key0, bool there, bool plain) {
+                unsigned k_at = k_put + buf * BUF, v_at = v_put + buf * BUF;
+                asm volatile("" : "+v"(k_at), "+v"(v_at));
                 int odd = 0;
+                const bool look = !plain || !there;
 #pragma unroll
                 for (int j = 0; j < LD; j++) {
-                    const int key = WK * wave + s_key + j * KEYS;
                     if (look) {
-                        if (!((int)(s.key0 + key < rq.len) & (int)(s.mine >= 0))) vr[j] = frag_t{{0, 0, 0, 0}};
+                        if (!((int)(key0 + WK * wave + s_key + j * KEYS < rq.len) & (int)there)) vr[j] = frag_t{{0, 0, 0, 0}};
                         odd |= has_odd<T>(vr[j]);
                     }
-                    *reinterpret_cast<frag_t *>(k0 + 16 * k_piece<DH>(key, s_ch)) = kr[j];
-                    *reinterpret_cast<frag_t *>(v0 + 16 * v_piece<DH>(key, s_ch)) = vr[j];
+                    constexpr int P = KEYS * DH / 8;                            // (pieces of the keys of a load)
+                    const int k_turn = 16 * (k_piece<DH>(j * KEYS, 0) - j * P), v_turn = 16 * (v_piece<DH>(j * KEYS, 0) - j * P);
+                    *reinterpret_cast<frag_t *>(stages + 16 * j * P + (k_at ^ k_turn)) = kr[j];
+                    *reinterpret_cast<frag_t *>(stages + 16 * j * P + (v_at ^ v_turn)) = vr[j];
                 }
-                if (look) {
-                    odd = __any(odd);
-                    if (lane == 0) odd_flag[buf][wave] = odd;
-                }
+                odd = look && __any(odd);
+                if (lane == 0) flags[buf][wave] = (unsigned char)(odd | (there ? 0 : 2));
             };
-            // does every row of the tile see every key of the stage?
-            auto plain_stage = [&](const Stage &s) {
-                bool there = true;
-#pragma unroll
-                for (int i = 0; i < SK / 16; i++) there = there && s.page[i] >= 0;
-                return there && all_seen(a, rq.len, s.key0, SK, pmin, pmax);
-            };
+            const Sight tile_all = sight_of_all(a, rq.len, pmin, pmax), all = sight_of_all(a, rq.len, wmin, wmax);
+            const Sight some = idle ? Sight{0, 0, 0} : sight_of_some(a, rq.len, wmin, wmax);
 
             if (b_hi > b_lo) {
-                Stage cur = stage_of(b_lo), next = b_lo + 1 < b_hi ? stage_of(b_lo + 1) : cur;
-                load(cur);
-                bool plain = plain_stage(cur);
-                store(0, cur, !plain);
+                find_places(b_lo);
+                int key0 = block_key<SHIFT>(bl, b_lo);
+                bool there = load(b_lo), plain = all_of(tile_all, key0, SK);
+                store(0, key0, there, plain);
                 __syncthreads();
                 for (int b = b_lo; b < b_hi; b++) {
-                    const int buf = (b - b_lo) & 1;
-                    const Stage after = b + 2 < b_hi ? stage_of(b + 2) : next;
-                    load(next);                                                     // (behind the last stage once more the same one)
-                    const unsigned char *k0 = stages + buf * BUF, *v0 = k0 + SK * DH * 2;
-                    const bool dirty = !plain && (odd_flag[buf][0] | odd_flag[buf][1] | odd_flag[buf][2] | odd_flag[buf][3]) != 0;
+                    const int buf = (b - b_lo) & 1, next = min(b + 1, b_hi - 1);      // (behind the last stage once more the same one)
+                    if (next > b && ((next - b_lo) & 63) == 0) find_places(next);
+                    there = load(next);
+                    unsigned k_at = k_get + buf * BUF, v_at = v_get + buf * BUF;
+                    asm volatile("" : "+v"(k_at), "+v"(v_at));
+                    const uint32_t flag_word = *reinterpret_cast<const uint32_t *>(flags[buf]);
 #pragma unroll
                     for (int h = 0; h < SK / 32; h++) {
-                        const int key0 = cur.key0 + 32 * h, pg0 = cur.page[2 * h], pg1 = cur.page[2 * h + 1];
-                        // keys that none of this wave's rows sees
-                        const bool none = idle || key0 >= rq.len || (a.causal && key0 > wmax) ||
-                                          (a.window && key0 >= a.sinks && (key0 + 31 <= wmin - a.window || key0 - wmax >= a.window));
-                        if (none) continue;
-                        const bool all = plain || (pg0 >= 0 && pg1 >= 0 && all_seen(a, rq.len, key0, 32, wmin, wmax));
-                        const unsigned char *kb = k0 + 32 * h * DH * 2, *vb = v0 + 32 * h * DH * 2;
+                        const int key32 = key0 + 32 * h;
+                        if (!any_of(some, key32, 32)) continue;
+                        const unsigned char *block = stages + 32 * h * DH * 2;
                         frag_t kf[2][KS];
 #pragma unroll
                         for (int s = 0; s < 2; s++)
 #pragma unroll
-                            for (int k = 0; k < KS; k++) kf[s][k] = *reinterpret_cast<const frag_t *>(kb + 16 * k_piece<DH>(16 * s + li, 4 * k + g));
+                            for (int k = 0; k < KS; k++) kf[s][k] = *reinterpret_cast<const frag_t *>(block + 16 * s * DH * 2 + (k_at ^ (unsigned)(k << 6)));
                         f32x4 z[NT][2];
 #pragma unroll
                         for (int t = 0; t < NT; t++)
@@ -871,26 +897,30 @@ __global__ __launch_bounds__(256, DH == 256 ? 1 : 2) void paged_rows_kernel(Page
                             }
                         frag_t vt[CT];
 #pragma unroll
-                        for (int c = 0; c < CT; c++) vt[c] = v_operand<DH>(vb, lane, c);
+                        for (int c = 0; c < CT; c++) vt[c] = v_operand_at(block + (v_at ^ (unsigned)(c << 5)), 16 * DH * 2);
+                        // (a 16-key tile lies in one page; its flags are those of the first wave that stages it)
+                        const uint32_t fl = (uint32_t)__builtin_amdgcn_readfirstlane((int)flag_word);
+                        const bool dirty = (fl & 0x01010101u) != 0;
+                        const int pg0 = -(int)(fl >> (8 * (2 * h * 16 / WK)) & 2), pg1 = -(int)(fl >> (8 * ((2 * h + 1) * 16 / WK)) & 2);
+                        const bool masked = (pg0 | pg1) != 0 || !(plain || all_of(all, key32, 32));
                         if (__builtin_expect(dirty, 0))
 #pragma unroll
                             for (int c = 0; c < CT; c++) clear_odd<T>(vt[c]);
 #pragma unroll
                         for (int t = 0; t < NT; t++) {
-                            if (!all) hide_unseen(z[t], sight[t], key0, g, pg0, pg1);
+                            if (masked) hide_unseen(z[t], sight[t], key32, g, pg0, pg1);
                             const frag_t pf = probabilities<T, CT>(z[t], a.sc, ref[t], lsum[t], o[t]);
                             if (__builtin_expect(dirty, 0))
-                                add_odd<T, DH>(vb, lane, pf, [&](int key) { return sees(sight[t], key0 + key, key & 16 ? pg1 : pg0); }, o[t]);
+                                add_odd<T, DH>(block + buf * BUF + SK * DH * 2, lane, pf, [&](int key) { return sees(sight[t], key32 + key, key & 16 ? pg1 : pg0); }, o[t]);
                             lsum[t] = Num<T>::mfma(ones, pf, lsum[t]);
 #pragma unroll
                             for (int c = 0; c < CT; c++) o[t][c] = Num<T>::mfma(vt[c], pf, o[t][c]);
                         }
                     }
-                    plain = plain_stage(next);
-                    store(buf ^ 1, next, !plain);
+                    key0 = block_key<SHIFT>(bl, next);
+                    plain = all_of(tile_all, key0, SK);
+                    store(buf ^ 1, key0, there, plain);
                     __syncthreads();
-                    cur = next;
-                    next = after;
                 }
             }
             // ---- results, or sums for the joining kernel
