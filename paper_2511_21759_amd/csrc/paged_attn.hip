@@ -225,34 +225,45 @@ __device__ __forceinline__ void store_out4(const PagedAttn &a, int row, int head
 
 // ---- pieces of the loops ----------------------------------------------------------------------------------------------
 
-// Probabilities of 32 keys for a row tile from its scores z (keys that are not seen: -infinity), as the operand of the product
+// Probabilities of 32 keys for NT row tiles from their scores z (keys that are not seen: -infinity), as the operand of the product
 // with V; the reference is raised, and sums and O rescaled, where a score passes it by too much.  It is common to the four lanes of
 // a row and only has to keep exp2 in range, so after the first blocks that is rare, and the common path has no exchange of lanes.
-template <class T, int CT>
-__device__ __forceinline__ frag_t probabilities(f32x4 (&z)[2], float sc, Reference &ref, f32x4 &lsum, f32x4 (&o)[CT]) {
-    float top = -INFINITY;
+template <class T, int CT, int NT>
+__device__ __forceinline__ void probabilities(f32x4 (*z)[2], float sc, Reference *ref, f32x4 *lsum, f32x4 (*o)[CT], frag_t *pf) {
+    float top[NT];
+    int over = 0;
 #pragma unroll
-    for (int s = 0; s < 2; s++)
+    for (int t = 0; t < NT; t++) {
+        top[t] = -INFINITY;
 #pragma unroll
-        for (int e = 0; e < 4; e++) top = fmaxf(top, z[s][e]);
-    if (__any(top > ref.limit)) {
-        top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32));
-        const float up = fmaxf(ref.at, top * sc - kShift), f = __builtin_amdgcn_exp2f(ref.at - up);
-        lsum *= f;
+        for (int s = 0; s < 2; s++)
 #pragma unroll
-        for (int c = 0; c < CT; c++) o[c] *= f;
-        ref.at = up;
-        ref.limit = (up + kRaise) / sc;
+            for (int e = 0; e < 4; e++) top[t] = fmaxf(top[t], z[t][s][e]);
+        over |= (int)(top[t] > ref[t].limit);
     }
-    float p[2][4];
+    if (__any(over))                            // (one branch for all row tiles)
 #pragma unroll
-    for (int s = 0; s < 2; s++)
+        for (int t = 0; t < NT; t++) {
+            float m = fmaxf(top[t], __shfl_xor(top[t], 16));
+            m = fmaxf(m, __shfl_xor(m, 32));
+            const float up = fmaxf(ref[t].at, m * sc - kShift), f = __builtin_amdgcn_exp2f(ref[t].at - up);
+            lsum[t] *= f;
 #pragma unroll
-        for (int e = 0; e < 4; e++) p[s][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[s][e], sc, -ref.at));
+            for (int c = 0; c < CT; c++) o[t][c] *= f;
+            ref[t].at = up;
+            ref[t].limit = (up + kRaise) / sc;
+        }
     // Probabilities are rounded to the type of V for the matrix cores; the sum that divides them at the end is that of the
     // rounded ones, so what equal rounding errors have in common drops out.
-    return frag_t{{Num<T>::pack(p[0][0], p[0][1]), Num<T>::pack(p[0][2], p[0][3]), Num<T>::pack(p[1][0], p[1][1]), Num<T>::pack(p[1][2], p[1][3])}};
+#pragma unroll
+    for (int t = 0; t < NT; t++) {
+        float p[2][4];
+#pragma unroll
+        for (int s = 0; s < 2; s++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) p[s][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[t][s][e], sc, -ref[t].at));
+        pf[t] = frag_t{{Num<T>::pack(p[0][0], p[0][1]), Num<T>::pack(p[0][2], p[0][3]), Num<T>::pack(p[1][0], p[1][1]), Num<T>::pack(p[1][2], p[1][3])}};
+    }
 }
 
 // Values of V that are infinite or no number must not reach a row that does not see their key, not even times zero.  In blocks
@@ -554,7 +565,8 @@ __global__ __launch_bounds__(64 * NW, DH == 256 || NT == 4 ? 1 : 2) void paged_a
                         if (NT > 1 && t + 2 == NT) load_k(base0, base1, k_next);
                         f32x4 (&z)[2] = st[t & 1];
                         if (!plain) hide_unseen(z, sight[t], key0, g, pg0, pg1);
-                        const frag_t pf = probabilities<T, CT>(z, a.sc, ref[t], lsum[t], o[t]);
+                        frag_t pf;
+                        probabilities<T, CT, 1>(st + (t & 1), a.sc, ref + t, lsum + t, o + t, &pf);
                         if (__builtin_expect(dirty, 0)) {
                             add_odd<T, DH>(mine, lane, pf, [&](int key) { return sees(sight[t], key0 + key, key & 16 ? pg1 : pg0); }, o[t]);
                             if (NT == 1) {
@@ -664,8 +676,9 @@ __global__ __launch_bounds__(64 * NW, DH == 256 || NT == 4 ? 1 : 2) void paged_a
 
 // Stages of SK keys, K and V, are loaded through registers into one of two LDS buffers while the other is worked on, one barrier
 // per stage; a wave holds NT row tiles for all keys, so nothing has to be merged at the end.  Bound by the matrix cores and the vector
-// ALU together: 32 keys of a row tile are 17 MFMAs of 16 cycles, and 8 exponentials of 16 and about 20 other instructions of 4.  Four
-// requests of 4096 rows at 8192 positions, 32 query heads over 8 of 128, take 1.95 ms causal (850 TFLOP/s).
+// ALU together, which hardly overlap: 32 keys of a row tile are 17 MFMAs of 16 cycles, and 8 exponentials of 16 and about 20 other
+// instructions of 4.  Four requests of 4096 rows at 8192 positions, 32 query heads over 8 of 128, take 1.68 ms causal (982 TFLOP/s),
+// 2.21 full (995; a library product reaches 1240).
 template <int DH>
 struct RowsShape {
     static constexpr int NT = DH == 256 ? 1 : 2, TILE_ROWS = 64 * NT, SHIFT = DH == 256 ? 5 : 6, SK = 1 << SHIFT;
@@ -740,12 +753,12 @@ __global__ __launch_bounds__(kPlanTiles) void paged_plan_kernel(PagedAttn a) {
 }
 
 template <class T, int DH>
-__global__ __launch_bounds__(256, DH == 256 ? 1 : 2) void paged_rows_kernel(PagedAttn a) {
+__global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void paged_rows_kernel(PagedAttn a) {
     typedef RowsShape<DH> Shape;
     constexpr int NT = Shape::NT, SK = Shape::SK, SHIFT = Shape::SHIFT, KS = DH / 32, CT = DH / 16;
     constexpr int WK = SK / 4, KEYS = 512 / DH, LD = WK / KEYS;              // keys that a wave stages; per load; loads each of K and V
     constexpr int BUF = 2 * SK * DH * 2;                                    // bytes of a stage
-    extern __shared__ __align__(16) unsigned char stages[];
+    extern __shared__ __align__(1024) unsigned char stages[];
     __shared__ __align__(4) unsigned char flags[2][4];                        // of a wave's part of a stage: 1 odd values, 2 in no page
 
     const int kv = a.pages.n_kv_heads, head = (int)(blockIdx.x % (unsigned)kv), x = (int)(blockIdx.x / (unsigned)kv);
@@ -784,10 +797,13 @@ __global__ __launch_bounds__(256, DH == 256 ? 1 : 2) void paged_rows_kernel(Page
     const size_t pos_stride = a.pages.pos_stride, page_stride = a.pages.page_stride;
     const int s_key = lane / (DH / 8), s_ch = lane % (DH / 8);
     const unsigned s_off = 2u * (s_key * (unsigned)pos_stride + s_ch * 8), s_step = 2u * KEYS * (unsigned)pos_stride;      // bytes
-    // Bytes of a stage where a lane writes and reads its pieces.  Those of other keys and channels differ from these by an exclusive or,
-    // which takes no register of its own, and a constant.
-    const unsigned k_put = 16 * k_piece<DH>(WK * wave + s_key, s_ch), v_put = SK * DH * 2 + 16 * v_piece<DH>(WK * wave + s_key, s_ch);
-    const unsigned k_get = 16 * k_piece<DH>(li, g), v_get = SK * DH * 2 + v_lane<DH>(lane, 0);
+    // LDS addresses of the first stage where a lane writes and reads its pieces.  Those of other keys and channels differ from these by an
+    // exclusive or, which takes no register of its own, and a constant.
+    typedef __attribute__((address_space(3))) unsigned char *lds_bytes;
+    const unsigned lds0 = (unsigned)(uintptr_t)(lds_bytes)stages;               // (a multiple of the keys' size)
+    auto lds_frag = [](unsigned at, int more) { return (frag_t *)((lds_bytes)(uintptr_t)at + more); };
+    const unsigned k_put = lds0 + 16 * k_piece<DH>(WK * wave + s_key, s_ch), v_put = lds0 + SK * DH * 2 + 16 * v_piece<DH>(WK * wave + s_key, s_ch);
+    const unsigned k_get = lds0 + 16 * k_piece<DH>(li, g), v_get = lds0 + SK * DH * 2 + v_lane<DH>(lane, 0);
     for (;;) {
         const int n_rows = rq.m * G, rho0 = (tile * 4 + wave) * 16 * NT;
         int pmin, pmax, wmin, wmax;                                             // positions of the tile's rows and of this wave's
@@ -854,8 +870,8 @@ __global__ __launch_bounds__(256, DH == 256 ? 1 : 2) void paged_rows_kernel(Page
                     }
                     constexpr int P = KEYS * DH / 8;                            // (pieces of the keys of a load)
                     const int k_turn = 16 * (k_piece<DH>(j * KEYS, 0) - j * P), v_turn = 16 * (v_piece<DH>(j * KEYS, 0) - j * P);
-                    *reinterpret_cast<frag_t *>(stages + 16 * j * P + (k_at ^ k_turn)) = kr[j];
-                    *reinterpret_cast<frag_t *>(stages + 16 * j * P + (v_at ^ v_turn)) = vr[j];
+                    *lds_frag(k_at ^ k_turn, 16 * j * P) = kr[j];
+                    *lds_frag(v_at ^ v_turn, 16 * j * P) = vr[j];
                 }
                 odd = look && __any(odd);
                 if (lane == 0) flags[buf][wave] = (unsigned char)(odd | (there ? 0 : 2));
@@ -885,7 +901,7 @@ __global__ __launch_bounds__(256, DH == 256 ? 1 : 2) void paged_rows_kernel(Page
 #pragma unroll
                         for (int s = 0; s < 2; s++)
 #pragma unroll
-                            for (int k = 0; k < KS; k++) kf[s][k] = *reinterpret_cast<const frag_t *>(block + 16 * s * DH * 2 + (k_at ^ (unsigned)(k << 6)));
+                            for (int k = 0; k < KS; k++) kf[s][k] = *lds_frag(k_at ^ (unsigned)(k << 6), (32 * h + 16 * s) * DH * 2);
                         f32x4 z[NT][2];
 #pragma unroll
                         for (int t = 0; t < NT; t++)
@@ -897,7 +913,7 @@ __global__ __launch_bounds__(256, DH == 256 ? 1 : 2) void paged_rows_kernel(Page
                             }
                         frag_t vt[CT];
 #pragma unroll
-                        for (int c = 0; c < CT; c++) vt[c] = v_operand_at(block + (v_at ^ (unsigned)(c << 5)), 16 * DH * 2);
+                        for (int c = 0; c < CT; c++) vt[c] = v_operand_at((const unsigned char *)lds_frag(v_at ^ (unsigned)(c << 5), 32 * h * DH * 2), 16 * DH * 2);
                         // (a 16-key tile lies in one page; its flags are those of the first wave that stages it)
                         const uint32_t fl = (uint32_t)__builtin_amdgcn_readfirstlane((int)flag_word);
                         const bool dirty = (fl & 0x01010101u) != 0;
@@ -906,15 +922,20 @@ __global__ __launch_bounds__(256, DH == 256 ? 1 : 2) void paged_rows_kernel(Page
                         if (__builtin_expect(dirty, 0))
 #pragma unroll
                             for (int c = 0; c < CT; c++) clear_odd<T>(vt[c]);
+                        if (masked)
+#pragma unroll
+                            for (int t = 0; t < NT; t++) hide_unseen(z[t], sight[t], key32, g, pg0, pg1);
+                        frag_t pf[NT];
+                        probabilities<T, CT, NT>(z, a.sc, ref, lsum, o, pf);
+                        if (__builtin_expect(dirty, 0))
+#pragma unroll
+                            for (int t = 0; t < NT; t++)
+                                add_odd<T, DH>(block + buf * BUF + SK * DH * 2, lane, pf[t], [&](int key) { return sees(sight[t], key32 + key, key & 16 ? pg1 : pg0); }, o[t]);
 #pragma unroll
                         for (int t = 0; t < NT; t++) {
-                            if (masked) hide_unseen(z[t], sight[t], key32, g, pg0, pg1);
-                            const frag_t pf = probabilities<T, CT>(z[t], a.sc, ref[t], lsum[t], o[t]);
-                            if (__builtin_expect(dirty, 0))
-                                add_odd<T, DH>(block + buf * BUF + SK * DH * 2, lane, pf, [&](int key) { return sees(sight[t], key32 + key, key & 16 ? pg1 : pg0); }, o[t]);
-                            lsum[t] = Num<T>::mfma(ones, pf, lsum[t]);
+                            lsum[t] = Num<T>::mfma(ones, pf[t], lsum[t]);
 #pragma unroll
-                            for (int c = 0; c < CT; c++) o[t][c] = Num<T>::mfma(vt[c], pf, o[t][c]);
+                            for (int c = 0; c < CT; c++) o[t][c] = Num<T>::mfma(vt[c], pf[t], o[t][c]);
                         }
                     }
                     key0 = block_key<SHIFT>(bl, next);
