@@ -1125,11 +1125,13 @@ void paged_attn_plan(const odb_pages &p, int n, int rows, int group, int max_row
     const int many = many_rows(p), keys = p.head_dim == 256 ? RowsShape<256>::SK : RowsShape<128>::SK;
     const long long groups = tiles(many) * p.n_kv_heads, stages = (max_len + keys - 1) / keys;
     if (most >= many) {
-        const bool whole = groups >= 256 || (groups >= 128 && stages <= 12);
-        const int pieces = (256 * (p.head_dim == 256 ? 1 : 2) + p.n_kv_heads - 1) / p.n_kv_heads;
+        // more of the smaller tiles than CUs
+        const bool crowded = (long long)rows * group / (many / 2) * p.n_kv_heads > 256;
+        const bool whole = groups >= 256 || (crowded && stages <= 32) || (groups >= 128 && stages <= 12);
+        const int pieces = (512 + p.n_kv_heads - 1) / p.n_kv_heads;
         // (the plan's sums are 32-bit, by the tables' columns: max_len may not hold)
         const bool fits = tiles(many) <= kPlanTiles && tiles(many) * (columns * p.page_size / keys + 8) < 1 << 30;
-        if (whole || (fits && tiles(many) * stages >= 24ll * pieces)) {
+        if (whole || (fits && tiles(many) * stages >= (crowded ? 12ll : 20ll) * pieces)) {
             *nt = kManyRows;
             *split = whole ? 0 : pieces;
             *items = whole ? tiles(many) : pieces;
