@@ -82,7 +82,12 @@ int odb::plan_paged_attention(const odb_attention *a, const odb_pages *pages, bo
     p.page_shift = page_shift(pages->page_size);
     p.rows_per_request = 1;
     const int max_rows = a->max_rows > 0 && a->max_rows < a->rows ? a->max_rows : a->rows;
-    paged_attn_plan(*pages, a->n, a->rows, p.group, max_rows, a->max_len > 0 && a->max_len < most ? a->max_len : most, a->columns, &nt, &p.split, &p.items);
+    long long max_len = a->max_len > 0 && a->max_len < most ? a->max_len : most;
+    if (a->window) {                                                   // what the rows of a request see together
+        const long long seen = (a->causal ? 1ll : 2ll) * a->window + a->sinks + max_rows;
+        max_len = seen < max_len ? seen : max_len;
+    }
+    paged_attn_plan(*pages, a->n, a->rows, p.group, max_rows, max_len, a->columns, &nt, &p.split, &p.items);
     if (a->rows == 0) p.split = 0;                                     // nothing is launched, no workspace
     // (a launch has fewer than 2^32 threads, 256 a workgroup; rows of a tile are counted in 32 bits, with room for a tile behind the last)
     if (p.items * pages->n_kv_heads >= 1 << 24 || (long long)a->rows * a->n_heads > 1 << 30)

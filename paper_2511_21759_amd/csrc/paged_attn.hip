@@ -1118,20 +1118,26 @@ void paged_attn_plan(const odb_pages &p, int n, int rows, int group, int max_row
     const long long most = (long long)max_rows * group;
     // Every request has at most one row tile that is not full.
     auto tiles = [&](int tile_rows) { return (long long)(n < rows ? n : rows) + (long long)rows * group / tile_rows; };
-    // Full tiles of many rows: whole where there is one for every CU, or half as many that each see few keys; in pieces where fewer
-    // see long keys, 24 stages a piece at least.  Else the waves split the keys of smaller tiles.  Whole / pieces / keys split by waves, 32
-    // query heads over 8: 600 rows of 600 positions 28 / 37 / 47 us, 512 of 8192 272 / 115 / 134, 900 of 32000 1032 / 643 / 983, 256 of 2048
-    // 73 / 54 / 36, 128 of 8192 269 / 52 / 53; 32 heads over 32, 1024 of 1024 43 / 60 / 52.
+    // Tiles of many rows, where more than half of one is full: whole if there is one for every CU, in pieces if fewer see long keys, or if
+    // requests of different lengths may leave CUs waiting for the longest.  Else the waves split the keys of smaller tiles, which
+    // need cuts of their own if they are not far more than the CUs.  Whole / pieces / keys split by waves, us; full attention, 32
+    // query heads over 8 of 128:
+    //   rows of positions    512 of 512  20 / 34 / 19    600 of 600  25 / 42 / 41    704 of 2000  59 / 59 / 75    704 of 5000  130 / 94 / 126
+    //                        256 of 2048 56 / 53 / 34    512 of 4096 106 / 68 / 67   512 of 8192  202 / 102 / 117  300 of 12000 292 / 110 / 118
+    //   requests x rows      32 x 24 of 4000  117 / 128 / 194      64 x 24 of 300 to 5000  148 / 109 / 162      8 x 24 of 2000  58 / 38 / 40
+    // 32 heads over 32: 8 x 64 of 700  27 / 41 / 30, 8 x 80 of 700  29 / 45 / 49, 8 x 80 of 2000  63 / 76 / 102
     const int many = many_rows(p), keys = p.head_dim == 256 ? RowsShape<256>::SK : RowsShape<128>::SK;
-    const long long groups = tiles(many) * p.n_kv_heads, stages = (max_len + keys - 1) / keys;
-    if (most >= many) {
+    const long long likely = min(tiles(many), (long long)n * ((most + many - 1) / many));      // (max_rows may not hold)
+    const long long groups = likely * p.n_kv_heads, stages = (max_len + keys - 1) / keys;
+    if (2 * most > many) {
         // more of the smaller tiles than CUs
         const bool crowded = (long long)rows * group / (many / 2) * p.n_kv_heads > 256;
-        const bool whole = groups >= 256 || (crowded && stages <= 32) || (groups >= 128 && stages <= 12);
-        const int pieces = (512 + p.n_kv_heads - 1) / p.n_kv_heads;
         // (the plan's sums are 32-bit, by the tables' columns: max_len may not hold)
         const bool fits = tiles(many) <= kPlanTiles && tiles(many) * (columns * p.page_size / keys + 8) < 1 << 30;
-        if (whole || (fits && tiles(many) * stages >= (crowded ? 12ll : 20ll) * pieces)) {
+        const bool ragged = n > 1 && groups < 1024 && stages >= 64;
+        const bool whole = groups >= 256 ? !(ragged && fits) : (crowded && stages <= 32) || (groups >= 128 && stages <= 12);
+        const int pieces = (512 + p.n_kv_heads - 1) / p.n_kv_heads;
+        if (whole || (fits && (groups >= 256 || likely * stages >= (crowded ? 12ll : 20ll) * pieces))) {
             *nt = kManyRows;
             *split = whole ? 0 : pieces;
             *items = whole ? tiles(many) : pieces;

@@ -128,7 +128,8 @@ def attention_many(q, k_pages, v_pages, tables, kv_len, rows, first, scale, caus
     row = 0
     for r, m in enumerate(rows):
         length = kv_len[r]
-        if m == 0:
+        if m == 0 or length <= 0:                 # (rows that see nothing stay zero)
+            row += m
             continue
         p = ((length - m if first is None else first[r]) + torch.arange(m))[:, None]
         key = torch.arange(length)[None, :]

@@ -308,6 +308,20 @@ def test_many_rows_whose_keys_are_split_over_workgroups(cache, dim, heads, kv, c
     assert (out[280:] == 3.0).all()
 
 
+@pytest.mark.parametrize("cache,dim,heads,kv,rows,lens", [
+    ("f16", 64, 32, 32, [66, 100, 1, 0, 70, 99, 80, 65, 91], [900, 101, 1, 40, 70, 0, 333, 640, 257]),                     # whole tiles
+    ("bf16", 128, 96, 32, [23, 33, 1, 42, 30, 24, 29, 1, 36], [900, 101, 1, 40, 70, 0, 333, 640, 257]),
+    ("f16", 64, 32, 32, [70, 80, 66, 1, 96], [4100, 1300, 70, 0, 2500]),                                                   # pieces
+    ("bf16", 256, 48, 16, [20, 11, 17, 0, 1, 20], [4100, 50, 700, 9, 1, 1200])])
+@pytest.mark.parametrize("causal,window,sinks", [(False, 0, 0), (True, 0, 0), (True, 600, 9)])
+@pytest.mark.parametrize("hint", [1.0, 0.7])
+def test_requests_that_fill_more_than_half_of_a_tile(cache, dim, heads, kv, rows, lens, causal, window, sinks, hint):
+    """... of many rows, with a bound on the rows that holds, and one that does not."""
+    rq = Requests(dim + len(rows), rows, lens, heads, kv, dim, cache, 16)
+    got = rq.run(causal=causal, window=window, sinks=sinks, max_rows=int(hint * max(rows)))
+    rq.check(got, causal=causal, window=window, sinks=sinks, oracle=plain.attention_many)
+
+
 @pytest.mark.parametrize("n", [250, 600])
 def test_split_rows_over_many_requests(n):
     """Many requests, one or two of many rows, most of one or none; their tables are wide, which is what the way of computing goes by."""
