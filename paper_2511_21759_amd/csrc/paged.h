@@ -69,6 +69,7 @@ struct PagedAttn {
     // joining kernel of each (row, head) the first of them, and their number * 64 + row of the tile (0: the row is done).
     int split;
     long long items;                    // workgroups of the grid per K/V head
+    long long stride;                   // many requests, no split: from one workgroup's item to the next one's
     int tile_rows;
     float *partial;
     float2 *ml;
