@@ -322,6 +322,20 @@ def test_requests_that_fill_more_than_half_of_a_tile(cache, dim, heads, kv, rows
     rq.check(got, causal=causal, window=window, sinks=sinks, oracle=plain.attention_many)
 
 
+@pytest.mark.parametrize("cache,dim,heads,rows,length", [("bf16", 64, 128, 200, 4500), ("f16", 256, 64, 200, 2500)])
+@pytest.mark.parametrize("causal,window,sinks", [(False, 0, 0), (True, 0, 0), (True, 4200, 70), (False, 2400, 3)])
+def test_whole_tiles_over_more_than_64_stages(cache, dim, heads, rows, length, causal, window, sinks):
+    rq = Requests(dim, [rows], [length], heads, heads, dim, cache, 16)
+    rq.tables[0, 7] = -1                                                   # a page that is not there, which the oracle sees as a hole
+    got = rq.run(causal=causal, window=window, sinks=sinks)
+    rq.tables[0, :-1] = np.r_[rq.tables[0, :7], rq.tables[0, 8:]]          # (positions behind it are 16 lower for the oracle, and so are the rows)
+    if window == 0:
+        rq.lens = [length - 16]
+        rq.check(got, first=[length - rows - 16], causal=causal, oracle=plain.attention_many)
+    rq = Requests(dim + 1, [rows], [length], heads, heads, dim, cache, 32)
+    rq.check(rq.run(causal=causal, window=window, sinks=sinks), causal=causal, window=window, sinks=sinks, oracle=plain.attention_many)
+
+
 @pytest.mark.parametrize("n", [250, 600])
 def test_split_rows_over_many_requests(n):
     """Many requests, one or two of many rows, most of one or none; their tables are wide, which is what the way of computing goes by."""
