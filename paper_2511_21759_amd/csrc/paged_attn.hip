@@ -708,8 +708,9 @@ __global__ __launch_bounds__(64 * NW, DH == 256 || NT == 4 ? 1 : 2) void paged_a
 // Stages of SK keys, K and V, are loaded through registers into one of two LDS buffers while the other is worked on, one barrier
 // per stage; a wave holds NT row tiles for all keys, so nothing has to be merged at the end.  Bound by the matrix cores and the vector
 // ALU together, which hardly overlap: 32 keys of a row tile are 17 MFMAs of 16 cycles, and 8 exponentials of 16 and about 20 other
-// instructions of 4.  Four requests of 4096 rows at 8192 positions, 32 query heads over 8 of 128, take 1.68 ms causal (982 TFLOP/s),
-// 2.21 full (995; a library product reaches 1240).
+// instructions of 4; scalar instructions count too (half as many of them, by looking 64 stages' pages up at once and comparing a
+// stage with ranges that are worked out once, were worth 12 %).  Four requests of 4096 rows at 8192 positions, 32 query heads over 8 of
+// 128, take 1.66 to 1.80 ms causal and 2.18 to 2.36 full, from card to card (1008 to 934 TFLOP/s; a library product reaches 1240).
 template <int DH>
 struct RowsShape {
     static constexpr int NT = DH == 256 ? 1 : 2, TILE_ROWS = 64 * NT, SHIFT = DH == 256 ? 5 : 6, SK = 1 << SHIFT;
