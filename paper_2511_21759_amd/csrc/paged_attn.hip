@@ -1182,9 +1182,15 @@ void paged_attn_plan(const odb_pages &p, int n, int rows, int group, int max_row
     // 107 us, with one 110, with four 107; two over 985 MB 156, 153, 158); with more rows every cut costs more sums (8 x 32 rows: one
     // 59 us, two 62, four 68).
     const int aim = (256 * (*nt == 1 && p.head_dim != 256 ? 2 : 1) + p.n_kv_heads - 1) / p.n_kv_heads;
-    // With four row tiles for every workgroup the lengths even out by themselves, and a tile then reads only the keys it sees.
-    *split = tiles(16 * *nt) >= 4 * aim || (max_len + 31) / 32 <= 16 ? 0 : aim;
-    *items = *split ? *split : numbers(16 * *nt);
+    // With four row tiles for every workgroup the lengths even out by themselves, and a tile then reads only the keys it sees.  Short
+    // keys are not worth the cuts and the join either.  Whole / pieces, single tokens, 32 heads over 8 of 128: 4 of 600 positions 12.3 /
+    // 15.6 us, 4 of 800 15.9 / 14.8, 16 of 800 17.9 / 21.3, 32 of 1000 26.6 / 32.9, 65 of 1000 62 / 57; 4 x 32 rows of 1000, 32 heads, 19.5 / 23.8.
+    const int tile_rows = 16 * *nt;
+    const long long pairs = min(tiles(tile_rows), (long long)n * ((most + tile_rows - 1) / tile_rows)) * p.n_kv_heads;
+    const long long channels = (max_len + 31) / 32 * p.head_dim;
+    const bool brief = channels <= 20 * 128 || (pairs >= 96 && pairs <= 512 && channels <= 32 * 128);
+    *split = tiles(tile_rows) >= 4 * aim || brief ? 0 : aim;
+    *items = *split ? *split : numbers(tile_rows);
 }
 
 size_t paged_attn_workspace(const odb_pages &p, int rows, int heads, int nt, int split) {

@@ -282,6 +282,16 @@ def test_ragged_rows_masks_and_sinks(cache, dim, causal, window, sinks):
     rq.check(rq.run(causal=causal, window=window, sinks=sinks), causal=causal, window=window, sinks=sinks)
 
 
+@pytest.mark.parametrize("cache,dim", [("f16", 64), ("bf16", 128), ("f16", 256)])
+@pytest.mark.parametrize("rows", [[2, 1, 5, 0, 3, 4], [9, 1, 10, 0, 4, 7], [5, 1, 21, 0, 20, 16], [5, 1, 33, 0, 70, 16]])
+@pytest.mark.parametrize("causal,window,sinks", [(False, 0, 0), (True, 0, 0), (True, 1700, 3), (False, 1700, 40), (True, 2000, 700)])
+def test_ragged_rows_whose_keys_are_split_over_workgroups(cache, dim, rows, causal, window, sinks):
+    """The tables are wide and the windows long, which is what the way of computing goes by; one request has many keys."""
+    lens = [40, 17, 210, 30, 2300, 601]
+    rq = Requests(dim + window + sum(rows), rows, lens, 6, 2, dim, cache, 32, extra_columns=300)
+    rq.check(rq.run(causal=causal, window=window, sinks=sinks), causal=causal, window=window, sinks=sinks, oracle=plain.attention_many)
+
+
 MANY = [("f16", 64, 64, 64), ("bf16", 128, 64, 64), ("bf16", 128, 96, 32), ("f16", 256, 40, 40), ("f16", 64, 120, 24)]
 
 
