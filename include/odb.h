@@ -423,7 +423,9 @@ typedef struct {
  *   len            dev int32 [n]: wanted[r], or held[r] where refused
  *   cu_rows        dev int32 [n + 1]: rows in front of each request; all are capped at rows_cap
  *   slots, positions   dev int32 [rows_cap]: for every row its position and its slot, page * page_size + position inside the
- *                  page; -1 where the position lies outside [0, len[r]) or its page outside the pool.  Entries behind the last row stay.
+ *                  page; -1 where the position lies outside [0, len[r]) or its page outside the pool.  Entries behind the last row stay:
+ *                  those of an earlier, longer step, say.  Where such a step's whole buffers go on, cu_rows + n is the row_end of
+ *                  odb_qk_norm_rope.
  *   state          dev int32 [4]: free pages afterwards (the next call's n_free), pages taken, given back, requests refused
  * Pages are not counted: one that several tables name (a prefix that requests share) is given back as often as requests that
  * hold it get shorter, so shared pages are kept out of what is given back.
@@ -470,6 +472,8 @@ int odb_rope_table(float *table_dev, int n_pos, int rot_dim, const odb_rope *rop
  *               either's values may remain, piece by piece.
  *   q_out       dev [rows, n_heads, head_dim] of the pages' dtype, rows q_out_row elements apart; may be q itself
  *               (same dtype and stride), otherwise it must not overlap q, k or v
+ *   row_end     dev int32 [1] or NULL: rows from this one on are padding rows, whatever their positions and slots (a captured step of
+ *               fixed size whose number of rows is known on the device alone)
  * Requirements: buffers aligned to 16 bytes, row strides multiples of 8, rot_dim a multiple of 16 in [16, head_dim].
  * Asynchronous on `stream`.  rows = 0 launches nothing.  Errors: ODB_E_INVALID_ARG, also where rows * ceil((n_heads + 2 n_kv_heads)
  * * head_dim / 1024) reaches 2^26. */
@@ -484,6 +488,7 @@ typedef struct {
     const int32_t *positions, *slots;
     void *q_out;
     long long q_out_row;
+    const int32_t *row_end;
 } odb_qk_rows;
 int odb_qk_norm_rope(const odb_qk_rows *rows, const odb_pages *pages, void *stream);
 

@@ -89,7 +89,8 @@ class odb_qk_rows(ctypes.Structure):
                 ("rows", ctypes.c_int), ("n_heads", ctypes.c_int), ("q_row", ctypes.c_longlong), ("k_row", ctypes.c_longlong),
                 ("v_row", ctypes.c_longlong), ("q_gain", ctypes.c_void_p), ("k_gain", ctypes.c_void_p), ("eps", ctypes.c_float),
                 ("table", ctypes.c_void_p), ("n_pos", ctypes.c_int), ("rot_dim", ctypes.c_int), ("interleaved", ctypes.c_int),
-                ("positions", ctypes.c_void_p), ("slots", ctypes.c_void_p), ("q_out", ctypes.c_void_p), ("q_out_row", ctypes.c_longlong)]
+                ("positions", ctypes.c_void_p), ("slots", ctypes.c_void_p), ("q_out", ctypes.c_void_p), ("q_out_row", ctypes.c_longlong),
+                ("row_end", ctypes.c_void_p)]
 
 
 class odb_attention(ctypes.Structure):
@@ -448,7 +449,7 @@ def odb_cache_read(cache: int, layer: int, kv: int, batch_index: int, pos0: int,
 # checks look at each tensor once.
 
 ROPE_SCALINGS = ("plain", "linear", "ntk", "yarn")
-_PACK_PAGES, _PACK_QK_ROWS, _PACK_ATTENTION = (struct.Struct(f).pack for f in ("@PPiiiiiqqq", "@PPPiiiqqqPPfPiiiPPPq", "@PPqqPPPPiiiifiiiiiPN"))
+_PACK_PAGES, _PACK_QK_ROWS, _PACK_ATTENTION = (struct.Struct(f).pack for f in ("@PPiiiiiqqq", "@PPPiiiqqqPPfPiiiPPPqP", "@PPqqPPPPiiiifiiiiiPN"))
 _torch = _raw_stream = None
 
 
@@ -511,16 +512,17 @@ def odb_page_tables(held, wanted, tables, free_pages, n_free, page_size: int, n_
     """held, wanted int32 [n]; tables int32 [n, columns] and free_pages int32 [n_pages], updated in place; n_free int32 [1];
     row_first, row_count int32 [n] or None -> (len int32 [n], cu_rows int32 [n + 1], slots, positions int32 [rows_cap],
     state int32 [4]).  `slots` and `positions` may be given (their length is then rows_cap; entries behind the last row
-    stay), as may `out` = (len, cu_rows, state)."""
+    stay, so a step over the whole buffers gives odb_qk_norm_rope row_end=cu_rows[n:]); buffers of this call's own hold -1 there.
+    `out` = (len, cu_rows, state) may be given too."""
     torch = _torch or _load_torch()
     index, n, i32, (rows, columns) = held.get_device(), held.numel(), torch.int32, tables.shape if tables.dim() == 2 else (-1, -1)
     if rows != n:
         _not_ints("tables", "[n, columns]")
     if slots is None:
-        slots = held.new_empty((rows_cap,))
+        slots = held.new_full((rows_cap,), -1)
     cap = slots.numel()
     if positions is None:
-        positions = held.new_empty((cap,))
+        positions = held.new_full((cap,), -1)
     per = (n,)
     p_held = _ints("held", held, per, index, i32)
     if out is None:
@@ -556,11 +558,11 @@ def odb_rope_table(n_pos: int, rot_dim: int, base: float, scaling: str = "plain"
 
 
 def odb_qk_norm_rope(q, k, v, k_pages, v_pages, table, positions, slots, q_gain=None, k_gain=None, eps: float = 1e-6,
-                     interleaved: bool = False, out=None):
+                     interleaved: bool = False, out=None, row_end=None):
     """q [rows, n_heads, head_dim], k and v [rows, n_kv_heads, head_dim], float32 or the pools' dtype, rows of any stride (three
     parts of one buffer, say); k_pages, v_pages [n_pages, n_kv_heads, page_size, head_dim]; table float32 [n_pos, rot_dim / 2, 2];
     positions, slots int32 [rows]; gains float32 [head_dim] -> queries [rows, n_heads, head_dim] in the pools' dtype.  K/V of
-    the rows go to the pools.  out may be q."""
+    the rows go to the pools.  out may be q.  row_end int32 [1]: rows from this one on are padding."""
     torch = _torch or _load_torch()
     index, pages, dtype, i32, f32 = q.get_device(), _pages(k_pages, v_pages), q.dtype, torch.int32, torch.float32
     shape = rows, heads, dim = q.shape
@@ -580,7 +582,7 @@ def odb_qk_norm_rope(q, k, v, k_pages, v_pages, table, positions, slots, q_gain=
                       _head_rows("k", k, index, dtype, kv), _head_rows("v", v, index, dtype, kv), 0 if q_gain is None else q_gain.data_ptr(),
                       0 if k_gain is None else k_gain.data_ptr(), eps, table.data_ptr(), table.shape[0], 2 * table.shape[1], bool(interleaved),
                       _ints("positions", positions, (rows,), index, i32), _ints("slots", slots, (rows,), index, i32), out.data_ptr(),
-                      out_row)
+                      out_row, 0 if row_end is None else _ints("row_end", row_end, (1,), index, i32))
     if rows:
         _on(index, lib().odb_qk_norm_rope, r, pages)
     return out

@@ -43,6 +43,7 @@ struct QkNormRope {
     void *q_out;
     long long q_out_row;
     odb_pages pages;
+    const int32_t *row_end;             // null: all rows count
 };
 // head_dim / 16 lanes a head; rows times this, 64 threads each, is below 2^32
 inline int qk_waves_per_row(int heads, const odb_pages &p) {

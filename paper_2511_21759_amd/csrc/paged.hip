@@ -271,7 +271,8 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkNormRope a, int wav
     if (row >= a.rows) return;
     const odb_pages &pg = a.pages;
     const int pos = a.positions[row], slot = a.slots[row];
-    const bool live = pos >= 0 && pos < a.n_pos;                // a padding row: queries become zero, nothing is stored
+    // a padding row: queries become zero, nothing is stored
+    const bool live = pos >= 0 && pos < a.n_pos && (!a.row_end || row < *a.row_end);
     const int page = slot >= 0 ? (int)((unsigned)slot / (unsigned)pg.page_size) : -1;
     const bool stored = live && page >= 0 && page < pg.n_pages;
     const size_t at = stored ? (size_t)page * pg.page_stride + (size_t)(slot - page * pg.page_size) * pg.pos_stride : 0;

@@ -1,0 +1,108 @@
+"""Calls of the paged K/V operators that a serving program makes beside the ordinary ones: buffers larger than a step's rows, captured
+steps that get shorter, scores far outside the usual range.  Plain forms and bounds are those of test_gpu_paged.py."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import paged_plain as plain                                          # noqa: E402
+from paper_2511_21759_amd import binding as B                        # noqa: E402
+
+pytestmark = pytest.mark.gpu
+F = 2.0 ** -24
+
+
+def ints(x):
+    return torch.tensor(np.asarray(x), dtype=torch.int32, device="cuda")
+
+
+# ---- rows behind a step's last one ---------------------------------------------------------------------------------------
+
+def test_entries_behind_the_last_row_of_own_buffers_are_padding():
+    """Without given buffers the binding allocates slots and positions; torch hands out memory that was used before."""
+    cap = 4096
+    for _ in range(3):
+        old = [torch.full((k * cap,), 5, dtype=torch.int32, device="cuda") for k in (1, 1, 2)]
+        del old
+        length, cu, slots, positions, state = B.odb_page_tables(ints([0, 7]), ints([3, 8]), ints([[-1, -1], [2, -1]]), ints([0, 1, 3, 4]), ints([2]), 16, 4,
+                                                                rows_cap=cap)
+        assert cu.tolist() == [0, 3, 4]
+        assert slots.tolist()[:4] == [16, 17, 18, 2 * 16 + 7] and positions.tolist()[:4] == [0, 1, 2, 7]
+        assert (slots[4:] == -1).all() and (positions[4:] == -1).all()
+
+
+class Step:
+    """A step of at most `cap` rows over buffers that stay: tables, rotation and store, attention."""
+    heads, kv, dim, page, n_pages, columns = 4, 2, 64, 16, 60, 9
+
+    def __init__(self, n, cap, seed):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        self.n = n
+        self.pools = [torch.randn(self.n_pages, self.kv, self.page, self.dim, generator=g, device="cuda").half() for _ in range(2)]
+        self.qkv = torch.randn(cap, self.heads + 2 * self.kv, self.dim, generator=g, device="cuda").half()
+        ids = torch.randperm(self.n_pages, generator=g, device="cuda").int()
+        self.tables = ids[:n * self.columns].view(n, self.columns).contiguous()
+        self.free, self.n_free = torch.zeros(self.n_pages, dtype=torch.int32, device="cuda"), ints([0])
+        self.held, self.first, self.count = ints([0] * n), ints([0] * n), ints([0] * n)
+        self.slots, self.positions = ints([-1] * cap), ints([-1] * cap)
+        self.table = B.odb_rope_table(self.page * self.columns, self.dim, 10000.0)
+
+    def run(self):
+        length, cu, slots, positions, _ = B.odb_page_tables(self.held, self.held, self.tables, self.free, self.n_free, self.page, self.n_pages, slots=self.slots,
+                                                            positions=self.positions, row_first=self.first, row_count=self.count)
+        h, kv = self.heads, self.kv
+        q = B.odb_qk_norm_rope(self.qkv[:, :h], self.qkv[:, h:h + kv], self.qkv[:, h + kv:], *self.pools, self.table, positions, slots, row_end=cu[self.n:])
+        return q, B.odb_paged_attention(q, *self.pools, self.tables, length, causal=True, cu_rows=cu, first_pos=self.first)
+
+    def set(self, held, first, count):
+        for to, x in ((self.held, held), (self.first, first), (self.count, count)):
+            to.copy_(ints(x))
+
+
+@pytest.mark.parametrize("graphed", [False, True])
+def test_a_long_step_followed_by_shorter_ones_stores_live_rows_only(graphed):
+    """Slots and positions keep the entries of the longer step behind the last row; row_end says where the rows end."""
+    n, cap = 3, 48
+    s = Step(n, cap, 4)
+    s.set([100, 90, 140], [80, 70, 140], [20, 20, 0])
+    s.run()
+    torch.cuda.synchronize()
+    if graphed:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = s.run()
+    for held, first, count in (([100, 90, 140], [80, 70, 120], [20, 8, 20]), ([101, 91, 141], [100, 90, 140], [1, 1, 1]), ([102, 90, 141], [101, 90, 0], [1, 0, 0]),
+                               ([0, 0, 0], [0, 0, 0], [0, 0, 0]), ([110, 90, 144], [100, 60, 142], [10, 30, 2])):
+        s.set(held, first, count)
+        s.qkv.copy_(torch.randn(s.qkv.shape, generator=torch.Generator().manual_seed(sum(held))))
+        before = [x.clone() for x in s.pools]
+        if graphed:
+            graph.replay()
+        else:
+            out = s.run()
+        torch.cuda.synchronize()
+        q = out[0].clone()
+        live = sum(count)
+        assert (q[live:] == 0).all() and (q[:live] != 0).any(-1).all()
+        at = [(r, p) for r in range(n) for p in range(first[r], first[r] + count[r])]
+        slots = [int(s.tables[r, p // 16]) * 16 + p % 16 for r, p in at]
+        for pool, was, lane in ((s.pools[0], before[0], slice(4, 6)), (s.pools[1], before[1], slice(6, 8))):
+            changed = (pool != was).any(-1).any(1).reshape(-1).nonzero().flatten().tolist()
+            assert changed == sorted(slots)
+        for i, slot in enumerate(slots):
+            assert torch.equal(s.pools[1][slot // 16, :, slot % 16], s.qkv[i, 6:8])
+
+
+@pytest.mark.parametrize("end,live", [(0, 0), (-5, 0), (-2 ** 31, 0), (3, 3), (20, 20), (21, 20), (2 ** 31 - 1, 20)])
+def test_row_end_of_any_value(end, live):
+    s = Step(1, 20, 9)
+    s.positions.copy_(torch.arange(20)), s.slots.copy_(torch.arange(20) + 32)
+    before = [x.clone() for x in s.pools]
+    q = B.odb_qk_norm_rope(s.qkv[:, :4], s.qkv[:, 4:6], s.qkv[:, 6:], *s.pools, s.table, s.positions, s.slots, row_end=ints([end]))
+    want_pools = [x.clone() for x in before]
+    cut = s.slots.clone()
+    cut[live:] = -1
+    want = B.odb_qk_norm_rope(s.qkv[:, :4], s.qkv[:, 4:6], s.qkv[:, 6:], *want_pools, s.table, s.positions, cut)
+    assert torch.equal(q[:live], want[:live]) and (q[live:] == 0).all()
+    for x, y in zip(s.pools, want_pools):
+        assert torch.equal(x, y)
