@@ -518,7 +518,9 @@ def odb_page_tables(held, wanted, tables, free_pages, n_free, page_size: int, n_
     index, n, i32, (rows, columns) = held.get_device(), held.numel(), torch.int32, tables.shape if tables.dim() == 2 else (-1, -1)
     if rows != n:
         _not_ints("tables", "[n, columns]")
-    if slots is None:
+    if slots is None and positions is None:
+        slots, positions = held.new_full((2, rows_cap), -1).unbind()
+    elif slots is None:
         slots = held.new_full((rows_cap,), -1)
     cap = slots.numel()
     if positions is None:
