@@ -542,6 +542,7 @@ long long odb_paged_attention_workspace(const odb_attention *a, const odb_pages 
  *   tokens      dev int32 [n, b]; first_pos, kv_len dev int32 [n]; tables dev int32 [n, columns]; positions, slots dev int32 [n * b]
  *   table       dev float [n_pos, head_dim / 2, 2] as odb_rope_table writes it (base: the model's rope_base)
  *   layer0      the first layer's pool, binary16, n_heads heads; those of the next layers lie layer_stride elements further each
+ *   n_layers    how many layers the pools were made for: the model's number, a call with another one is refused
  *   skip        rows of each request in front of those that conf and argmax are written for (a prompt's)
  *   conf, argmax   dev float / int32 [n, b - skip]; both NULL: only K/V are wanted
  *   unmask      dev uint8 [n, b] or NULL: the acceptance of odb_block_step with threshold tau, for b <= 256 and skip 0
@@ -562,6 +563,7 @@ typedef struct {
     float *conf;
     int32_t *argmax;
     uint8_t *unmask;
+    int n_layers;
 } odb_paged_rows;
 int odb_step_paged(odb_model *m, const odb_paged_rows *rows, const odb_pages *layer0, void *stream);
 

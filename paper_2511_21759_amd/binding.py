@@ -107,7 +107,7 @@ class odb_paged_rows(ctypes.Structure):
                 ("kv_len", ctypes.c_void_p), ("tables", ctypes.c_void_p), ("columns", ctypes.c_int), ("positions", ctypes.c_void_p),
                 ("slots", ctypes.c_void_p), ("table", ctypes.c_void_p), ("n_pos", ctypes.c_int), ("layer_stride", ctypes.c_longlong),
                 ("skip", ctypes.c_int), ("max_len", ctypes.c_int), ("tau", ctypes.c_float), ("conf", ctypes.c_void_p),
-                ("argmax", ctypes.c_void_p), ("unmask", ctypes.c_void_p)]
+                ("argmax", ctypes.c_void_p), ("unmask", ctypes.c_void_p), ("n_layers", ctypes.c_int)]
 
 
 EVENT_KINDS = ("refresh", "step", "shared")
@@ -660,7 +660,8 @@ def odb_step_paged(model: int, tokens, k_pages, v_pages, tables, first_pos, kv_l
     r = odb_paged_rows(_ints("tokens", tokens, (n, b), index, i32), n, b, _ints("first_pos", first_pos, (n,), index, i32),
                        _ints("kv_len", kv_len, (n,), index, i32), _ints("tables", tables, (n, tables.shape[1]), index, i32), tables.shape[1],
                        _ints("positions", positions, (n * b,), index, i32), _ints("slots", slots, (n * b,), index, i32), table.data_ptr(), table.shape[0],
-                       k_pages.stride(0), skip, max_len, 0.0 if tau is None else tau, *(None if t is None else t.data_ptr() for t in (conf, argmax, unmask)))
+                       k_pages.stride(0), skip, max_len, 0.0 if tau is None else tau, *(None if t is None else t.data_ptr() for t in (conf, argmax, unmask)),
+                       k_pages.shape[0])
     _on(index, lib().odb_step_paged, model, ctypes.byref(r), _pages(k_pages[0], v_pages[0]))
     return conf, argmax, unmask
 

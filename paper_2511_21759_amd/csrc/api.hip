@@ -1093,6 +1093,7 @@ int odb_step_paged(odb_model *mh, const odb_paged_rows *args, const odb_pages *l
     if (layer0->dtype != ODB_F16 || layer0->n_kv_heads != H || layer0->head_dim != dh)
         return fail(ODB_E_INVALID_ARG, "%s: pages of %d heads of %d, dtype %d; the model has %d of %d in binary16", who, layer0->n_kv_heads, layer0->head_dim,
                     layer0->dtype, H, dh);
+    if (r.n_layers != cfg.n_layers) return fail(ODB_E_INVALID_ARG, "%s: pools of %d layers; the model has %d", who, r.n_layers, cfg.n_layers);
     if (cfg.n_layers > 1 && (r.layer_stride < 8 || r.layer_stride & 7)) return fail(ODB_E_INVALID_ARG, "%s: layer_stride=%lld", who, r.layer_stride);
     const int rows = r.n * r.b, rows_pad = ru(rows, 16), mt = rows_pad / 16;
     const bool head = r.conf != nullptr, fused_head = r.unmask != nullptr;
