@@ -463,7 +463,7 @@ int odb_rope_table(float *table_dev, int n_pos, int rot_dim, const odb_rope *rop
  * q and k of each head are divided by their root mean square, sqrt(mean of squares + eps), and multiplied by the gain
  * (skipped where the gain is NULL); then the first rot_dim channels of each head turn by the angles of the row's
  * position: pairs are (j, j + rot_dim / 2), or with `interleaved` (2j, 2j + 1).  Queries go to q_out, keys and values to the
- * row's slot.  All in 32 bits with one rounding at the end.
+ * row's slot.  All in 32 bits with one rounding at the end, to an infinity beyond the type's range.
  *   q [rows, n_heads, head_dim], k, v [rows, n_kv_heads, head_dim]: dev, in_dtype ODB_F32 or the pages' dtype; the heads of a
  *       row follow each other, rows are q_row, k_row, v_row elements apart (three parts of one buffer, say)
  *   table       dev float [n_pos, rot_dim / 2, 2] as odb_rope_table writes it
@@ -547,7 +547,8 @@ long long odb_paged_attention_workspace(const odb_attention *a, const odb_pages 
  *   conf, argmax   dev float / int32 [n, b - skip]; both NULL: only K/V are wanted
  *   unmask      dev uint8 [n, b] or NULL: the acceptance of odb_block_step with threshold tau, for b <= 256 and skip 0
  *   max_len     upper bound of kv_len as for odb_paged_attention
- * Uses the model's scratch (see the conventions above).  Asynchronous on `stream`.  Errors: ODB_E_INVALID_ARG for NULL inputs,
+ * Q, K and V beyond the binary16 range are clamped and reported by odb_model_status, as in the dense calls (what padding rows
+ * hold is not).  Uses the model's scratch (see the conventions above).  Asynchronous on `stream`.  Errors: ODB_E_INVALID_ARG for NULL inputs,
  * n * b outside [1, 65536], pools that do not fit the model, and what odb_paged_attention refuses. */
 typedef struct {
     const int32_t *tokens;

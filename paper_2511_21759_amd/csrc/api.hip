@@ -1127,7 +1127,7 @@ int odb_step_paged(odb_model *mh, const odb_paged_rows *args, const odb_pages *l
     launch_embed(m, r.tokens, rm, h, norm_out(m, base, pl, m.g1, mt), ao, rows % 16 ? (size_t)rows_pad * d * 2 : 0, s);
 
     QkNormRope qk{qkv, qkv + d, qkv + 2 * (size_t)d, ODB_F32, 3ll * d, 3ll * d, 3ll * d, rows, H, nullptr, nullptr, 0.f, r.table, r.n_pos, dh, 1, r.positions,
-                  r.slots, q, d, *layer0, nullptr};
+                  r.slots, q, d, *layer0, nullptr, m.counters};
     pa.q = q; pa.out = ao; pa.q_row = pa.out_row = d; pa.out_mt = mt;
     pa.rows_per_request = r.b;
     pa.first = r.first_pos; pa.kv_len = r.kv_len; pa.tables = r.tables;

@@ -44,6 +44,7 @@ struct QkNormRope {
     long long q_out_row;
     odb_pages pages;
     const int32_t *row_end;             // null: all rows count
+    unsigned *status;                   // a model's status word: binary16 values saturate and are reported there; null: they become infinite
 };
 // head_dim / 16 lanes a head; rows times this, 64 threads each, is below 2^32
 inline int qk_waves_per_row(int heads, const odb_pages &p) {

@@ -342,6 +342,19 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkNormRope a, int wav
         if (!stored) return;
         dst = (TO *)(is_k ? pg.k : pg.v) + at + (size_t)head * pg.head_stride;
     }
+    if (a.status) {                                             // (of the model's forward, whose type is binary16)
+        int out = 0;
+#pragma unroll
+        for (int i = 0; i < 8; i += 4) out |= (int)out_of_f16(x[i], x[i + 1], x[i + 2], x[i + 3]) | (int)out_of_f16(y[i], y[i + 1], y[i + 2], y[i + 3]);
+        if (out) {
+            atomicOr(a.status, kStatusSaturated);
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                x[i] = fminf(fmaxf(x[i], -65504.f), 65504.f);
+                y[i] = fminf(fmaxf(y[i], -65504.f), 65504.f);
+            }
+        }
+    }
     store8(dst + c0, x);
     store8(dst + c1, y);
 }

@@ -195,7 +195,7 @@ int odb_qk_norm_rope(const odb_qk_rows *rows, const odb_pages *pages, void *stre
         return fail(ODB_E_INVALID_ARG, "%s: q_out overlaps q, k or v without being q itself", who);
     if (r.rows == 0) return ODB_OK;
     launch_qk_norm_rope(QkNormRope{r.q, r.k, r.v, r.in_dtype, r.q_row, r.k_row, r.v_row, r.rows, r.n_heads, r.q_gain, r.k_gain, r.eps, r.table, r.n_pos,
-                                   r.rot_dim, r.interleaved, r.positions, r.slots, r.q_out, r.q_out_row, *pages, r.row_end}, (hipStream_t)stream);
+                                   r.rot_dim, r.interleaved, r.positions, r.slots, r.q_out, r.q_out_row, *pages, r.row_end, nullptr}, (hipStream_t)stream);
     HIP_TRY(hipGetLastError());
     return ODB_OK;
 }
