@@ -508,7 +508,8 @@ int odb_qk_norm_rope(const odb_qk_rows *rows, const odb_pages *pages, void *stre
  *   workspace  dev, odb_paged_attention_workspace() bytes, aligned to 256, NULL where that says 0; holds the
  *            sums of keys that are split over workgroups, means nothing between calls, must not be shared by calls that
  *            overlap in time
- * Scores and sums are 32-bit; probabilities are rounded to the pages' dtype for the product with V.  The order of all
+ * Scores and sums are 32-bit; probabilities are rounded to the pages' dtype for the product with V.  The largest score that a row
+ * sees, times scale * log2(e), has to stay below 2^29 in magnitude (the results of a row where it does not are no numbers).  The order of all
  * additions follows from the arguments and the lengths alone, so the same call gives the same bits.
  * Asynchronous on `stream`.  Errors: ODB_E_INVALID_ARG for NULL buffers, n outside [1, 4096], rows outside [0, 2^24] (0: nothing is
  * launched), n_heads no multiple of n_kv_heads, columns < 1, columns * page_size > 2^30, a scale that is not positive or, times

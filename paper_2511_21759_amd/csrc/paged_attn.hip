@@ -49,6 +49,12 @@ template <> struct Num<__bf16> {
 constexpr float kShift = 8.0f, kRaise = 15.0f, kNone = -3.402823466e38f;
 struct Reference { float at = kNone, limit = kNone; };          // in units of log2; limit: the score beyond which it is raised
 
+// A reference has 24 bits, so far from zero its own rounding moves the probabilities by a power of two: below kBeyond by up to 2^16 down and,
+// where it would be more than 2^7 up, down instead, which keeps that of the largest score inside binary16 and not zero.  A row whose reference
+// lies beyond gets no number for its sum (the one whose bits are all ones: others take a register).
+constexpr float kBeyond = 1 << 29;
+__device__ __forceinline__ float checked_sum(float at, float sum) { return fabsf(at) >= kBeyond && at != kNone ? __builtin_bit_cast(float, -1) : sum; }
+
 // ---- which keys -------------------------------------------------------------------------------------------------------
 
 constexpr int kFar = 1 << 30;                       // lengths, windows and positions are at most this
@@ -277,12 +283,15 @@ __device__ __forceinline__ void probabilities(f32x4 (*z)[2], float sc, Reference
         for (int t = 0; t < NT; t++) {
             float m = fmaxf(top[t], __shfl_xor(top[t], 16));
             m = fmaxf(m, __shfl_xor(m, 32));
-            const float up = fmaxf(ref[t].at, m * sc - kShift), f = __builtin_amdgcn_exp2f(ref[t].at - up);
+            float up = fmaxf(ref[t].at, m * sc - kShift);
+            up += __builtin_fmaf(m, sc, -up) > kRaise ? fabsf(up) * 0x1.8p-24f : 0.f;      // (rounded down by more than 7: the next number)
+            const float f = __builtin_amdgcn_exp2f(ref[t].at - up);
             lsum[t] *= f;
 #pragma unroll
             for (int c = 0; c < CT; c++) o[t][c] *= f;
             ref[t].at = up;
             ref[t].limit = (up + kRaise) / sc;
+            ref[t].limit -= fabsf(ref[t].limit) * 0x1p-22f;                               // (its own roundings)
         }
     // Probabilities are rounded to the type of V for the matrix cores; the sum that divides them at the end is that of the
     // rounded ones, so what equal rounding errors have in common drops out.
@@ -663,6 +672,7 @@ __global__ __launch_bounds__(64 * NW, DH == 256 || NT == 4 ? 1 : 2) void paged_a
 #pragma unroll
                         for (int i = 0; i < 4; i++) { sum[i] += u[i]; sum[4 + i] += v[i]; }
                     }
+                    l = checked_sum(top, l);
                     const int i = rho / G, hq = head * G + (rho - i * G), row = rq.row0 + i;
                     if (!whole) {
                         float *dst = a.partial + ((size_t)place * TILE_ROWS + t * 16 + r) * DH + c;
@@ -985,7 +995,7 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void paged_rows_kernel(Paged
                 const int in_tile = wave * 16 * NT + t * 16 + (tid & 15), rho = tile * Shape::TILE_ROWS + in_tile, eg = (tid >> 4) & 3;
                 if (rho >= n_rows) continue;
                 const int i = rho / G, hq = head * G + (rho - i * G);
-                const float l = lsum[t][0];
+                const float l = checked_sum(ref[t].at, lsum[t][0]);
                 if (!whole) {
                     const long long place = ((2ll * x + (b_lo == 0)) * kv + head) * Shape::TILE_ROWS + in_tile;
 #pragma unroll

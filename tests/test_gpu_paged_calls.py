@@ -106,3 +106,85 @@ def test_row_end_of_any_value(end, live):
     assert torch.equal(q[:live], want[:live]) and (q[live:] == 0).all()
     for x, y in zip(s.pools, want_pools):
         assert torch.equal(x, y)
+
+
+# ---- scores far outside the usual range -----------------------------------------------------------------------------------
+
+# (rows of each request, positions, query heads, K/V heads, head size, page, columns beside those that are needed): what reaches each
+# way of computing - keys whole and split over workgroups with 1, 2 and 4 row tiles, many rows whole and in pieces
+WAYS = [([1, 1], [100, 333], 4, 2, 64, 16, 1), ([1, 1], [1700, 900], 4, 2, 128, 32, 300), ([5, 3], [200, 150], 8, 2, 128, 16, 1),
+        ([9, 9], [1500, 2000], 6, 2, 256, 16, 100), ([33, 40], [2000, 900], 4, 2, 64, 32, 300), ([40, 20], [300, 70], 4, 2, 128, 32, 1),
+        ([260, 131], [301, 140], 64, 64, 64, 16, 1), ([150, 129], [3500, 2000], 16, 16, 64, 16, 1), ([150], [1500], 16, 16, 256, 16, 400)]
+
+
+@pytest.mark.parametrize("cache", ["f16", "bf16"])
+@pytest.mark.parametrize("rows,lens,heads,kv,dim,page,more", WAYS)
+@pytest.mark.parametrize("power,step,scale", [(18, 0, 1.0), (23, 0, 1.0), (25, 2, 1.0), (27, 4, 2.0 ** -4), (27, 4, 1.0), (28, 5, 1.0), (30, 7, 2.0 ** -2)])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_scores_of_any_size(rows, lens, heads, kv, dim, page, more, cache, power, step, scale, sign):
+    """Scores sign * 2^power + 2^step * f, f whole numbers: exact in 32 bits, whatever the order of their sums, so the softmax is known."""
+    dt = torch.float16 if cache == "f16" else torch.bfloat16
+    g = torch.Generator().manual_seed(power + dim)
+    need = [-(-x // page) for x in lens]
+    n_pages = sum(need) + 1
+    k, v = torch.zeros(n_pages, kv, page, dim), torch.randn(n_pages, kv, page, dim, generator=g).to(dt)
+    q = torch.zeros(sum(rows), heads, dim)
+    q[..., 0], q[..., 1] = 2.0 ** step, sign * 2.0 ** (power // 2)
+    # f of every 16 keys reaches 12 once; the first block of a request lies 2^(power - 4) lower, so that references are raised
+    f = torch.randint(0, 12, (n_pages, 1, page), generator=g).float().expand(n_pages, kv, page).clone()
+    f[:, :, ::16] = 12
+    k[..., 0], k[..., 1] = f, 2.0 ** (power - power // 2)
+    tables, at = np.full((len(lens), max(need) + more), -1, np.int32), 0
+    ids = torch.randperm(n_pages, generator=g).tolist()
+    for r, x in enumerate(need):
+        tables[r, :x] = ids[at:at + x]
+        at += x
+        if lens[r] > 64:
+            k[tables[r, 0], :, :16, 1] -= sign * 2.0 ** (power - power // 2 - 4)
+    q, k = q.to(dt), k.to(dt)
+    cu = ints(np.r_[0, np.cumsum(rows)])
+    got = B.odb_paged_attention(q.cuda(), k.cuda(), v.cuda(), ints(tables), ints(lens), causal=True, cu_rows=cu, scale=scale).cpu().double()
+    want, size, _ = plain.attention_many(q.double(), k, v, tables, lens, rows, None, scale, True, 0, 0)
+    # A probability is off by its rounding u to the type; by exp2, 4 F; by the 32-bit forms of scale * log2(e), 2 F of the distance of a score
+    # from the largest, which is at most 12 steps where the probability counts, and below 2^15, where references are not taken from
+    # scores, of the score; numerator and denominator both.  The sums over the keys add their number times F / 4.
+    u = torch.finfo(dt).eps / 2
+    off = u + 4 * F + 2 * F * 1.45 * scale * 12 * 2.0 ** step + max(lens) * F / 4
+    bound = 2 * off * size * (1 + 4 * off) + u * want.abs() * (1 + u) + torch.finfo(dt).tiny
+    assert torch.isfinite(got).all()
+    err = (got - want).abs()
+    assert (err <= bound).all(), (err / bound).max().item()
+
+
+@pytest.mark.parametrize("cache", ["f16", "bf16"])
+@pytest.mark.parametrize("rows,lens,heads,kv,dim,page,more", WAYS)
+@pytest.mark.parametrize("sign", [1, -1])
+def test_rows_whose_scores_are_beyond_the_range_become_no_numbers(rows, lens, heads, kv, dim, page, more, cache, sign):
+    """The first row of each request has scores of 2^29 and more in units of log2; the others stay what they are."""
+    dt = torch.float16 if cache == "f16" else torch.bfloat16
+    g = torch.Generator().manual_seed(dim)
+    need = [-(-x // page) for x in lens]
+    k, v = (torch.randn(sum(need), kv, page, dim, generator=g) for _ in range(2))
+    k[..., 0] = 2.0 ** 15
+    tables, at = np.full((len(lens), max(need) + more), -1, np.int32), 0
+    for r, x in enumerate(need):
+        tables[r, :x] = np.arange(at, at + x)
+        at += x
+    q = torch.randn(sum(rows), heads, dim, generator=g)
+    q[..., 0] = 0
+    cu = np.r_[0, np.cumsum(rows)]
+    args = k.to(dt).cuda(), v.to(dt).cuda(), ints(tables), ints(lens)
+    kw = dict(causal=False, cu_rows=ints(cu), scale=1.0)
+    q[cu[:-1], :, 0] = sign * 2.0 ** 14
+    q = q.to(dt)
+    got = B.odb_paged_attention(q.cuda(), *args, **kw).cpu().double()
+    beyond = torch.zeros(sum(rows), dtype=torch.bool)
+    beyond[cu[:-1]] = True
+    assert got[beyond].isnan().all() and torch.isfinite(got[~beyond]).all()
+    want, size, big = plain.attention_many(q.double(), k.to(dt), v.to(dt), tables, lens, rows, None, 1.0, False, 0, 0)
+    # the bound of test_gpu_paged.py; the other rows are not the same to the last bit as without these neighbours, since rows of a tile raise
+    # their references together, which moves the roundings of their probabilities
+    u = torch.finfo(dt).eps / 2
+    off = u + (dim + 4) * F * big[..., None] + 8 * F + max(lens) * F / 4
+    bound = 2 * off * size * (1 + 4 * off) + u * want.abs() * (1 + u) + torch.finfo(dt).tiny * torch.finfo(dt).eps
+    assert ((got - want).abs()[~beyond] <= bound[~beyond]).all()
