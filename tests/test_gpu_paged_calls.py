@@ -114,7 +114,7 @@ def test_row_end_of_any_value(end, live):
 # way of computing - keys whole and split over workgroups with 1, 2 and 4 row tiles, many rows whole and in pieces
 WAYS = [([1, 1], [100, 333], 4, 2, 64, 16, 1), ([1, 1], [1700, 900], 4, 2, 128, 32, 300), ([5, 3], [200, 150], 8, 2, 128, 16, 1),
         ([9, 9], [1500, 2000], 6, 2, 256, 16, 100), ([33, 40], [2000, 900], 4, 2, 64, 32, 300), ([40, 20], [300, 70], 4, 2, 128, 32, 1),
-        ([260, 131], [301, 140], 64, 64, 64, 16, 1), ([150, 129], [3500, 2000], 16, 16, 64, 16, 1), ([150], [1500], 16, 16, 256, 16, 400)]
+        ([260, 131], [301, 140], 64, 64, 64, 16, 1), ([150, 129], [3500, 2000], 16, 16, 64, 16, 500), ([150], [1500], 16, 16, 256, 16, 400)]
 
 
 @pytest.mark.parametrize("cache", ["f16", "bf16"])

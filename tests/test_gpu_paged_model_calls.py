@@ -1,5 +1,5 @@
-"""odb_step_paged where it leaves the ordinary: values beyond the binary16 range, pools of another model, many rows and requests.  Bars
-are those of test_gpu_paged_model.py."""
+"""odb_step_paged where it leaves the ordinary: values beyond the binary16 range, pools of another model, many rows and requests, further
+turns.  Bars are those of test_gpu_paged_model.py."""
 import numpy as np
 import pytest
 
@@ -8,7 +8,7 @@ torch = pytest.importorskip("torch")
 from oracle import odb_oracle as o                                   # noqa: E402
 from paper_2511_21759_amd import binding as B                        # noqa: E402
 from paper_2511_21759_amd import workloads as W                      # noqa: E402
-from test_gpu_paged_model import KV_TOL, LOG_CONF, Paged, ints       # noqa: E402
+from test_gpu_paged_model import KV_TOL, LOG_CONF, MARGIN, Paged, decide, ints       # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -102,5 +102,172 @@ def test_padding_rows_report_nothing():
         pg.forward(np.array([[9], [5]]), [0, 0], [1, 1], tau=0.5)
         with pytest.raises(B.OdbError, match="binary16"):
             B.odb_model_status(model)
+    finally:
+        B.odb_model_destroy(model)
+
+
+# ---- many rows and requests -----------------------------------------------------------------------------------------------
+
+def random_pages(shape, model, lens, page, seed):
+    """Requests of those lengths over pools of random numbers."""
+    columns = -(-max(lens) // page)
+    need = [-(-x // page) for x in lens]
+    pg = Paged(shape, model, len(lens), columns, page, sum(need) + 1)
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    for pool in (pg.k, pg.v):
+        pool.copy_(0.4 * torch.randn(pool.shape, generator=g, device="cuda"))
+    ids, tables, at = np.random.default_rng(seed).permutation(sum(need) + 1), np.full((len(lens), columns), -1, np.int32), 0
+    for r, x in enumerate(need):
+        tables[r, :x] = ids[at:at + x]
+        at += x
+    pg.tables = ints(tables)
+    return pg
+
+
+@pytest.mark.parametrize("n,b,head_gain", [(600, 1, None), (530, 70, None), (64, 16, 32.0)])
+def test_many_requests_equal_a_few_at_a_time(n, b, head_gain):
+    """One pass over all requests against passes over at most ten, from the same pools: confidences and the K/V that are stored."""
+    shape = W.MODEL_SHAPES["tiny"]
+    model = B.odb_model_create(shape)
+    try:
+        B.odb_model_init_random(model, W.WEIGHT_SEED, W.WEIGHT_STD)
+        if head_gain is not None:
+            B.odb_model_set_tensor(model, B.T_GF, 0, np.full(shape["d_model"], int(np.float32(head_gain).view(np.uint32)) >> 16, np.uint16))
+        rng = np.random.default_rng(n)
+        lens = [int(x) for x in rng.integers(b, b + 80, n)]
+        first = [int(rng.integers(0, x - b + 1)) for x in lens]
+        tokens = rng.integers(0, shape["vocab"], (n, b))
+        pg = random_pages(shape, model, lens, 16, n)
+        positions = np.concatenate([f + np.arange(b) for f in first])
+        table = pg.tables.cpu().numpy()
+        slots = np.concatenate([table[r, (f + np.arange(b)) // 16] * 16 + (f + np.arange(b)) % 16 for r, f in enumerate(first)])
+
+        def step(lo, hi, k, v):
+            return B.odb_step_paged(model, ints(tokens[lo:hi]), k, v, pg.tables[lo:hi].contiguous(), ints(first[lo:hi]), ints(lens[lo:hi]), ints(positions[lo * b:hi * b]),
+                                    ints(slots[lo * b:hi * b]), pg.table, tau=0.5)
+        pools = [[x.clone() for x in (pg.k, pg.v)] for _ in range(2)]
+        conf, argmax, unmask = step(0, n, *pools[0])
+        parts = [step(lo, min(lo + 10, n), *pools[1]) for lo in range(0, n, 10)]
+        want_conf, want_argmax = (torch.cat([p[i] for p in parts]) for i in (0, 1))
+        assert (conf.log() - want_conf.log()).abs().max() <= LOG_CONF
+        # (a greedy token whose probability is above one half by more than the bar cannot change)
+        sure = want_conf > 0.55
+        assert (argmax[sure] == want_argmax[sure]).all() and (head_gain is None or sure.any())
+        for x, y, before in zip(pools[0], pools[1], (pg.k, pg.v)):
+            assert (x - y).abs().max() <= KV_TOL * y.abs().max()
+            changed = (x != before).any(-1).any(0).any(1)                # [pages, positions]
+            assert changed.flatten().nonzero().flatten().tolist() == sorted(slots.tolist())
+        B.odb_model_status(model)
+    finally:
+        B.odb_model_destroy(model)
+
+
+def test_a_refresh_of_700_positions_equals_the_dense_one_at_the_8b_width():
+    shape = dict(W.MODEL_SHAPES["8b"], n_layers=2)
+    model = B.odb_model_create(shape)
+    try:
+        B.odb_model_init_random(model, W.WEIGHT_SEED, W.WEIGHT_STD)
+        wl = W.decode_workload(shape, 300, 400, 32, 1, 5)
+        pg = Paged(shape, model, 1, 44, 16, 45)
+        conf, argmax, _ = pg.forward(wl.tokens, [0], [700], skip=300)
+        dense = B.odb_cache_create(model, 1, 700)
+        conf_d, argmax_d = B.odb_prefill(model, dense, ints(wl.tokens), 300)
+        assert conf.shape == conf_d.shape and (conf.log() - conf_d.log()).abs().max() <= LOG_CONF
+        for layer in range(2):
+            for kv in (0, 1):
+                want = B.odb_cache_read(dense, layer, kv, 0, 0, 700, shape["n_heads"], shape["head_dim"])
+                assert np.abs(pg.keys(0, layer, kv, 700) - want).max() <= KV_TOL * np.abs(want).max()
+        B.odb_cache_destroy(dense)
+        B.odb_model_status(model)
+    finally:
+        B.odb_model_destroy(model)
+
+
+def sure_of(logits):
+    """Rows whose two largest probabilities are further apart than the bar's margin."""
+    p = np.sort(np.exp(logits - logits.max(-1, keepdims=True)), -1)
+    return (p[..., -1] - p[..., -2]) / p.sum(-1) > MARGIN
+
+
+@pytest.mark.parametrize("n,b", [(24, 16), (7, 32), (3, 16)])
+def test_decisions_of_steps_equal_the_dense_ones_at_the_8b_width(n, b):
+    """n sequences of one length, which the dense cache takes too; a sharper last norm makes the decisions clear."""
+    shape = dict(W.MODEL_SHAPES["8b"], n_layers=2)
+    model = B.odb_model_create(shape)
+    try:
+        B.odb_model_init_random(model, W.WEIGHT_SEED, W.WEIGHT_STD)
+        B.odb_model_set_tensor(model, B.T_GF, 0, np.full(shape["d_model"], int(np.float32(12.0).view(np.uint32)) >> 16, np.uint16))
+        length, off = 80, 40
+        wl = W.decode_workload(shape, 30, length - 30, b, 1, 9, batch=n)
+        pg = Paged(shape, model, n, 5, 16, 5 * n + 1)
+        pg.forward(wl.tokens, [0] * n, [length] * n, head=False)
+        dense = B.odb_cache_create(model, n, length)
+        B.odb_prefill(model, dense, ints(wl.tokens), 0)
+        drafts = wl.tokens[:, off:off + b]
+        z = B.odb_block_step_logits(model, dense, ints(drafts[:, None]), off, shape["vocab"]).double().cpu().numpy()[:, 0]
+        conf_d, argmax_d, unmask_d = (x.cpu().numpy()[:, 0] for x in B.odb_block_step(model, dense, ints(drafts[:, None]), off, 0.9))
+        conf, argmax, unmask = (x.cpu().numpy() for x in pg.forward(drafts, [off] * n, [length] * n, tau=0.9))
+        assert np.abs(np.log(conf) - np.log(conf_d)).max() <= LOG_CONF
+        sure = sure_of(z)
+        assert sure.any() and (argmax[sure] == argmax_d[sure]).all()
+        for r in range(n):
+            masked = drafts[r] == shape["mask_id"]
+            best = np.sort(conf_d[r][masked])[-2:] if masked.sum() > 1 else np.array([0.0, 1.0])
+            # the acceptance is known where no confidence is near the threshold, and, if none passes it, where the most confident leads
+            if masked.any() and not (np.abs(conf_d[r] - 0.9) <= 0.9 * LOG_CONF).any() and (best[1] > 0.95 or best[1] - best[0] > 2 * LOG_CONF * best[1]):
+                assert (unmask[r] == unmask_d[r]).all(), r
+        B.odb_cache_destroy(dense)
+        B.odb_model_status(model)
+    finally:
+        B.odb_model_destroy(model)
+
+
+def oracle_step(cfg, w, cache, tokens, off):
+    """The block's logits in 64 bits, its K/V left in `cache` as the pages keep them."""
+    b = len(tokens)
+    h = w.embed_rows(tokens)
+    for layer in range(cfg.n_layers):
+        def kv(kn, vn, layer=layer):
+            cache.k[layer][off:off + b], cache.v[layer][off:off + b] = kn, vn
+            return [(slice(0, b), cache.k[layer], cache.v[layer])]
+        h, _, _ = o._layer(cfg, w, layer, h, off + np.arange(b), kv)
+    return o._head(cfg, w, h)
+
+
+@pytest.mark.parametrize("gain", [None, 32.0])
+def test_further_steps_see_the_blocks_of_earlier_ones(gain):
+    """Three turns on overlapping and other blocks of ragged requests: the oracle keeps a stepped block's K/V as the pages do."""
+    shape = W.MODEL_SHAPES["tiny"]
+    cfg = o.Config(**shape)
+    w = o.Weights(cfg, W.WEIGHT_SEED, W.WEIGHT_STD)
+    model = B.odb_model_create(shape)
+    try:
+        B.odb_model_init_random(model, W.WEIGHT_SEED, W.WEIGHT_STD)
+        if gain is not None:
+            w.set_values(o.T_GF, 0, np.full(cfg.d_model, gain, np.float32))
+            B.odb_model_set_tensor(model, B.T_GF, 0, w.bits(o.T_GF, 0))
+        lens, b, rng = [70, 33, 129], 16, np.random.default_rng(2)
+        work = [W.decode_workload(shape, 10, x - 10, b, 1, 70 + x) for x in lens]
+        pg, caches = Paged(shape, model, 3, 6, 32, 14), []
+        for r, wl in enumerate(work):
+            pg.forward(wl.tokens, [0], [lens[r]], which=[r], head=False)
+            caches.append(o.prefill(cfg, w, wl.tokens[0], 0)[0])
+        for offs in ([40, 17, 113], [48, 1, 77], [40, 9, 64]):
+            drafts = rng.integers(0, shape["vocab"] - 1, (3, b))
+            drafts[rng.random((3, b)) < 0.5] = shape["mask_id"]
+            conf, argmax, unmask = (x.cpu().numpy() for x in pg.forward(drafts, offs, lens, tau=0.9))
+            for r in range(3):
+                z = oracle_step(cfg, w, caches[r], drafts[r], offs[r])
+                conf_o, argmax_o = o.confidence_argmax(z)
+                decide(conf[r], argmax[r], conf_o, argmax_o, z)
+                unmask_o = o.threshold_unmask(drafts[r], conf_o, 0.9, cfg.mask_id)
+                masked = drafts[r] == shape["mask_id"]
+                best = np.sort(conf_o[masked])[-2:] if masked.sum() > 1 else np.array([0.0, 1.0])
+                if not (np.abs(conf_o - 0.9) <= 0.9 * LOG_CONF).any() and (best[1] > 0.95 or best[1] - best[0] > 2 * LOG_CONF * best[1]):
+                    assert (unmask[r] == unmask_o).all()
+                for layer in range(cfg.n_layers):
+                    for kv, want in ((0, caches[r].k[layer]), (1, caches[r].v[layer])):
+                        assert np.abs(pg.keys(r, layer, kv, lens[r]) - want).max() <= KV_TOL * np.abs(want).max()
+        B.odb_model_status(model)
     finally:
         B.odb_model_destroy(model)
