@@ -471,7 +471,8 @@ int odb_rope_table(float *table_dev, int n_pos, int rot_dim, const odb_rope *rop
  *               is stored.  A slot outside the pool stores nothing.  Slots must differ: of two rows with the same slot
  *               either's values may remain, piece by piece.
  *   q_out       dev [rows, n_heads, head_dim] of the pages' dtype, rows q_out_row elements apart; may be q itself
- *               (same dtype and stride), otherwise it must not overlap q, k or v
+ *               (same dtype and stride; k and v then lie beside it, between its rows only with its stride), otherwise its
+ *               range, from the first row's beginning to the last one's end, must not overlap those of q, k and v
  *   row_end     dev int32 [1] or NULL: rows from this one on are padding rows, whatever their positions and slots (a captured step of
  *               fixed size whose number of rows is known on the device alone)
  * Requirements: buffers aligned to 16 bytes, row strides multiples of 8, rot_dim a multiple of 16 in [16, head_dim].
@@ -514,7 +515,7 @@ int odb_qk_norm_rope(const odb_qk_rows *rows, const odb_pages *pages, void *stre
  * Asynchronous on `stream`.  Errors: ODB_E_INVALID_ARG for NULL buffers, n outside [1, 4096], rows outside [0, 2^24] (0: nothing is
  * launched), n_heads no multiple of n_kv_heads, columns < 1, columns * page_size > 2^30, a scale that is not positive or, times
  * log2(e), not finite, window or sinks negative or above 2^30, a workspace that is too small, buffers not aligned to 16 bytes, row
- * strides that are no multiples of 8, out overlapping q, rows * n_heads above 2^30, pools
+ * strides that are no multiples of 8, out's range overlapping q's, rows * n_heads above 2^30, pools
  * outside the requirements above. */
 typedef struct {
     const void *q;

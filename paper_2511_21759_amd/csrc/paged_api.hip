@@ -193,6 +193,15 @@ int odb_qk_norm_rope(const odb_qk_rows *rows, const odb_pages *pages, void *stre
     if (!in_place && (overlap(out, Range{r.q, span(r.rows, r.q_row, r.n_heads, dim, eb)}) || overlap(out, Range{r.k, span(r.rows, r.k_row, kv, dim, eb)}) ||
                       overlap(out, Range{r.v, span(r.rows, r.v_row, kv, dim, eb)})))
         return fail(ODB_E_INVALID_ARG, "%s: q_out overlaps q, k or v without being q itself", who);
+    // (in place, the rows of k and v may lie between those of q, as in a fused buffer, but a lane must not read what another has written)
+    auto beside = [&](const void *x, long long row) {
+        if (!overlap(out, Range{x, span(r.rows, row, kv, dim, eb)})) return true;
+        if (r.rows > 1 && row != r.q_row) return false;
+        const long long bytes = r.rows > 1 ? row * eb : 1ll << 62, gap = (((intptr_t)x - (intptr_t)r.q) % bytes + bytes) % bytes;
+        return gap >= (long long)r.n_heads * dim * eb && gap + (long long)kv * dim * eb <= bytes;
+    };
+    if (in_place && !(beside(r.k, r.k_row) && beside(r.v, r.v_row)))
+        return fail(ODB_E_INVALID_ARG, "%s: in place, k and v must not share elements with q (rows of one stride, or buffers apart)", who);
     if (r.rows == 0) return ODB_OK;
     launch_qk_norm_rope(QkNormRope{r.q, r.k, r.v, r.in_dtype, r.q_row, r.k_row, r.v_row, r.rows, r.n_heads, r.q_gain, r.k_gain, r.eps, r.table, r.n_pos,
                                    r.rot_dim, r.interleaved, r.positions, r.slots, r.q_out, r.q_out_row, *pages, r.row_end, nullptr}, (hipStream_t)stream);

@@ -188,3 +188,35 @@ def test_rows_whose_scores_are_beyond_the_range_become_no_numbers(rows, lens, he
     off = u + (dim + 4) * F * big[..., None] + 8 * F + max(lens) * F / 4
     bound = 2 * off * size * (1 + 4 * off) + u * want.abs() * (1 + u) + torch.finfo(dt).tiny * torch.finfo(dt).eps
     assert ((got - want).abs()[~beyond] <= bound[~beyond]).all()
+
+
+# ---- in place -------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("rows", [1, 2, 33])
+@pytest.mark.parametrize("order", ["qkv", "kvq", "vqk"])
+def test_rotation_in_place_with_keys_and_values_on_either_side(rows, order):
+    g = torch.Generator().manual_seed(rows)
+    width = dict(q=4, k=2, v=2)
+    fused = torch.randn(rows, 8, 64, generator=g).half().cuda()
+    at, parts = 0, {}
+    for name in order:
+        parts[name] = fused[:, at:at + width[name]]
+        at += width[name]
+    table, positions, slots = B.odb_rope_table(64, 64, 10000.0), ints(np.arange(rows)), ints(np.arange(rows)[::-1] + 5)
+    pools = [[torch.zeros(6, 2, 16, 64, dtype=torch.float16, device="cuda") for _ in range(2)] for _ in range(2)]
+    want = B.odb_qk_norm_rope(parts["q"], parts["k"], parts["v"], *pools[0], table, positions, slots)
+    before = {name: x.clone() for name, x in parts.items()}
+    got = B.odb_qk_norm_rope(parts["q"], parts["k"], parts["v"], *pools[1], table, positions, slots, out=parts["q"])
+    assert got.data_ptr() == parts["q"].data_ptr() and torch.equal(got, want)
+    assert all(torch.equal(parts[x], before[x]) for x in "kv") and all(torch.equal(x, y) for x, y in zip(*pools))
+
+
+def test_queries_that_are_also_the_keys():
+    """One tensor as Q and K: right into another buffer, refused in place, where keys would be read after they were turned."""
+    x = torch.randn(20, 2, 64, generator=torch.Generator().manual_seed(1)).half().cuda()
+    table, positions, slots = B.odb_rope_table(64, 64, 10000.0), ints(np.arange(20)), ints(np.arange(20))
+    k, v = (torch.zeros(2, 2, 16, 64, dtype=torch.float16, device="cuda") for _ in range(2))
+    q = B.odb_qk_norm_rope(x, x, x, k, v, table, positions, slots)
+    assert torch.equal(q, k.permute(0, 2, 1, 3).reshape(-1, 2, 64)[:20])
+    with pytest.raises(B.OdbError, match="in place"):
+        B.odb_qk_norm_rope(x, x, x, k, v, table, positions, slots, out=x)

@@ -24,3 +24,23 @@ def test_row_end_is_one_number_on_the_device_of_the_others():
     for bad in (torch.zeros(2, dtype=i32), torch.zeros((), dtype=i32), torch.zeros(1), torch.zeros(1, dtype=torch.int64)):
         with pytest.raises(TypeError):
             B.odb_qk_norm_rope(**rows, row_end=bad)
+
+
+INVALID = -1
+
+
+def qk_rows(**kw):
+    """Heads 4 over 2 of 64, in place in a fused buffer of 512 elements a row."""
+    big = 1 << 30
+    a = dict(q=big, k=big + 2 * 256, v=big + 2 * 384, in_dtype=0, rows=5, n_heads=4, q_row=512, k_row=512, v_row=512, q_gain=None, k_gain=None, eps=1e-5,
+             table=0x10000, n_pos=100, rot_dim=64, interleaved=0, positions=0x20000, slots=0x30000, q_out=big, q_out_row=512)
+    a.update(kw)
+    return B.odb_qk_rows(**a)
+
+
+@pytest.mark.parametrize("kw", [dict(k=1 << 30), dict(v=1 << 30), dict(k=(1 << 30) + 2 * 192), dict(v=(1 << 30) + 2 * 248), dict(k=(1 << 30) - 2 * 64),
+                                dict(v=(1 << 30) + 2 * 448), dict(k=(1 << 30) + 2 * 512), dict(k=(1 << 30) + 2 * 256, k_row=520), dict(v=(1 << 30) + 2 * 384, v_row=1024)])
+def test_keys_and_values_that_share_elements_with_queries_in_place_are_refused(kw):
+    lib, pages = B.lib(), B.odb_pages(k=0x10000, v=0x20000, n_pages=10, page_size=16, n_kv_heads=2, head_dim=64, dtype=0, page_stride=2048, head_stride=1024, pos_stride=64)
+    assert lib.odb_qk_norm_rope(ctypes.byref(qk_rows(**kw)), ctypes.byref(pages), None) == INVALID
+    assert b"in place" in lib.odb_last_error()
