@@ -418,7 +418,7 @@ typedef struct {
  *   tables         dev int32 [n, columns], read and written: entries of pages that were taken; all others stay as they are
  *   free_pages     dev int32 [n_pages], read and written; n_free dev int32 [1]: how many of its entries are free pages
  *   row_first, row_count   dev int32 [n]: the positions that the step computes, row_count[r] of them from row_first[r] on;
- *                  either may be NULL: held[r], and wanted[r] - held[r] (none where that is negative)
+ *                  either may be NULL: held[r], and wanted[r] - held[r] (none where that is negative or wanted[r] no length of the table)
  * written:
  *   len            dev int32 [n]: wanted[r], or held[r] where refused
  *   cu_rows        dev int32 [n + 1]: rows in front of each request; all are capped at rows_cap
@@ -443,7 +443,8 @@ int odb_page_tables(const int32_t *held_dev, const int32_t *wanted_dev, int n, i
  *   ODB_ROPE_LINEAR  f_j / factor
  *   ODB_ROPE_NTK     base * factor^(rot_dim / (rot_dim - 2)) instead of base (rot_dim = 2: unchanged)
  *   ODB_ROPE_YARN    f_j (w + (1 - w) / factor), w = (original_len * f_j / 2 pi - beta_slow) / (beta_fast - beta_slow)
- *                    clamped to [0, 1] (YaRN, arXiv 2309.00071: by the turns that a pair makes in the original context) */
+ *                    clamped to [0, 1] (YaRN, arXiv 2309.00071: by the turns that a pair makes in the original context; a ramp over
+ *                    the pairs' numbers between two bounds, as some configurations have it, is not expressed so) */
 enum { ODB_ROPE_PLAIN = 0, ODB_ROPE_LINEAR, ODB_ROPE_NTK, ODB_ROPE_YARN };
 typedef struct {
     double base;
@@ -505,7 +506,8 @@ int odb_qk_norm_rope(const odb_qk_rows *rows, const odb_pages *pages, void *stre
  *            pool stands for positions that nobody sees
  *   first_pos  dev int32 [n], or NULL: the rows are the last positions, kv_len[r] - their number
  *   max_rows, max_len   upper bounds of a request's rows and positions, or 0 where none are known (rows; columns *
- *            page_size).  They choose the way of computing; a bound that does not hold costs time, not correctness.
+ *            page_size).  They choose the way of computing; a bound that does not hold costs time, not correctness, and so does
+ *            none: max_rows is 1 for single tokens, with cu_rows or without (24 of 1000 positions 26 us, with 0 34).
  *   workspace  dev, odb_paged_attention_workspace() bytes, aligned to 256, NULL where that says 0; holds the
  *            sums of keys that are split over workgroups, means nothing between calls, must not be shared by calls that
  *            overlap in time

@@ -602,7 +602,8 @@ def odb_paged_attention(q, k_pages, v_pages, tables, kv_len, *, causal: bool, cu
                         window: int = 0, sinks: int = 0, max_rows: int = 0, max_len: int = 0, out=None, workspace=None):
     """q [rows, n_heads, head_dim] of the pages' dtype; tables int32 [n, columns]; kv_len int32 [n]; cu_rows int32 [n + 1] (None:
     one row per request); first_pos int32 [n] (None: the rows are the last positions); scale defaults to head_dim ** -0.5
-    -> [rows, n_heads, head_dim].  The workspace comes from torch's allocator unless a uint8 tensor is given."""
+    -> [rows, n_heads, head_dim].  max_rows and max_len, bounds of a request's rows and positions, choose the way of computing: give
+    max_rows=1 for single tokens.  The workspace comes from torch's allocator unless a uint8 tensor is given."""
     torch = _torch or _load_torch()
     index, pages, i32 = q.get_device(), _pages(k_pages, v_pages), torch.int32
     shape = rows, heads, dim = q.shape

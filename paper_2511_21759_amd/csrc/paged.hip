@@ -261,7 +261,9 @@ __device__ __forceinline__ void store8(T *p, f32x8 x) {
 // part hold two neighbouring eights that pass through.  A wave does as many heads of one row as it has groups of lanes, and nothing
 // else: with loops over more heads, which would load the row's angles once for all of them, the large call is slower.  Bound by the
 // memory, every element read and written once: 16411 rows of 48 heads of 128 bfloat16, 408 MB, take 81 us (5.0 TB/s; a copy reaches
-// 4.9), with two or three times as many heads per wave 84 to 89; loads past the caches take 100.
+// 4.9), with two or three times as many heads per wave 84 to 89; loads past the caches take 100.  Few rows are bound by loads that wait
+// for each other, position and slot, then angles, then the row (9 rows 3.8 us, 224 of 96 heads 5.6), though the row's address needs
+// neither of the first.
 template <class TI, class TO, int DH, bool INTER>
 __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkNormRope a, int waves_per_row) {
     constexpr int LANES = DH / 16, HEADS = 64 / LANES;          // lanes per head, heads per wave

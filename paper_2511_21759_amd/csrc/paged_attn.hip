@@ -1162,13 +1162,16 @@ void paged_attn_plan(const odb_pages &p, int n, int rows, int group, int max_row
     auto tiles = [&](int tile_rows) { return (long long)(n < rows ? n : rows) + (long long)rows * group / tile_rows; };
     auto numbers = [&](int tile_rows) { return (n + (long long)rows * group / tile_rows) | 1; };      // (find_place; odd: no pattern survives)
     // Tiles of many rows, where more than half of one is full: whole if there is one for every CU, in pieces if fewer see long keys, or if
-    // requests of different lengths may leave CUs waiting for the longest.  Else the waves split the keys of smaller tiles, which
-    // need cuts of their own if they are not far more than the CUs.  Whole / pieces / keys split by waves, us; full attention, 32
+    // there may be requests whose lengths differ and leave CUs waiting for the longest.  Else the waves split the keys of smaller tiles,
+    // which need cuts of their own if they are not far more than the CUs.  Whole / pieces / keys split by waves, us; full attention, 32
     // query heads over 8 of 128:
-    //   rows of positions    512 of 512  20 / 34 / 19    600 of 600  25 / 42 / 41    704 of 2000  59 / 59 / 75    704 of 5000  130 / 94 / 126
-    //                        256 of 2048 56 / 53 / 34    512 of 4096 106 / 68 / 67   512 of 8192  202 / 102 / 117  300 of 12000 292 / 110 / 118
-    //   requests x rows      32 x 24 of 4000  117 / 128 / 194      64 x 24 of 300 to 5000  148 / 109 / 162      8 x 24 of 2000  58 / 38 / 40
-    // 32 heads over 32: 8 x 64 of 700  27 / 41 / 30, 8 x 80 of 700  29 / 45 / 49, 8 x 80 of 2000  63 / 76 / 102
+    //   rows of positions    512 of 512  21 / 35 / 19    600 of 600  25 / 42 / 39    704 of 2000  60 / 59 / 73    704 of 5000  130 / 95 / 127
+    //                        256 of 2048 57 / 53 / 33    512 of 4096 107 / 68 / 63   512 of 8192  203 / 105 / 114  300 of 12000 295 / 113 / 117
+    //   requests x rows      32 x 24 of 4000  114 / 126 / 135      64 x 24 of 300 to 5000  149 / 109 / 162      8 x 24 of 2000  58 / 38 / 39
+    // 32 heads over 32: 8 x 64 of 700  27 / 27 / 27, 8 x 80 of 700  28 / 44 / 43, 8 x 80 of 2000  63 / 76 / 81
+    // Lengths themselves are not known here, so `ragged` is a guess: that requests of up to 64 stages are of like lengths, and longer ones
+    // are not.  Whole / pieces where it is right and where it is not: 32 x 24 rows of 300 to 5000 115 / 64, of 8000 each 216 / 215, of 5000 each
+    // 143 / 151, of 300 to 3600 93 / 56; 64 x 24 of 1000 to 8000 253 / 199, of 5000 each 241 / 249, of 300 to 3600 114 / 98.
     const int many = many_rows(p), keys = p.head_dim == 256 ? RowsShape<256>::SK : RowsShape<128>::SK;
     const long long likely = min(tiles(many), (long long)n * ((most + many - 1) / many));      // (max_rows may not hold)
     const long long groups = likely * p.n_kv_heads, stages = (max_len + keys - 1) / keys;
@@ -1188,13 +1191,18 @@ void paged_attn_plan(const odb_pages &p, int n, int rows, int group, int max_row
         }
     }
     *nt = most <= 16 ? 1 : most <= 32 || p.head_dim == 256 ? 2 : 4;
-    // One round of workgroups.  Two per CU hide each other's starts and ends where a tile is 16 rows (64 single tokens over 555 MB:
-    // 107 us, with one 110, with four 107; two over 985 MB 156, 153, 158); with more rows every cut costs more sums (8 x 32 rows: one
-    // 59 us, two 62, four 68).
+    // One round of workgroups, two per CU where a tile is 16 rows (one / two / four: 64 single tokens over 555 MB 96 / 97 / 100 us, two over
+    // 985 MB 152 / 154 / 157, 48 of 17 to 16384 positions over 32 heads 194 / 192 / 188); with more rows every cut costs more sums (8 x 32 rows
+    // of 500 to 3000: 50 / 52 / 57).
     const int aim = (256 * (*nt == 1 && p.head_dim != 256 ? 2 : 1) + p.n_kv_heads - 1) / p.n_kv_heads;
-    // With four row tiles for every workgroup the lengths even out by themselves, and a tile then reads only the keys it sees.  Short
-    // keys are not worth the cuts and the join either.  Whole / pieces, single tokens, 32 heads over 8 of 128: 4 of 600 positions 12.3 /
-    // 15.6 us, 4 of 800 15.9 / 14.8, 16 of 800 17.9 / 21.3, 32 of 1000 26.6 / 32.9, 65 of 1000 62 / 57; 4 x 32 rows of 1000, 32 heads, 19.5 / 23.8.
+    // Where the bound on the row tiles, which counts one more than the full ones for every request, is four of that round the keys stay
+    // whole, and a tile reads only those that it sees.  Short keys are not worth the cuts and the join either.  Whole / pieces:
+    //   equal lengths     64 single tokens of 2000, 32 heads over 32  333 / 326 us    16 x 32 rows of 1500  77 / 83    32 x 32 of 1500  147 / 158
+    //   blocks, ragged    16 x 32 rows of 500 to 3000, 32 heads over 32  71 / 70       32 x 32  137 / 138
+    //   tokens, ragged    64 of 17 to 16384, 32 heads over 32  457 / 284               256, 32 over 8  663 / 397
+    // The last line is what this rule, which does not know the lengths, gives away: all workgroups of such a call run at once, and the longest
+    // request sets its time.  Short keys, 32 heads over 8 of 128: 4 single tokens of 600 positions 14.2 / 15.8, 4 of 800 16.1 / 14.8, 16 of 800
+    // 19.0 / 21.3, 32 of 1000 25.6 / 31.3, 65 of 1000 60 / 54; 4 x 32 rows of 1000, 32 heads over 32, 19.7 / 23.8.
     const int tile_rows = 16 * *nt;
     const long long pairs = min(tiles(tile_rows), (long long)n * ((most + tile_rows - 1) / tile_rows)) * p.n_kv_heads;
     const long long channels = (max_len + 31) / 32 * p.head_dim;
