@@ -1168,7 +1168,7 @@ void paged_attn_plan(const odb_pages &p, int n, int rows, int group, int max_row
     //   rows of positions    512 of 512  21 / 35 / 19    600 of 600  25 / 42 / 39    704 of 2000  60 / 59 / 73    704 of 5000  130 / 95 / 127
     //                        256 of 2048 57 / 53 / 33    512 of 4096 107 / 68 / 63   512 of 8192  203 / 105 / 114  300 of 12000 295 / 113 / 117
     //   requests x rows      32 x 24 of 4000  114 / 126 / 135      64 x 24 of 300 to 5000  149 / 109 / 162      8 x 24 of 2000  58 / 38 / 39
-    // 32 heads over 32: 8 x 64 of 700  27 / 27 / 27, 8 x 80 of 700  28 / 44 / 43, 8 x 80 of 2000  63 / 76 / 81
+    // 32 heads over 32: 8 x 80 of 700  28 / 44 / 43, 8 x 80 of 2000  63 / 76 / 81
     // Lengths themselves are not known here, so `ragged` is a guess: that requests of up to 64 stages are of like lengths, and longer ones
     // are not.  Whole / pieces where it is right and where it is not: 32 x 24 rows of 300 to 5000 115 / 64, of 8000 each 216 / 215, of 5000 each
     // 143 / 151, of 300 to 3600 93 / 56; 64 x 24 of 1000 to 8000 253 / 199, of 5000 each 241 / 249, of 300 to 3600 114 / 98.
