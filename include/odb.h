@@ -24,6 +24,8 @@
  *     on one stream at a time (they share scratch).  A model's scratch grows with the largest call it has served
  *     and is freed with the model; beside the activations of that call it holds 32 MiB of partial sums for split
  *     projections, with many rows up to 96 MiB (16 bytes per row and channel; 32 MiB where more cannot be had).
+ *     While a stream is captured into a graph scratch cannot grow (ODB_E_UNSUPPORTED: make the call once before);
+ *     that of a captured call stays where it is when a larger call takes new scratch later.
  *   - Every function returns ODB_OK (0) or a negative ODB_E_* code; a message
  *     for the last failure on the calling thread is kept in odb_last_error().
  *     Arguments are validated on the host before any kernel is launched, so an

@@ -102,10 +102,25 @@ size_t lm_stats_excess(const odb_config &c, int rows_pad) {
     return align_up(row * parts, 256) - align_up(row * wide, 256);
 }
 
+// A call that is captured into a graph finds its scratch there already, and leaves word that the graph holds its address.
 int ensure_scratch(Model &m, size_t bytes, hipStream_t s) {
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing(s, &capture) != hipSuccess) (void)hipGetLastError();
+    if (capture != hipStreamCaptureStatusNone) {
+        if (bytes > m.scratch_bytes)
+            return fail(ODB_E_UNSUPPORTED, "scratch of %zu bytes cannot be allocated while the stream is captured: make the call once before", bytes);
+        m.scratch_captured = true;
+    }
     if (bytes <= m.scratch_bytes) return ODB_OK;
     HIP_TRY(hipStreamSynchronize(s));
-    dev_free(m, m.scratch);
+    if (m.scratch_captured) {
+        Model::OldScratch *old = new (std::nothrow) Model::OldScratch{m.scratch, m.old_scratch};
+        if (!old) return fail(ODB_E_NOMEM, "host allocation failed");
+        m.old_scratch = old;
+        m.scratch_captured = false;
+    } else {
+        dev_free(m, m.scratch);
+    }
     m.scratch = nullptr;
     m.scratch_bytes = 0;
     size_t want = align_up(bytes + bytes / 8, 1 << 20);
@@ -539,6 +554,12 @@ void odb_model_destroy(odb_model *mh) {
     dev_free(m, m.gf);
     dev_free(m, m.counters);
     dev_free(m, m.scratch);
+    while (m.old_scratch) {
+        Model::OldScratch *old = m.old_scratch;
+        m.old_scratch = old->next;
+        dev_free(m, old->p);
+        delete old;
+    }
     dev_free(m, m.staging);
     if (m.prof_ev) {
         for (int i = 0; i < 3 * m.prof_cap; i++) (void)hipEventDestroy(m.prof_ev[i]);

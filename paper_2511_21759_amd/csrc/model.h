@@ -32,6 +32,8 @@ struct Model {
     // scratch, grown on demand (see api.hip)
     void *scratch;
     size_t scratch_bytes;
+    bool scratch_captured;     // a graph holds its address: it stays until the model goes, also when a larger one takes its place
+    struct OldScratch { void *p; OldScratch *next; } *old_scratch;
     bool least_partials;       // no more room for K-split partial sums than every call has (see plan_scratch)
     unsigned *counters;        // [0] status word (kStatus* bits), [1024..2048) Workspace::arrive, [2048..3072) Workspace::exchange
     bool ksplit_reduce;        // workgroups of a launch may exchange partial sums (ODB_OPT_KSPLIT_REDUCE)

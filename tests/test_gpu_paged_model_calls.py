@@ -271,3 +271,57 @@ def test_further_steps_see_the_blocks_of_earlier_ones(gain):
         B.odb_model_status(model)
     finally:
         B.odb_model_destroy(model)
+
+
+# ---- captured ---------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dense", [False, True])
+def test_captured_steps_outlive_larger_calls(dense):
+    """A graph holds the address of the scratch that its step uses; a larger call takes new scratch, and the graph is replayed again."""
+    shape = W.MODEL_SHAPES["tiny"]
+    model = B.odb_model_create(shape)
+    try:
+        B.odb_model_init_random(model, W.WEIGHT_SEED, W.WEIGHT_STD)
+        lens, b, rng = [70, 33, 129], 16, np.random.default_rng(4)
+        pg = random_pages(shape, model, lens, 16, 8)
+        table = pg.tables.cpu().numpy()
+        first = [40, 17, 100]
+        positions = np.concatenate([f + np.arange(b) for f in first])
+        slots = np.concatenate([table[r, (f + np.arange(b)) // 16] * 16 + (f + np.arange(b)) % 16 for r, f in enumerate(first)])
+        tokens = ints(rng.integers(0, shape["vocab"], (3, b)))
+        args = [ints(first), ints(lens), ints(positions), ints(slots)]
+        cache = B.odb_cache_create(model, 1, 1200)
+        small = W.decode_workload(shape, 20, 44, b, 1, 3)
+
+        def step():
+            if dense:
+                return B.odb_block_step(model, cache, tokens[None, :1], 24, 0.5)
+            return B.odb_step_paged(model, tokens, pg.k, pg.v, pg.tables, *args, pg.table, tau=0.5)
+        graph = torch.cuda.CUDAGraph()
+        if not dense:
+            with pytest.raises(B.OdbError, match="captured"):         # nothing was allocated yet
+                with torch.cuda.graph(graph):
+                    step()
+            graph = torch.cuda.CUDAGraph()
+        B.odb_prefill(model, cache, ints(small.tokens), 0)
+        step()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph):
+            out = step()
+        large = W.decode_workload(shape, 500, 700, b, 1, 5)
+        for turn in range(4):
+            tokens.copy_(ints(rng.integers(0, shape["vocab"], (3, b))))
+            if turn in (1, 3):                                        # takes more scratch than everything before
+                B.odb_prefill(model, cache, ints(large.tokens[:, :400 * turn]), 0)
+                B.odb_prefill(model, cache, ints(small.tokens), 0)
+                fill = [torch.full((1 << 24,), float("nan"), device="cuda") for _ in range(4)]       # what was freed would be written over
+            graph.replay()
+            torch.cuda.synchronize()
+            got = [x.clone() for x in out]
+            for x, y in zip(got, step()):
+                assert torch.equal(x, y), turn
+        del fill
+        B.odb_model_status(model)
+        B.odb_cache_destroy(cache)
+    finally:
+        B.odb_model_destroy(model)
