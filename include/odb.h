@@ -501,7 +501,7 @@ int odb_qk_norm_rope(const odb_qk_rows *rows, const odb_pages *pages, void *stre
  * sees key i (whatever the pages hold there, the rows' own K/V included once they are stored) iff
  *   i < kv_len[r],  and with causal i <= p,  and with window > 0  |p - i| < window or i < sinks.
  * A row that sees no key becomes zero.  What lies at positions that a row does not see has no influence on it, not even
- * if it is infinite or no number.  Query head h reads K/V head h / (n_heads / n_kv_heads).
+ * if it is infinite or no number; a key whose score is minus infinity counts as one that is not seen.  Query head h reads K/V head h / (n_heads / n_kv_heads).
  *   q, out   dev [rows, n_heads, head_dim] of the pages' dtype, rows q_row / out_row elements apart
  *   cu_rows  dev int32 [n + 1], rising from 0; NULL: one row per request (rows = n).  Rows that belong to no request stay.
  *   kv_len   dev int32 [n], clamped to [0, columns * page_size];  tables dev int32 [n, columns]: an entry outside the
