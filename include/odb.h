@@ -574,6 +574,76 @@ typedef struct {
 } odb_paged_rows;
 int odb_step_paged(odb_model *m, const odb_paged_rows *rows, const odb_pages *layer0, void *stream);
 
+/* ---- Paged K/V in 8 bits ---------------------------------------------------------------------------------------
+ * Pages as above, at half the bytes: an element is a code, and its value is code * scale, with one scale, float >= 0, for every `group`
+ * consecutive positions of a page and K/V head, K and V each their own.  Codes are ODB_INT8, -127 .. 127, or ODB_E4M3 (four bits of
+ * exponent, three of mantissa, largest 448; the codes 0x7f and 0xff are no numbers and are never stored).
+ * Element (page, head, position inside the page, channel) of k and of v lies at page * page_stride + head * head_stride + position *
+ * pos_stride + channel bytes, its scale at page * scale_page_stride + head * scale_head_stride + position / group floats.
+ * Requirements: page_size, head_dim and n_pages as for odb_pages; group 1, 16, 32 or 64, at most page_size; strides not negative, those of codes
+ * multiples of 16, pos_stride below 2^24, with group 1 those of scales multiples of 4; all four buffers aligned to 16 bytes.  Scales must be
+ * finite numbers that are not negative where positions are visible; what codes and scales hold elsewhere means nothing. */
+enum { ODB_INT8 = 3, ODB_E4M3 = 4 };
+typedef struct {
+    void *k, *v;                    /* dev: codes */
+    float *k_scale, *v_scale;       /* dev */
+    int n_pages, page_size, n_kv_heads, head_dim, codes, group;
+    int dtype;                      /* of queries and results: ODB_F16 or ODB_BF16 */
+    long long page_stride, head_stride, pos_stride, scale_page_stride, scale_head_stride;
+} odb_quant_pages;
+
+/* odb_qk_norm_rope into such pages: norms of queries and keys, their rotation, and K/V to codes in one pass over the projection's output.
+ * Request r (of n) has rows cu_rows[r] .. cu_rows[r + 1] - 1, at positions first_pos[r], first_pos[r] + 1, ... of its pages, as for
+ * odb_paged_attention; kv_len[r] is its length with them.  For every group of positions that rows fall into, and every K/V head:
+ *   a = the largest magnitude of the new values;  s = a / M (M = 127 or 448), or the scale that is there if that is larger and other
+ *   positions of the group below kv_len[r] stay;  codes of the new values = value / s to the nearest code, ties to even (value * M / a
+ *   in 32 bits, so that the rounding of s moves no tie);  where s grows, codes that stay are rounded anew to it, else they are left alone.
+ * A group whose values are all below 2^-100, with nothing that stays, has codes and scale zero.  Positions of the group that are not
+ * below kv_len[r] are left alone.  The same call again writes the same codes and scales.
+ * Of values that are not finite, infinities become the largest code of their sign and no numbers become zero; they do not count for a,
+ * and *odd is set to 1 (it is never cleared).
+ *   q, k, v, in_dtype, rows, n_heads, strides, gains, eps, table, n_pos, rot_dim, interleaved, q_out   as for odb_qk_norm_rope; in_dtype is
+ *               ODB_F32 or the pages' dtype, which q_out has
+ *   positions   dev int32 [rows]: of the angles.  A position outside [0, n_pos) marks a padding row: its queries become zero, nothing is stored
+ *   cu_rows     dev int32 [n + 1], rising from 0, or NULL: one row per request (rows = n).  Rows that belong to no request are padding
+ *   first_pos   dev int32 [n], or NULL: the rows are the last positions
+ *   kv_len      dev int32 [n], tables dev int32 [n, columns], as for odb_paged_attention.  Rows at positions that are not below kv_len[r], or
+ *               in no page of the pool, are not stored.  No group may hold new rows of two requests, or new rows of one and positions
+ *               that another reads (a prefix that requests share ends with a group)
+ *   odd         dev int32 [1] or NULL
+ * Asynchronous on `stream`.  rows = 0 launches nothing.  Errors: ODB_E_INVALID_ARG, also for sizes beyond one launch (2^24 workgroups). */
+typedef struct {
+    const void *q, *k, *v;
+    int in_dtype, rows, n_heads;
+    long long q_row, k_row, v_row;
+    const float *q_gain, *k_gain;
+    float eps;
+    const float *table;
+    int n_pos, rot_dim, interleaved;
+    const int32_t *positions;
+    void *q_out;
+    long long q_out_row;
+    const int32_t *cu_rows, *first_pos, *kv_len, *tables;
+    int columns, n;
+    int32_t *odd;
+} odb_quant_rows;
+int odb_qk_norm_rope_quant(const odb_quant_rows *rows, const odb_quant_pages *pages, void *stream);
+
+/* Values of positions: k_out and v_out, dev [rows, n_kv_heads, head_dim] of out_dtype (ODB_F16, ODB_BF16 or ODB_F32), rows k_row and v_row elements
+ * apart.  slots dev int32 [rows] as odb_page_tables writes them; a slot outside the pool gives zeros.  code * scale in 32 bits, rounded
+ * once, to an infinity beyond the type's range.  (pages->dtype is not looked at.)  Requirements: outputs aligned to 16 bytes, strides multiples of 8,
+ * outputs that do not overlap.  Asynchronous on `stream`.  rows = 0 launches nothing.  Errors: ODB_E_INVALID_ARG, also where rows * n_kv_heads *
+ * head_dim reaches 2^34. */
+int odb_paged_read_quant(const odb_quant_pages *pages, const int32_t *slots, int rows, int out_dtype, void *k_out, void *v_out, long long k_row,
+                         long long v_row, void *stream);
+
+/* odb_paged_attention over such pages: the same arguments and masks, and the same errors; q and out have pages->dtype.
+ * Queries meet the codes in binary16, which holds every code (bfloat16 queries as multiples of a power of two of their row's largest, within
+ * 2^-33 of it), probabilities times V's scales are rounded to binary16; scores and sums are 32-bit.  The largest score that a row sees, times
+ * scale * log2(e), has to stay below 2^27 in magnitude (the results of a row where it does not are no numbers). */
+int odb_paged_attention_quant(const odb_attention *a, const odb_quant_pages *pages, void *stream);
+long long odb_paged_attention_quant_workspace(const odb_attention *a, const odb_quant_pages *pages);
+
 /* Copies cached K (kv = 0, post-RoPE, logical channel order) or V (kv = 1) of
  * positions pos0 .. pos0+n-1 of one sequence and layer to host memory as
  * float [n, n_heads, head_dim].  Synchronous (device-wide). */

@@ -26,7 +26,8 @@ SYMBOLS = (
     "odb_predict_length", "odb_accept_jump", "odb_block_step_shared", "odb_block_step_static",
     "odb_block_step_shared_rows", "odb_block_step_shared_logits", "odb_cache_truncate", "odb_generate",
     "odb_speculative_jump", "odb_page_tables", "odb_rope_table", "odb_qk_norm_rope", "odb_paged_attention",
-    "odb_paged_attention_workspace", "odb_step_paged",
+    "odb_paged_attention_workspace", "odb_step_paged", "odb_qk_norm_rope_quant", "odb_paged_read_quant", "odb_paged_attention_quant",
+    "odb_paged_attention_quant_workspace",
 )
 
 KERNEL_CLASSES = ("gemm_qkv", "attention", "gemm_o", "gemm_gate_up", "gemm_down", "gemm_lm_head", "rmsnorm")
@@ -110,6 +111,24 @@ class odb_paged_rows(ctypes.Structure):
                 ("argmax", ctypes.c_void_p), ("unmask", ctypes.c_void_p), ("n_layers", ctypes.c_int)]
 
 
+class odb_quant_pages(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("n_pages", ctypes.c_int), ("page_size", ctypes.c_int), ("n_kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int),
+                ("codes", ctypes.c_int), ("group", ctypes.c_int), ("dtype", ctypes.c_int), ("page_stride", ctypes.c_longlong),
+                ("head_stride", ctypes.c_longlong), ("pos_stride", ctypes.c_longlong), ("scale_page_stride", ctypes.c_longlong),
+                ("scale_head_stride", ctypes.c_longlong)]
+
+
+class odb_quant_rows(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("in_dtype", ctypes.c_int),
+                ("rows", ctypes.c_int), ("n_heads", ctypes.c_int), ("q_row", ctypes.c_longlong), ("k_row", ctypes.c_longlong),
+                ("v_row", ctypes.c_longlong), ("q_gain", ctypes.c_void_p), ("k_gain", ctypes.c_void_p), ("eps", ctypes.c_float),
+                ("table", ctypes.c_void_p), ("n_pos", ctypes.c_int), ("rot_dim", ctypes.c_int), ("interleaved", ctypes.c_int),
+                ("positions", ctypes.c_void_p), ("q_out", ctypes.c_void_p), ("q_out_row", ctypes.c_longlong), ("cu_rows", ctypes.c_void_p),
+                ("first_pos", ctypes.c_void_p), ("kv_len", ctypes.c_void_p), ("tables", ctypes.c_void_p), ("columns", ctypes.c_int),
+                ("n", ctypes.c_int), ("odd", ctypes.c_void_p)]
+
+
 EVENT_KINDS = ("refresh", "step", "shared")
 
 _lib = None
@@ -163,6 +182,11 @@ def lib() -> ctypes.CDLL:
     L.odb_paged_attention_workspace.argtypes = [vp, vp]
     L.odb_paged_attention_workspace.restype = ctypes.c_longlong
     L.odb_step_paged.argtypes = [vp, vp, vp, vp]
+    L.odb_qk_norm_rope_quant.argtypes = [vp, vp, vp]
+    L.odb_paged_read_quant.argtypes = [vp, vp, ci, ci, vp, vp, ctypes.c_longlong, ctypes.c_longlong, vp]
+    L.odb_paged_attention_quant.argtypes = [vp, vp, vp]
+    L.odb_paged_attention_quant_workspace.argtypes = [vp, vp]
+    L.odb_paged_attention_quant_workspace.restype = ctypes.c_longlong
     L.odb_strerror.argtypes = [ci]
     L.odb_strerror.restype = ctypes.c_char_p
     L.odb_last_error.restype = ctypes.c_char_p
@@ -450,15 +474,17 @@ def odb_cache_read(cache: int, layer: int, kv: int, batch_index: int, pos0: int,
 
 ROPE_SCALINGS = ("plain", "linear", "ntk", "yarn")
 _PACK_PAGES, _PACK_QK_ROWS, _PACK_ATTENTION = (struct.Struct(f).pack for f in ("@PPiiiiiqqq", "@PPPiiiqqqPPfPiiiPPPqP", "@PPqqPPPPiiiifiiiiiPN"))
+_PACK_QUANT_PAGES, _PACK_QUANT_ROWS = (struct.Struct(f).pack for f in ("@PPPPiiiiiiiqqqqq", "@PPPiiiqqqPPfPiiiPPqPPPPiiP"))
 _torch = _raw_stream = None
 
 
 def _load_torch():
-    global _torch, _raw_stream, _DTYPES
+    global _torch, _raw_stream, _DTYPES, _CODES
     import torch
     _torch = torch
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)          # (see _stream)
     _DTYPES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
+    _CODES = {torch.int8: 3, torch.float8_e4m3fn: 4}
     return torch
 
 
@@ -604,8 +630,15 @@ def odb_paged_attention(q, k_pages, v_pages, tables, kv_len, *, causal: bool, cu
     one row per request); first_pos int32 [n] (None: the rows are the last positions); scale defaults to head_dim ** -0.5
     -> [rows, n_heads, head_dim].  max_rows and max_len, bounds of a request's rows and positions, choose the way of computing: give
     max_rows=1 for single tokens.  The workspace comes from torch's allocator unless a uint8 tensor is given."""
-    torch = _torch or _load_torch()
-    index, pages, i32 = q.get_device(), _pages(k_pages, v_pages), torch.int32
+    _torch or _load_torch()
+    pages = _pages(k_pages, v_pages)
+    return _attention(odb_paged_attention_workspace, lib().odb_paged_attention, q, k_pages, pages, k_pages.dtype, tables, kv_len, causal, cu_rows, first_pos,
+                      scale, window, sinks, max_rows, max_len, out, workspace)
+
+
+def _attention(workspace_of, call, q, k_pages, pages, dtype, tables, kv_len, causal, cu_rows, first_pos, scale, window, sinks, max_rows, max_len, out, workspace):
+    torch = _torch
+    index, i32 = q.get_device(), torch.int32
     shape = rows, heads, dim = q.shape
     if k_pages.get_device() != index or dim != k_pages.shape[3]:
         raise TypeError("q and the pools must lie on one device and have heads of the same size")
@@ -614,7 +647,7 @@ def odb_paged_attention(q, k_pages, v_pages, tables, kv_len, *, causal: bool, cu
     n, columns = tables.shape
     if cu_rows is None and rows != n:
         raise ValueError("without cu_rows every request has one row (%d rows, %d requests)" % (rows, n))
-    q_row = _head_rows("q", q, index, k_pages.dtype, shape)
+    q_row = _head_rows("q", q, index, dtype, shape)
     if out is None:
         out, out_row = q.new_empty(shape), heads * dim
     else:
@@ -629,13 +662,118 @@ def odb_paged_attention(q, k_pages, v_pages, tables, kv_len, *, causal: bool, cu
     if rows == 0:
         return out
     a = _PACK_ATTENTION(*fields, 0, 0)
-    need = odb_paged_attention_workspace(a, pages)
+    need = workspace_of(a, pages)
     if need:
         if workspace is None:
             workspace = q.new_empty((need,), dtype=torch.uint8)
         a = _PACK_ATTENTION(*fields, workspace.data_ptr(), workspace.numel())
-    _on(index, lib().odb_paged_attention, a, pages)
+    _on(index, call, a, pages)
     return out
+
+
+def _quant_pages(k_pages, v_pages, k_scale, v_scale, dtype=0):
+    """Pools of codes [n_pages, n_kv_heads, page_size, head_dim], int8 or float8_e4m3fn, and their scales, float32 [n_pages, n_kv_heads,
+    page_size / group], as a packed odb_quant_pages."""
+    shape, strides = k_pages.shape, k_pages.stride()
+    if len(shape) != 4 or v_pages.shape != shape or v_pages.stride() != strides or strides[3] != 1:
+        raise TypeError("k_pages and v_pages must be [n_pages, n_kv_heads, page_size, head_dim] with the same strides, the last one 1")
+    if v_pages.dtype is not k_pages.dtype or v_pages.get_device() != k_pages.get_device() or k_pages.dtype not in _CODES:
+        raise TypeError("k_pages and v_pages must be int8 or float8_e4m3fn, of one dtype and device")
+    s_shape, s_strides = k_scale.shape, k_scale.stride()
+    if len(s_shape) != 3 or s_shape[:2] != shape[:2] or s_shape[2] < 1 or shape[2] % s_shape[2] or v_scale.shape != s_shape or v_scale.stride() != s_strides \
+            or (s_strides[2] != 1 and s_shape[2] != 1):
+        raise TypeError("k_scale and v_scale must be [n_pages, n_kv_heads, page_size / group] with the same strides, the last one 1")
+    if any(t.dtype is not _torch.float32 or t.get_device() != k_pages.get_device() for t in (k_scale, v_scale)):
+        raise TypeError("k_scale and v_scale must be float32, on the device of the codes")
+    return _PACK_QUANT_PAGES(k_pages.data_ptr(), v_pages.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), shape[0], shape[2], shape[1], shape[3],
+                             _CODES[k_pages.dtype], shape[2] // s_shape[2], dtype, strides[0], strides[1], strides[2], s_strides[0], s_strides[1])
+
+
+def odb_qk_norm_rope_quant(q, k, v, k_pages, v_pages, k_scale, v_scale, table, positions, tables, kv_len, *, cu_rows=None, first_pos=None, q_gain=None,
+                           k_gain=None, eps: float = 1e-6, interleaved: bool = False, dtype=None, out=None, odd=None):
+    """odb_qk_norm_rope into pages of 8-bit codes: k_pages, v_pages int8 or float8_e4m3fn [n_pages, n_kv_heads, page_size, head_dim], their
+    scales float32 [n_pages, n_kv_heads, page_size / group].  The requests as in odb_paged_attention: tables int32 [n, columns], kv_len int32 [n]
+    (with the rows), cu_rows int32 [n + 1] (None: one row per request), first_pos int32 [n] (None: the rows are the last positions); positions
+    int32 [rows] are those of the angles -> queries [rows, n_heads, head_dim] of `dtype`, float16 or bfloat16 (that of out, or of q, where none
+    is given).  odd int32 [1] becomes 1 where a value that is not finite was stored."""
+    torch = _torch or _load_torch()
+    index, given, i32, f32 = q.get_device(), q.dtype, torch.int32, torch.float32
+    if dtype is None:
+        dtype = out.dtype if out is not None else given
+    if dtype not in (torch.float16, torch.bfloat16):
+        raise TypeError("queries become float16 or bfloat16: give dtype")
+    pages = _quant_pages(k_pages, v_pages, k_scale, v_scale, _DTYPES[dtype])
+    shape = rows, heads, dim = q.shape
+    kv = (rows, k_pages.shape[1], dim)
+    if k_pages.get_device() != index or dim != k_pages.shape[3] or given not in _DTYPES:
+        raise TypeError("q and the pools must lie on one device and have heads of the same size, q of float16, bfloat16 or float32")
+    if tables.dim() != 2:
+        _not_ints("tables", "[n, columns]")
+    n, columns = tables.shape
+    if cu_rows is None and rows != n:
+        raise ValueError("without cu_rows every request has one row (%d rows, %d requests)" % (rows, n))
+    if out is None:
+        out, out_row = q.new_empty(shape, dtype=dtype), heads * dim
+    else:
+        out_row = _head_rows("out", out, index, dtype, shape)
+    if table.dtype is not f32 or table.dim() != 3 or table.shape[2] != 2 or table.get_device() != index or not table.is_contiguous():
+        raise TypeError("table must be a contiguous float32 tensor [n_pos, rot_dim / 2, 2] on the device of the others")
+    for gain in (q_gain, k_gain):
+        if gain is not None and (gain.dtype is not f32 or gain.shape != (dim,) or gain.get_device() != index or not gain.is_contiguous()):
+            raise TypeError("q_gain and k_gain must be contiguous float32 tensors [head_dim] on the device of the others")
+    r = _PACK_QUANT_ROWS(q.data_ptr(), k.data_ptr(), v.data_ptr(), _DTYPES[given], rows, heads, _head_rows("q", q, index, given, shape),
+                         _head_rows("k", k, index, given, kv), _head_rows("v", v, index, given, kv), 0 if q_gain is None else q_gain.data_ptr(),
+                         0 if k_gain is None else k_gain.data_ptr(), eps, table.data_ptr(), table.shape[0], 2 * table.shape[1], bool(interleaved),
+                         _ints("positions", positions, (rows,), index, i32), out.data_ptr(), out_row,
+                         0 if cu_rows is None else _ints("cu_rows", cu_rows, (n + 1,), index, i32),
+                         0 if first_pos is None else _ints("first_pos", first_pos, (n,), index, i32), _ints("kv_len", kv_len, (n,), index, i32),
+                         _ints("tables", tables, (n, columns), index, i32), columns, n, 0 if odd is None else _ints("odd", odd, (1,), index, i32))
+    if rows:
+        _on(index, lib().odb_qk_norm_rope_quant, r, pages)
+    return out
+
+
+def odb_paged_read_quant(k_pages, v_pages, k_scale, v_scale, slots, dtype=None, out=None):
+    """Values at slots int32 [rows] (outside the pool: zeros) -> (k, v), each [rows, n_kv_heads, head_dim] of dtype float16 (the default),
+    bfloat16 or float32, or `out` = (k, v)."""
+    torch = _torch or _load_torch()
+    pages, index = _quant_pages(k_pages, v_pages, k_scale, v_scale), k_pages.get_device()
+    if out is not None:
+        dtype = out[0].dtype
+    elif dtype is None:
+        dtype = torch.float16
+    if dtype not in _DTYPES:
+        raise TypeError("values are read as float16, bfloat16 or float32")
+    rows, heads, dim = shape = torch.Size((slots.numel(), k_pages.shape[1], k_pages.shape[3]))
+    if out is None:
+        k, v = k_pages.new_empty((2, *shape), dtype=dtype).unbind()
+        k_row = v_row = heads * dim
+    else:
+        k, v = out
+        k_row, v_row = (_head_rows(name, t, index, dtype, shape) for name, t in (("out[0]", k), ("out[1]", v)))
+    p_slots = _ints("slots", slots, (rows,), index, torch.int32)
+    if rows:
+        _on(index, lib().odb_paged_read_quant, pages, p_slots, rows, _DTYPES[dtype], k.data_ptr(), v.data_ptr(), k_row, v_row)
+    return k, v
+
+
+def odb_paged_attention_quant_workspace(attention, pages) -> int:
+    """Of an odb_attention and odb_quant_pages, or their bytes."""
+    n = lib().odb_paged_attention_quant_workspace(*(x if isinstance(x, bytes) else ctypes.byref(x) for x in (attention, pages)))
+    if n < 0:
+        _check(n)
+    return n
+
+
+def odb_paged_attention_quant(q, k_pages, v_pages, k_scale, v_scale, tables, kv_len, *, causal: bool, cu_rows=None, first_pos=None,
+                              scale: Optional[float] = None, window: int = 0, sinks: int = 0, max_rows: int = 0, max_len: int = 0, out=None, workspace=None):
+    """odb_paged_attention over pages of 8-bit codes (see odb_qk_norm_rope_quant); q float16 or bfloat16."""
+    torch = _torch or _load_torch()
+    if q.dtype not in (torch.float16, torch.bfloat16):
+        raise TypeError("q must be float16 or bfloat16")
+    pages = _quant_pages(k_pages, v_pages, k_scale, v_scale, _DTYPES[q.dtype])
+    return _attention(odb_paged_attention_quant_workspace, lib().odb_paged_attention_quant, q, k_pages, pages, q.dtype, tables, kv_len, causal, cu_rows,
+                      first_pos, scale, window, sinks, max_rows, max_len, out, workspace)
 
 
 def odb_step_paged(model: int, tokens, k_pages, v_pages, tables, first_pos, kv_len, positions, slots, table, tau: Optional[float] = None,

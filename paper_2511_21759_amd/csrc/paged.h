@@ -88,5 +88,60 @@ size_t paged_attn_workspace(const odb_pages &p, int rows, int heads, int nt, int
 // Checks a call's sizes and fills the fields that follow from them (paged_api.hip); buffers: the pools' addresses are checked too
 int plan_paged_attention(const odb_attention *a, const odb_pages *pages, bool buffers, PagedAttn &p, int &nt);
 void launch_paged_attention(PagedAttn a, int nt, void *workspace, hipStream_t s);
+// Pieces of it that the attention over 8-bit pages shares: fields that follow from the way and the workspace; the plan of many rows in pieces;
+// the sum of the parts that pieces have left, to rows of pages.dtype.
+void paged_attn_setup(PagedAttn &a, int nt, void *workspace);
+void launch_paged_plan(const PagedAttn &a, hipStream_t s);
+void launch_paged_join(const PagedAttn &a, hipStream_t s);
+
+// ---- pages of 8-bit codes: `pages` of these structures has the codes' addresses and strides (bytes), and the type of queries and results
+
+struct QuantScales {
+    float *k, *v;                       // [page][K/V head][group]
+    long long page_stride, head_stride;
+    int codes, group_shift;             // ODB_INT8 or ODB_E4M3; log2 of the positions that share a scale
+};
+struct PagedAttnQuant : PagedAttn {
+    QuantScales scales;
+};
+void paged_attn_quant_plan(const odb_pages &p, int n, int rows, int group, int max_rows, long long max_len, long long columns, int *nt, int *split,
+                           long long *items);
+int plan_paged_attention_quant(const odb_attention *a, const odb_quant_pages *pages, bool buffers, PagedAttnQuant &p, int &nt);
+void launch_paged_attention_quant(PagedAttnQuant a, int nt, void *workspace, hipStream_t s);
+void launch_paged_attention_int8(const PagedAttnQuant &a, int nt, hipStream_t s);
+void launch_paged_attention_e4m3(const PagedAttnQuant &a, int nt, hipStream_t s);
+
+struct QkNormRopeQuant {
+    const void *q, *k, *v;
+    int in_dtype;
+    long long q_row, k_row, v_row;
+    int rows, heads;
+    const float *q_gain, *k_gain;
+    float eps;
+    const float *table;
+    int n_pos, rot, interleaved;
+    const int32_t *positions;
+    void *q_out;
+    long long q_out_row;
+    const int32_t *cu_rows, *first, *kv_len, *tables;      // as in PagedAttn
+    int rows_per_request, columns, n, page_shift;
+    odb_pages pages;
+    QuantScales scales;
+    unsigned *odd, odd_bit;             // null, or where values that are infinite or no number are reported, by this bit
+    unsigned *status;                   // a model's status word: queries saturate to binary16 and are reported there; null: they become infinite
+};
+void launch_qk_norm_rope_quant(const QkNormRopeQuant &a, hipStream_t s);
+// of its launch (256 threads each): below 2^24
+long long quant_workgroups(int n, int rows, int heads, bool cu_rows, int rows_per_request, const odb_pages &p, const QuantScales &s);
+
+struct PagedReadQuant {
+    odb_pages pages;
+    QuantScales scales;
+    const int32_t *slots;
+    int rows, out_dtype;
+    void *k, *v;
+    long long k_row, v_row;
+};
+void launch_paged_read_quant(const PagedReadQuant &a, hipStream_t s);
 
 }  // namespace odb

@@ -2,6 +2,7 @@
 // turns queries and keys and stores keys and values in their pages.  Attention over the pages is in paged_attn.hip.
 #include "launch.h"
 #include "paged.h"
+#include "paged_rope.h"
 
 namespace odb {
 
@@ -238,24 +239,6 @@ void launch_rope_angles(const RopeTable &a, hipStream_t s) {
 
 // ---- norms and rotation of queries and keys, K/V to their pages ------------------------------------------------------
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-typedef float f32x8 __attribute__((ext_vector_type(8)));
-template <class T> struct Vec;
-template <> struct Vec<_Float16> { typedef f16x8 v8; };
-template <> struct Vec<__bf16> { typedef bf16x8 v8; };
-template <> struct Vec<float> { typedef f32x8 v8; };
-
-template <class T>
-__device__ __forceinline__ f32x8 load8(const T *p) {
-    return __builtin_convertvector(*reinterpret_cast<const typename Vec<T>::v8 *>(p), f32x8);
-}
-// one rounding, to nearest even, of a value computed in 32 bits; beyond the type's range it becomes infinite
-template <class T>
-__device__ __forceinline__ void store8(T *p, f32x8 x) {
-    *reinterpret_cast<typename Vec<T>::v8 *>(p) = __builtin_convertvector(x, typename Vec<T>::v8);
-}
-
 // A head is held by DH / 16 lanes with 16 channels each: in the half layout channel pair (j, j + rot / 2) sits in one lane as
 // elements of its first and its second eight, in the interleaved layout (2j, 2j + 1) inside each eight.  Lanes behind the rotated
 // part hold two neighbouring eights that pass through.  A wave does as many heads of one row as it has groups of lanes, and nothing
@@ -279,21 +262,11 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkNormRope a, int wav
     const bool stored = live && page >= 0 && page < pg.n_pages;
     const size_t at = stored ? (size_t)page * pg.page_stride + (size_t)(slot - page * pg.page_size) * pg.pos_stride : 0;
 
-    const int half = a.rot / 2, turning = a.rot / 16;           // lanes of a head that turn
-    const bool turns = l < turning;
-    int c0, c1;                                                 // first channels of the lane's two eights
-    if (INTER) { c0 = l * 16; c1 = c0 + 8; }
-    else if (turns) { c0 = l * 8; c1 = c0 + half; }
-    else { c0 = a.rot + (l - turning) * 16; c1 = c0 + 8; }
+    const HeadLane hl = head_lane<INTER>(l, a.rot);
+    const int c0 = hl.c0, c1 = hl.c1;
+    const bool turns = hl.turns;
     float cs[8], sn[8];
-    if (turns && live) {
-        const float *t = a.table + (size_t)pos * a.rot + l * 16;       // eight (cos, sin)
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const float4 x = *reinterpret_cast<const float4 *>(t + 4 * i);
-            cs[2 * i] = x.x; sn[2 * i] = x.y; cs[2 * i + 1] = x.z; sn[2 * i + 1] = x.w;
-        }
-    }
+    if (turns && live) load_angles(a.table + (size_t)pos * a.rot + l * 16, cs, sn);
     const int kv = pg.n_kv_heads, total = a.heads + 2 * kv;
     const int h = part * HEADS + slice;
     if (h >= total) return;
@@ -305,36 +278,8 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkNormRope a, int wav
     f32x8 x = load8(src + c0), y = load8(src + c1);
     if (is_q || is_k) {
         const float *gain = is_q ? a.q_gain : a.k_gain;
-        if (gain) {
-            float ss = 0.f;
-#pragma unroll
-            for (int i = 0; i < 8; i++) ss += x[i] * x[i] + y[i] * y[i];
-#pragma unroll
-            for (int o = LANES / 2; o > 0; o >>= 1) ss += __shfl_xor(ss, o);
-            const float r = 1.0f / sqrtf(ss / (float)DH + a.eps);
-            const f32x8 g0 = load8(gain + c0), g1 = load8(gain + c1);
-            x = x * r * g0;
-            y = y * r * g1;
-        }
-        if (turns) {
-            if (INTER) {
-#pragma unroll
-                for (int i = 0; i < 4; i++) {
-                    const float u = x[2 * i], v = x[2 * i + 1], p = y[2 * i], q = y[2 * i + 1];
-                    x[2 * i] = u * cs[i] - v * sn[i];
-                    x[2 * i + 1] = v * cs[i] + u * sn[i];
-                    y[2 * i] = p * cs[4 + i] - q * sn[4 + i];
-                    y[2 * i + 1] = q * cs[4 + i] + p * sn[4 + i];
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; i++) {
-                    const float u = x[i], v = y[i];
-                    x[i] = u * cs[i] - v * sn[i];
-                    y[i] = v * cs[i] + u * sn[i];
-                }
-            }
-        }
+        if (gain) norm_head<DH>(x, y, gain, a.eps, c0, c1);
+        if (turns) turn_head<INTER>(x, y, cs, sn);
     }
     TO *dst;
     if (is_q) {

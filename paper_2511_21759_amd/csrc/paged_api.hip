@@ -36,14 +36,15 @@ int check_columns(const char *who, int columns, int page_size) {
     return ODB_OK;
 }
 
-int check_pages(const char *who, const odb_pages *p, bool buffers = true) {
+// align: of strides, in elements
+int check_pages(const char *who, const odb_pages *p, bool buffers = true, int align = 8) {
     if (!p) return fail(ODB_E_INVALID_ARG, "%s: pages is NULL", who);
     int rc = check_pool(who, p->n_pages, p->page_size);
     if (rc) return rc;
     if (p->dtype != ODB_F16 && p->dtype != ODB_BF16) return fail(ODB_E_INVALID_ARG, "%s: pages of dtype %d", who, p->dtype);
     if (p->head_dim != 64 && p->head_dim != 128 && p->head_dim != 256) return fail(ODB_E_INVALID_ARG, "%s: head_dim=%d (64, 128 or 256)", who, p->head_dim);
     if (p->n_kv_heads < 1 || p->n_kv_heads > 65536) return fail(ODB_E_INVALID_ARG, "%s: n_kv_heads=%d", who, p->n_kv_heads);
-    if (p->page_stride < 0 || p->head_stride < 0 || p->pos_stride < 0 || (p->page_stride | p->head_stride | p->pos_stride) & 7 || p->pos_stride >= 1 << 24)
+    if (p->page_stride < 0 || p->head_stride < 0 || p->pos_stride < 0 || (p->page_stride | p->head_stride | p->pos_stride) & (align - 1) || p->pos_stride >= 1 << 24)
         return fail(ODB_E_INVALID_ARG, "%s: page strides %lld, %lld, %lld", who, p->page_stride, p->head_stride, p->pos_stride);
     if (buffers && (!p->k || !p->v || !aligned16(p->k) || !aligned16(p->v))) return fail(ODB_E_INVALID_ARG, "%s: pools are NULL or not aligned to 16 bytes", who);
     return ODB_OK;
@@ -55,6 +56,23 @@ int check_rows(const char *who, const char *name, const void *p, long long strid
     return ODB_OK;
 }
 
+// Pages of 8-bit codes as the structures of the launchers have them
+int check_quant_pages(const char *who, const odb_quant_pages *p, bool buffers, odb_pages &codes, QuantScales &s) {
+    if (!p) return fail(ODB_E_INVALID_ARG, "%s: pages is NULL", who);
+    codes = odb_pages{p->k, p->v, p->n_pages, p->page_size, p->n_kv_heads, p->head_dim, p->dtype, p->page_stride, p->head_stride, p->pos_stride};
+    int rc = check_pages(who, &codes, buffers, 16);
+    if (rc) return rc;
+    if (p->codes != ODB_INT8 && p->codes != ODB_E4M3) return fail(ODB_E_INVALID_ARG, "%s: codes=%d", who, p->codes);
+    if ((p->group != 1 && p->group != 16 && p->group != 32 && p->group != 64) || p->group > p->page_size)
+        return fail(ODB_E_INVALID_ARG, "%s: groups of %d positions in pages of %d (1, 16, 32 or 64)", who, p->group, p->page_size);
+    if (p->scale_page_stride < 0 || p->scale_head_stride < 0 || (p->group == 1 && (p->scale_page_stride | p->scale_head_stride) & 3))
+        return fail(ODB_E_INVALID_ARG, "%s: scale strides %lld, %lld", who, p->scale_page_stride, p->scale_head_stride);
+    if (buffers && (!p->k_scale || !p->v_scale || !aligned16(p->k_scale) || !aligned16(p->v_scale)))
+        return fail(ODB_E_INVALID_ARG, "%s: scales are NULL or not aligned to 16 bytes", who);
+    s = QuantScales{p->k_scale, p->v_scale, p->scale_page_stride, p->scale_head_stride, p->codes, p->group == 1 ? 0 : p->group == 16 ? 4 : p->group == 32 ? 5 : 6};
+    return ODB_OK;
+}
+
 size_t span(int rows, long long stride, int heads, int dim, int bytes) {
     return rows < 1 ? 0 : ((size_t)(rows - 1) * (size_t)stride + (size_t)heads * dim) * bytes;
 }
@@ -62,21 +80,18 @@ size_t span(int rows, long long stride, int heads, int dim, int bytes) {
 }  // namespace
 
 // checks what does not need buffers, and fills the launch's fields that follow from it
-int odb::plan_paged_attention(const odb_attention *a, const odb_pages *pages, bool buffers, PagedAttn &p, int &nt) {
-    const char *who = "paged_attention";
-    if (!a) return fail(ODB_E_INVALID_ARG, "%s: NULL argument", who);
-    int rc = check_pages(who, pages, buffers);
-    if (rc) return rc;
+// (the pages have been looked at)
+template <class Plan>
+static int plan_attention(const char *who, const odb_attention *a, const odb_pages *pages, Plan plan, PagedAttn &p, int &nt) {
     if (a->n < 1 || a->n > kMaxRequests) return fail(ODB_E_INVALID_ARG, "%s: n=%d outside [1, %d]", who, a->n, kMaxRequests);
     if (a->rows < 0 || a->rows > 1 << 24) return fail(ODB_E_INVALID_ARG, "%s: rows=%d outside [0, 2^24]", who, a->rows);
     if (a->n_heads < 1 || a->n_heads % pages->n_kv_heads) return fail(ODB_E_INVALID_ARG, "%s: %d query heads over %d K/V heads", who, a->n_heads, pages->n_kv_heads);
-    rc = check_columns(who, a->columns, pages->page_size);
+    int rc = check_columns(who, a->columns, pages->page_size);
     if (rc) return rc;
     if (!(a->scale > 0.f) || !isfinite(a->scale * 1.44269504088896340736f)) return fail(ODB_E_INVALID_ARG, "%s: scale=%g", who, (double)a->scale);
     if (a->window < 0 || a->window > 1 << 30 || a->sinks < 0 || a->sinks > 1 << 30) return fail(ODB_E_INVALID_ARG, "%s: window=%d, sinks=%d", who, a->window, a->sinks);
     if (a->max_rows < 0 || a->max_len < 0) return fail(ODB_E_INVALID_ARG, "%s: max_rows=%d, max_len=%d", who, a->max_rows, a->max_len);
     const long long most = (long long)a->columns * pages->page_size;
-    p = PagedAttn{};
     p.columns = a->columns; p.n = a->n; p.rows = a->rows; p.heads = a->n_heads; p.group = a->n_heads / pages->n_kv_heads;
     p.pages = *pages;
     p.page_shift = page_shift(pages->page_size);
@@ -87,11 +102,86 @@ int odb::plan_paged_attention(const odb_attention *a, const odb_pages *pages, bo
         const long long seen = (a->causal ? 1ll : 2ll) * a->window + a->sinks + max_rows;
         max_len = seen < max_len ? seen : max_len;
     }
-    paged_attn_plan(*pages, a->n, a->rows, p.group, max_rows, max_len, a->columns, &nt, &p.split, &p.items);
+    plan(*pages, a->n, a->rows, p.group, max_rows, max_len, a->columns, &nt, &p.split, &p.items);
     if (a->rows == 0) p.split = 0;                                     // nothing is launched, no workspace
     // (a launch has fewer than 2^32 threads, 256 a workgroup; rows of a tile are counted in 32 bits, with room for a tile behind the last)
     if (p.items * pages->n_kv_heads >= 1 << 24 || (long long)a->rows * a->n_heads > 1 << 30)
         return fail(ODB_E_INVALID_ARG, "%s: %d rows of %d heads are too many for one launch", who, a->rows, a->n_heads);
+    return ODB_OK;
+}
+
+int odb::plan_paged_attention(const odb_attention *a, const odb_pages *pages, bool buffers, PagedAttn &p, int &nt) {
+    const char *who = "paged_attention";
+    if (!a) return fail(ODB_E_INVALID_ARG, "%s: NULL argument", who);
+    const int rc = check_pages(who, pages, buffers);
+    if (rc) return rc;
+    p = PagedAttn{};
+    return plan_attention(who, a, pages, paged_attn_plan, p, nt);
+}
+
+int odb::plan_paged_attention_quant(const odb_attention *a, const odb_quant_pages *pages, bool buffers, PagedAttnQuant &p, int &nt) {
+    const char *who = "paged_attention_quant";
+    if (!a) return fail(ODB_E_INVALID_ARG, "%s: NULL argument", who);
+    p = PagedAttnQuant{};
+    odb_pages codes;
+    const int rc = check_quant_pages(who, pages, buffers, codes, p.scales);
+    if (rc) return rc;
+    return plan_attention(who, a, &codes, paged_attn_quant_plan, p, nt);
+}
+
+// what an attention call needs beside its plan: buffers, a workspace; and the launch's fields that come from them
+static int bind_attention(const char *who, const odb_attention *a, PagedAttn &p, int nt) {
+    if (!a->cu_rows && a->rows != a->n) return fail(ODB_E_INVALID_ARG, "%s: without cu_rows every request has one row (%d rows, %d requests)", who, a->rows, a->n);
+    const int dim = p.pages.head_dim;
+    int rc;
+    if ((rc = check_rows(who, "q", a->q, a->q_row, a->n_heads, dim)) || (rc = check_rows(who, "out", a->out, a->out_row, a->n_heads, dim))) return rc;
+    if (!a->kv_len || !a->tables) return fail(ODB_E_INVALID_ARG, "%s: NULL kv_len or tables", who);
+    if (overlap(Range{a->out, span(a->rows, a->out_row, a->n_heads, dim, 2)}, Range{a->q, span(a->rows, a->q_row, a->n_heads, dim, 2)}))
+        return fail(ODB_E_INVALID_ARG, "%s: out overlaps q", who);
+    const size_t need = paged_attn_workspace(p.pages, p.rows, p.heads, nt, p.split);
+    if (need && (!a->workspace || (uintptr_t)a->workspace & 255 || a->workspace_bytes < need))
+        return fail(ODB_E_INVALID_ARG, "%s: a workspace of %zu bytes aligned to 256, given %zu", who, need, a->workspace ? a->workspace_bytes : 0);
+    p.q = a->q; p.out = a->out; p.q_row = a->q_row; p.out_row = a->out_row;
+    p.cu_rows = a->cu_rows; p.first = a->first_pos; p.kv_len = a->kv_len; p.tables = a->tables;
+    p.sc = a->scale * 1.44269504088896340736f;
+    p.causal = a->causal != 0; p.window = a->window; p.sinks = a->sinks;
+    return ODB_OK;
+}
+
+// sizes, gains and rows of a call that norms and turns, and that its queries go where nothing else is read (R: odb_qk_rows or odb_quant_rows)
+template <class R, class TooMany>
+static int check_turned_rows(const char *who, const R &r, const odb_pages &pages, TooMany too_many) {
+    const int dim = pages.head_dim, kv = pages.n_kv_heads;
+    if (r.rows < 0 || r.rows > 1 << 24) return fail(ODB_E_INVALID_ARG, "%s: rows=%d outside [0, 2^24]", who, r.rows);
+    if (r.n_heads < 1 || r.n_heads > 65536) return fail(ODB_E_INVALID_ARG, "%s: n_heads=%d", who, r.n_heads);
+    if (too_many()) return fail(ODB_E_INVALID_ARG, "%s: %d rows of %d heads are too many for one launch", who, r.rows, r.n_heads);
+    if (r.in_dtype != ODB_F32 && r.in_dtype != pages.dtype) return fail(ODB_E_INVALID_ARG, "%s: rows of dtype %d into pages of dtype %d", who, r.in_dtype, pages.dtype);
+    int rc;
+    if (!(rc = check_rows(who, "q", r.q, r.q_row, r.n_heads, dim)) && !(rc = check_rows(who, "k", r.k, r.k_row, kv, dim)) &&
+        !(rc = check_rows(who, "v", r.v, r.v_row, kv, dim)))
+        rc = check_rows(who, "q_out", r.q_out, r.q_out_row, r.n_heads, dim);
+    if (rc) return rc;
+    if (!r.table || !aligned16(r.table) || !r.positions) return fail(ODB_E_INVALID_ARG, "%s: NULL table or positions", who);
+    if ((r.q_gain == nullptr) != (r.k_gain == nullptr) || !aligned16(r.q_gain) || !aligned16(r.k_gain))
+        return fail(ODB_E_INVALID_ARG, "%s: gains are given for q and k together, aligned to 16 bytes", who);
+    if (r.q_gain && (!(r.eps >= 0.f) || !isfinite(r.eps))) return fail(ODB_E_INVALID_ARG, "%s: eps=%g", who, (double)r.eps);
+    if (r.n_pos < 1 || r.n_pos > 1 << 22) return fail(ODB_E_INVALID_ARG, "%s: n_pos=%d outside [1, 2^22]", who, r.n_pos);
+    if (r.rot_dim < 16 || r.rot_dim > dim || r.rot_dim % 16) return fail(ODB_E_INVALID_ARG, "%s: rot_dim=%d is no multiple of 16 in [16, %d]", who, r.rot_dim, dim);
+    const bool in_place = r.q_out == r.q && r.in_dtype == pages.dtype && r.q_out_row == r.q_row;
+    const int eb = r.in_dtype == ODB_F32 ? 4 : 2;
+    const Range out{r.q_out, span(r.rows, r.q_out_row, r.n_heads, dim, 2)};
+    if (!in_place && (overlap(out, Range{r.q, span(r.rows, r.q_row, r.n_heads, dim, eb)}) || overlap(out, Range{r.k, span(r.rows, r.k_row, kv, dim, eb)}) ||
+                      overlap(out, Range{r.v, span(r.rows, r.v_row, kv, dim, eb)})))
+        return fail(ODB_E_INVALID_ARG, "%s: q_out overlaps q, k or v without being q itself", who);
+    // (in place, the rows of k and v may lie between those of q, as in a fused buffer, but a lane must not read what another has written)
+    auto beside = [&](const void *x, long long row) {
+        if (!overlap(out, Range{x, span(r.rows, row, kv, dim, eb)})) return true;
+        if (r.rows > 1 && row != r.q_row) return false;
+        const long long bytes = r.rows > 1 ? row * eb : 1ll << 62, gap = (((intptr_t)x - (intptr_t)r.q) % bytes + bytes) % bytes;
+        return gap >= (long long)r.n_heads * dim * eb && gap + (long long)kv * dim * eb <= bytes;
+    };
+    if (in_place && !(beside(r.k, r.k_row) && beside(r.v, r.v_row)))
+        return fail(ODB_E_INVALID_ARG, "%s: in place, k and v must not share elements with q (rows of one stride, or buffers apart)", who);
     return ODB_OK;
 }
 
@@ -172,39 +262,63 @@ int odb_qk_norm_rope(const odb_qk_rows *rows, const odb_pages *pages, void *stre
     int rc = check_pages(who, pages);
     if (rc) return rc;
     const odb_qk_rows &r = *rows;
-    const int dim = pages->head_dim, kv = pages->n_kv_heads;
-    if (r.rows < 0 || r.rows > 1 << 24) return fail(ODB_E_INVALID_ARG, "%s: rows=%d outside [0, 2^24]", who, r.rows);
-    if (r.n_heads < 1 || r.n_heads > 65536) return fail(ODB_E_INVALID_ARG, "%s: n_heads=%d", who, r.n_heads);
-    if ((long long)r.rows * qk_waves_per_row(r.n_heads, *pages) >= 1 << 26) return fail(ODB_E_INVALID_ARG, "%s: %d rows of %d heads are too many for one launch", who, r.rows, r.n_heads);
-    if (r.in_dtype != ODB_F32 && r.in_dtype != pages->dtype) return fail(ODB_E_INVALID_ARG, "%s: rows of dtype %d into pages of dtype %d", who, r.in_dtype, pages->dtype);
-    if (!(rc = check_rows(who, "q", r.q, r.q_row, r.n_heads, dim)) && !(rc = check_rows(who, "k", r.k, r.k_row, kv, dim)) &&
-        !(rc = check_rows(who, "v", r.v, r.v_row, kv, dim)))
-        rc = check_rows(who, "q_out", r.q_out, r.q_out_row, r.n_heads, dim);
-    if (rc) return rc;
-    if (!r.table || !aligned16(r.table) || !r.positions || !r.slots) return fail(ODB_E_INVALID_ARG, "%s: NULL table, positions or slots", who);
-    if ((r.q_gain == nullptr) != (r.k_gain == nullptr) || !aligned16(r.q_gain) || !aligned16(r.k_gain))
-        return fail(ODB_E_INVALID_ARG, "%s: gains are given for q and k together, aligned to 16 bytes", who);
-    if (r.q_gain && (!(r.eps >= 0.f) || !isfinite(r.eps))) return fail(ODB_E_INVALID_ARG, "%s: eps=%g", who, (double)r.eps);
-    if (r.n_pos < 1 || r.n_pos > 1 << 22) return fail(ODB_E_INVALID_ARG, "%s: n_pos=%d outside [1, 2^22]", who, r.n_pos);
-    if (r.rot_dim < 16 || r.rot_dim > dim || r.rot_dim % 16) return fail(ODB_E_INVALID_ARG, "%s: rot_dim=%d is no multiple of 16 in [16, %d]", who, r.rot_dim, dim);
-    const bool in_place = r.q_out == r.q && r.in_dtype == pages->dtype && r.q_out_row == r.q_row;
-    const int eb = r.in_dtype == ODB_F32 ? 4 : 2;
-    const Range out{r.q_out, span(r.rows, r.q_out_row, r.n_heads, dim, 2)};
-    if (!in_place && (overlap(out, Range{r.q, span(r.rows, r.q_row, r.n_heads, dim, eb)}) || overlap(out, Range{r.k, span(r.rows, r.k_row, kv, dim, eb)}) ||
-                      overlap(out, Range{r.v, span(r.rows, r.v_row, kv, dim, eb)})))
-        return fail(ODB_E_INVALID_ARG, "%s: q_out overlaps q, k or v without being q itself", who);
-    // (in place, the rows of k and v may lie between those of q, as in a fused buffer, but a lane must not read what another has written)
-    auto beside = [&](const void *x, long long row) {
-        if (!overlap(out, Range{x, span(r.rows, row, kv, dim, eb)})) return true;
-        if (r.rows > 1 && row != r.q_row) return false;
-        const long long bytes = r.rows > 1 ? row * eb : 1ll << 62, gap = (((intptr_t)x - (intptr_t)r.q) % bytes + bytes) % bytes;
-        return gap >= (long long)r.n_heads * dim * eb && gap + (long long)kv * dim * eb <= bytes;
-    };
-    if (in_place && !(beside(r.k, r.k_row) && beside(r.v, r.v_row)))
-        return fail(ODB_E_INVALID_ARG, "%s: in place, k and v must not share elements with q (rows of one stride, or buffers apart)", who);
+    if ((rc = check_turned_rows(who, r, *pages, [&] { return (long long)r.rows * qk_waves_per_row(r.n_heads, *pages) >= 1 << 26; }))) return rc;
+    if (!r.slots) return fail(ODB_E_INVALID_ARG, "%s: NULL slots", who);
     if (r.rows == 0) return ODB_OK;
     launch_qk_norm_rope(QkNormRope{r.q, r.k, r.v, r.in_dtype, r.q_row, r.k_row, r.v_row, r.rows, r.n_heads, r.q_gain, r.k_gain, r.eps, r.table, r.n_pos,
                                    r.rot_dim, r.interleaved, r.positions, r.slots, r.q_out, r.q_out_row, *pages, r.row_end, nullptr}, (hipStream_t)stream);
+    HIP_TRY(hipGetLastError());
+    return ODB_OK;
+}
+
+int odb_qk_norm_rope_quant(const odb_quant_rows *rows, const odb_quant_pages *pages, void *stream) {
+    const char *who = "qk_norm_rope_quant";
+    if (!rows) return fail(ODB_E_INVALID_ARG, "%s: NULL argument", who);
+    odb_pages codes;
+    QuantScales scales;
+    int rc = check_quant_pages(who, pages, true, codes, scales);
+    if (rc) return rc;
+    const odb_quant_rows &r = *rows;
+    if (r.n < 1 || r.n > kMaxRequests) return fail(ODB_E_INVALID_ARG, "%s: n=%d outside [1, %d]", who, r.n, kMaxRequests);
+    if ((rc = check_turned_rows(who, r, codes, [&] { return quant_workgroups(r.n, r.rows, r.n_heads, r.cu_rows != nullptr, 1, codes, scales) >= 1 << 24; })) ||
+        (rc = check_columns(who, r.columns, codes.page_size)))
+        return rc;
+    if (!r.cu_rows && r.rows != r.n) return fail(ODB_E_INVALID_ARG, "%s: without cu_rows every request has one row (%d rows, %d requests)", who, r.rows, r.n);
+    if (!r.kv_len || !r.tables) return fail(ODB_E_INVALID_ARG, "%s: NULL kv_len or tables", who);
+    if (r.rows == 0) return ODB_OK;
+    launch_qk_norm_rope_quant(QkNormRopeQuant{r.q, r.k, r.v, r.in_dtype, r.q_row, r.k_row, r.v_row, r.rows, r.n_heads, r.q_gain, r.k_gain, r.eps, r.table, r.n_pos,
+                                              r.rot_dim, r.interleaved, r.positions, r.q_out, r.q_out_row, r.cu_rows, r.first_pos, r.kv_len, r.tables, 1, r.columns,
+                                              r.n, page_shift(codes.page_size), codes, scales, (unsigned *)r.odd, 1u, nullptr}, (hipStream_t)stream);
+    HIP_TRY(hipGetLastError());
+    return ODB_OK;
+}
+
+int odb_paged_read_quant(const odb_quant_pages *pages, const int32_t *slots, int rows, int out_dtype, void *k_out, void *v_out, long long k_row,
+                         long long v_row, void *stream) {
+    const char *who = "paged_read_quant";
+    if (!pages) return fail(ODB_E_INVALID_ARG, "%s: pages is NULL", who);
+    odb_quant_pages any = *pages;
+    any.dtype = ODB_F16;
+    PagedReadQuant p{};
+    int rc = check_quant_pages(who, &any, true, p.pages, p.scales);
+    if (rc) return rc;
+    const int dim = any.head_dim, kv = any.n_kv_heads;
+    if (rows < 0 || rows > 1 << 24) return fail(ODB_E_INVALID_ARG, "%s: rows=%d outside [0, 2^24]", who, rows);
+    if ((long long)rows * kv * dim >= 1ll << 34) return fail(ODB_E_INVALID_ARG, "%s: %d rows of %d heads are too many for one launch", who, rows, kv);
+    if (!slots) return fail(ODB_E_INVALID_ARG, "%s: NULL slots", who);
+    if (out_dtype != ODB_F16 && out_dtype != ODB_BF16 && out_dtype != ODB_F32) return fail(ODB_E_INVALID_ARG, "%s: out_dtype=%d", who, out_dtype);
+    if ((rc = check_rows(who, "k_out", k_out, k_row, kv, dim)) || (rc = check_rows(who, "v_out", v_out, v_row, kv, dim))) return rc;
+    const int eb = out_dtype == ODB_F32 ? 4 : 2;
+    // (the rows of one may lie between those of the other)
+    const Range ko{k_out, span(rows, k_row, kv, dim, eb)}, vo{v_out, span(rows, v_row, kv, dim, eb)};
+    if (overlap(ko, vo)) {
+        const long long bytes = k_row * eb, gap = rows > 1 ? (((intptr_t)v_out - (intptr_t)k_out) % bytes + bytes) % bytes : 0, own = (long long)kv * dim * eb;
+        if (rows == 1 || k_row != v_row || gap < own || gap + own > bytes) return fail(ODB_E_INVALID_ARG, "%s: k_out and v_out overlap", who);
+    }
+    if (rows == 0) return ODB_OK;
+    p.slots = slots; p.rows = rows; p.out_dtype = out_dtype;
+    p.k = k_out; p.v = v_out; p.k_row = k_row; p.v_row = v_row;
+    launch_paged_read_quant(p, (hipStream_t)stream);
     HIP_TRY(hipGetLastError());
     return ODB_OK;
 }
@@ -217,26 +331,30 @@ long long odb_paged_attention_workspace(const odb_attention *a, const odb_pages 
 }
 
 int odb_paged_attention(const odb_attention *a, const odb_pages *pages, void *stream) {
-    const char *who = "paged_attention";
     PagedAttn p;
     int nt;
     int rc = plan_paged_attention(a, pages, true, p, nt);
-    if (rc) return rc;
-    if (!a->cu_rows && a->rows != a->n) return fail(ODB_E_INVALID_ARG, "%s: without cu_rows every request has one row (%d rows, %d requests)", who, a->rows, a->n);
-    const int dim = pages->head_dim;
-    if ((rc = check_rows(who, "q", a->q, a->q_row, a->n_heads, dim)) || (rc = check_rows(who, "out", a->out, a->out_row, a->n_heads, dim))) return rc;
-    if (!a->kv_len || !a->tables) return fail(ODB_E_INVALID_ARG, "%s: NULL kv_len or tables", who);
-    if (overlap(Range{a->out, span(a->rows, a->out_row, a->n_heads, dim, 2)}, Range{a->q, span(a->rows, a->q_row, a->n_heads, dim, 2)}))
-        return fail(ODB_E_INVALID_ARG, "%s: out overlaps q", who);
-    const size_t need = paged_attn_workspace(*pages, p.rows, p.heads, nt, p.split);
-    if (need && (!a->workspace || (uintptr_t)a->workspace & 255 || a->workspace_bytes < need))
-        return fail(ODB_E_INVALID_ARG, "%s: a workspace of %zu bytes aligned to 256, given %zu", who, need, a->workspace ? a->workspace_bytes : 0);
+    if (rc || (rc = bind_attention("paged_attention", a, p, nt))) return rc;
     if (a->rows == 0) return ODB_OK;
-    p.q = a->q; p.out = a->out; p.q_row = a->q_row; p.out_row = a->out_row;
-    p.cu_rows = a->cu_rows; p.first = a->first_pos; p.kv_len = a->kv_len; p.tables = a->tables;
-    p.sc = a->scale * 1.44269504088896340736f;
-    p.causal = a->causal != 0; p.window = a->window; p.sinks = a->sinks;
     launch_paged_attention(p, nt, a->workspace, (hipStream_t)stream);
+    HIP_TRY(hipGetLastError());
+    return ODB_OK;
+}
+
+long long odb_paged_attention_quant_workspace(const odb_attention *a, const odb_quant_pages *pages) {
+    PagedAttnQuant p;
+    int nt;
+    const int rc = plan_paged_attention_quant(a, pages, false, p, nt);
+    return rc ? rc : (long long)paged_attn_workspace(p.pages, p.rows, p.heads, nt, p.split);
+}
+
+int odb_paged_attention_quant(const odb_attention *a, const odb_quant_pages *pages, void *stream) {
+    PagedAttnQuant p;
+    int nt;
+    int rc = plan_paged_attention_quant(a, pages, true, p, nt);
+    if (rc || (rc = bind_attention("paged_attention_quant", a, p, nt))) return rc;
+    if (a->rows == 0) return ODB_OK;
+    launch_paged_attention_quant(p, nt, a->workspace, (hipStream_t)stream);
     HIP_TRY(hipGetLastError());
     return ODB_OK;
 }
