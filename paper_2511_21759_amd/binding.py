@@ -671,22 +671,33 @@ def _attention(workspace_of, call, q, k_pages, pages, dtype, tables, kv_len, cau
     return out
 
 
-def _quant_pages(k_pages, v_pages, k_scale, v_scale, dtype=0):
-    """Pools of codes [n_pages, n_kv_heads, page_size, head_dim], int8 or float8_e4m3fn, and their scales, float32 [n_pages, n_kv_heads,
-    page_size / group], as a packed odb_quant_pages."""
-    shape, strides = k_pages.shape, k_pages.stride()
-    if len(shape) != 4 or v_pages.shape != shape or v_pages.stride() != strides or strides[3] != 1:
+def _refuse_quant_pages(k_pages, v_pages, k_scale, v_scale):
+    """Says what is wrong with pools that _quant_pages does not take."""
+    strides = k_pages.stride()
+    if len(strides) != 4 or v_pages.shape != k_pages.shape or v_pages.stride() != strides or strides[3] != 1:
         raise TypeError("k_pages and v_pages must be [n_pages, n_kv_heads, page_size, head_dim] with the same strides, the last one 1")
     if v_pages.dtype is not k_pages.dtype or v_pages.get_device() != k_pages.get_device() or k_pages.dtype not in _CODES:
         raise TypeError("k_pages and v_pages must be int8 or float8_e4m3fn, of one dtype and device")
-    s_shape, s_strides = k_scale.shape, k_scale.stride()
-    if len(s_shape) != 3 or s_shape[:2] != shape[:2] or s_shape[2] < 1 or shape[2] % s_shape[2] or v_scale.shape != s_shape or v_scale.stride() != s_strides \
-            or (s_strides[2] != 1 and s_shape[2] != 1):
-        raise TypeError("k_scale and v_scale must be [n_pages, n_kv_heads, page_size / group] with the same strides, the last one 1")
     if any(t.dtype is not _torch.float32 or t.get_device() != k_pages.get_device() for t in (k_scale, v_scale)):
         raise TypeError("k_scale and v_scale must be float32, on the device of the codes")
-    return _PACK_QUANT_PAGES(k_pages.data_ptr(), v_pages.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), shape[0], shape[2], shape[1], shape[3],
-                             _CODES[k_pages.dtype], shape[2] // s_shape[2], dtype, strides[0], strides[1], strides[2], s_strides[0], s_strides[1])
+    raise TypeError("k_scale and v_scale must be [n_pages, n_kv_heads, page_size / group] with the same strides, the last one 1")
+
+
+def _quant_pages(k_pages, v_pages, k_scale, v_scale, index, dtype=0):
+    """Pools of codes [n_pages, n_kv_heads, page_size, head_dim], int8 or float8_e4m3fn, and their scales, float32 [n_pages, n_kv_heads,
+    page_size / group], all on device `index`, as a packed odb_quant_pages.  (One expression where all is well: what a call of a few rows
+    takes is mostly this side of it.)"""
+    shape, strides, s_shape, s_strides, codes, f32 = k_pages.shape, k_pages.stride(), k_scale.shape, k_scale.stride(), _CODES.get(k_pages.dtype), _torch.float32
+    if (codes is None or len(shape) != 4 or v_pages.shape != shape or v_pages.stride() != strides or strides[3] != 1 or v_pages.dtype is not k_pages.dtype
+            or len(s_shape) != 3 or v_scale.shape != s_shape or v_scale.stride() != s_strides or k_scale.dtype is not f32 or v_scale.dtype is not f32
+            or s_shape[0] != shape[0] or s_shape[1] != shape[1] or s_shape[2] < 1 or shape[2] % s_shape[2] or (s_strides[2] != 1 and s_shape[2] != 1)
+            or not k_pages.get_device() == v_pages.get_device() == k_scale.get_device() == v_scale.get_device()):
+        _refuse_quant_pages(k_pages, v_pages, k_scale, v_scale)
+    if k_pages.get_device() != index:
+        raise TypeError("the pools and the other tensors must lie on one device")
+    n_pages, heads, page, dim = shape
+    return _PACK_QUANT_PAGES(k_pages.data_ptr(), v_pages.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), n_pages, page, heads, dim, codes,
+                             page // s_shape[2], dtype, strides[0], strides[1], strides[2], s_strides[0], s_strides[1])
 
 
 def odb_qk_norm_rope_quant(q, k, v, k_pages, v_pages, k_scale, v_scale, table, positions, tables, kv_len, *, cu_rows=None, first_pos=None, q_gain=None,
@@ -700,13 +711,13 @@ def odb_qk_norm_rope_quant(q, k, v, k_pages, v_pages, k_scale, v_scale, table, p
     index, given, i32, f32 = q.get_device(), q.dtype, torch.int32, torch.float32
     if dtype is None:
         dtype = out.dtype if out is not None else given
-    if dtype not in (torch.float16, torch.bfloat16):
+    if dtype is not torch.bfloat16 and dtype is not torch.float16:
         raise TypeError("queries become float16 or bfloat16: give dtype")
-    pages = _quant_pages(k_pages, v_pages, k_scale, v_scale, _DTYPES[dtype])
+    pages = _quant_pages(k_pages, v_pages, k_scale, v_scale, index, _DTYPES[dtype])
     shape = rows, heads, dim = q.shape
     kv = (rows, k_pages.shape[1], dim)
-    if k_pages.get_device() != index or dim != k_pages.shape[3] or given not in _DTYPES:
-        raise TypeError("q and the pools must lie on one device and have heads of the same size, q of float16, bfloat16 or float32")
+    if dim != k_pages.shape[3] or given not in _DTYPES:
+        raise TypeError("q and the pools must have heads of the same size, q of float16, bfloat16 or float32")
     if tables.dim() != 2:
         _not_ints("tables", "[n, columns]")
     n, columns = tables.shape
@@ -716,17 +727,19 @@ def odb_qk_norm_rope_quant(q, k, v, k_pages, v_pages, k_scale, v_scale, table, p
         out, out_row = q.new_empty(shape, dtype=dtype), heads * dim
     else:
         out_row = _head_rows("out", out, index, dtype, shape)
-    if table.dtype is not f32 or table.dim() != 3 or table.shape[2] != 2 or table.get_device() != index or not table.is_contiguous():
+    t_shape = table.shape
+    if table.dtype is not f32 or len(t_shape) != 3 or t_shape[2] != 2 or table.get_device() != index or not table.is_contiguous():
         raise TypeError("table must be a contiguous float32 tensor [n_pos, rot_dim / 2, 2] on the device of the others")
     for gain in (q_gain, k_gain):
         if gain is not None and (gain.dtype is not f32 or gain.shape != (dim,) or gain.get_device() != index or not gain.is_contiguous()):
             raise TypeError("q_gain and k_gain must be contiguous float32 tensors [head_dim] on the device of the others")
+    per = (n,)
     r = _PACK_QUANT_ROWS(q.data_ptr(), k.data_ptr(), v.data_ptr(), _DTYPES[given], rows, heads, _head_rows("q", q, index, given, shape),
                          _head_rows("k", k, index, given, kv), _head_rows("v", v, index, given, kv), 0 if q_gain is None else q_gain.data_ptr(),
-                         0 if k_gain is None else k_gain.data_ptr(), eps, table.data_ptr(), table.shape[0], 2 * table.shape[1], bool(interleaved),
+                         0 if k_gain is None else k_gain.data_ptr(), eps, table.data_ptr(), t_shape[0], 2 * t_shape[1], bool(interleaved),
                          _ints("positions", positions, (rows,), index, i32), out.data_ptr(), out_row,
                          0 if cu_rows is None else _ints("cu_rows", cu_rows, (n + 1,), index, i32),
-                         0 if first_pos is None else _ints("first_pos", first_pos, (n,), index, i32), _ints("kv_len", kv_len, (n,), index, i32),
+                         0 if first_pos is None else _ints("first_pos", first_pos, per, index, i32), _ints("kv_len", kv_len, per, index, i32),
                          _ints("tables", tables, (n, columns), index, i32), columns, n, 0 if odd is None else _ints("odd", odd, (1,), index, i32))
     if rows:
         _on(index, lib().odb_qk_norm_rope_quant, r, pages)
@@ -737,20 +750,22 @@ def odb_paged_read_quant(k_pages, v_pages, k_scale, v_scale, slots, dtype=None, 
     """Values at slots int32 [rows] (outside the pool: zeros) -> (k, v), each [rows, n_kv_heads, head_dim] of dtype float16 (the default),
     bfloat16 or float32, or `out` = (k, v)."""
     torch = _torch or _load_torch()
-    pages, index = _quant_pages(k_pages, v_pages, k_scale, v_scale), k_pages.get_device()
+    index = slots.get_device()
+    pages = _quant_pages(k_pages, v_pages, k_scale, v_scale, index)
     if out is not None:
         dtype = out[0].dtype
     elif dtype is None:
         dtype = torch.float16
     if dtype not in _DTYPES:
         raise TypeError("values are read as float16, bfloat16 or float32")
-    rows, heads, dim = shape = torch.Size((slots.numel(), k_pages.shape[1], k_pages.shape[3]))
+    rows, (_, heads, _, dim) = slots.numel(), k_pages.shape
     if out is None:
-        k, v = k_pages.new_empty((2, *shape), dtype=dtype).unbind()
+        shape = (rows, heads, dim)
+        k, v = slots.new_empty(shape, dtype=dtype), slots.new_empty(shape, dtype=dtype)
         k_row = v_row = heads * dim
     else:
         k, v = out
-        k_row, v_row = (_head_rows(name, t, index, dtype, shape) for name, t in (("out[0]", k), ("out[1]", v)))
+        k_row, v_row = (_head_rows(name, t, index, dtype, torch.Size((rows, heads, dim))) for name, t in (("out[0]", k), ("out[1]", v)))
     p_slots = _ints("slots", slots, (rows,), index, torch.int32)
     if rows:
         _on(index, lib().odb_paged_read_quant, pages, p_slots, rows, _DTYPES[dtype], k.data_ptr(), v.data_ptr(), k_row, v_row)
@@ -769,9 +784,9 @@ def odb_paged_attention_quant(q, k_pages, v_pages, k_scale, v_scale, tables, kv_
                               scale: Optional[float] = None, window: int = 0, sinks: int = 0, max_rows: int = 0, max_len: int = 0, out=None, workspace=None):
     """odb_paged_attention over pages of 8-bit codes (see odb_qk_norm_rope_quant); q float16 or bfloat16."""
     torch = _torch or _load_torch()
-    if q.dtype not in (torch.float16, torch.bfloat16):
+    if q.dtype is not torch.bfloat16 and q.dtype is not torch.float16:
         raise TypeError("q must be float16 or bfloat16")
-    pages = _quant_pages(k_pages, v_pages, k_scale, v_scale, _DTYPES[q.dtype])
+    pages = _quant_pages(k_pages, v_pages, k_scale, v_scale, q.get_device(), _DTYPES[q.dtype])
     return _attention(odb_paged_attention_quant_workspace, lib().odb_paged_attention_quant, q, k_pages, pages, q.dtype, tables, kv_len, causal, cu_rows,
                       first_pos, scale, window, sinks, max_rows, max_len, out, workspace)
 

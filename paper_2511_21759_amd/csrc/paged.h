@@ -103,9 +103,10 @@ struct QuantScales {
 };
 struct PagedAttnQuant : PagedAttn {
     QuantScales scales;
+    int slots;                          // kManyRows: workgroups per K/V head that run at once; the tiles of a round that is not full are cut.  0: they are not
 };
 void paged_attn_quant_plan(const odb_pages &p, int n, int rows, int group, int max_rows, long long max_len, long long columns, int *nt, int *split,
-                           long long *items);
+                           long long *items, int *slots);
 int plan_paged_attention_quant(const odb_attention *a, const odb_quant_pages *pages, bool buffers, PagedAttnQuant &p, int &nt);
 void launch_paged_attention_quant(PagedAttnQuant a, int nt, void *workspace, hipStream_t s);
 void launch_paged_attention_int8(const PagedAttnQuant &a, int nt, hipStream_t s);

@@ -126,7 +126,8 @@ int odb::plan_paged_attention_quant(const odb_attention *a, const odb_quant_page
     odb_pages codes;
     const int rc = check_quant_pages(who, pages, buffers, codes, p.scales);
     if (rc) return rc;
-    return plan_attention(who, a, &codes, paged_attn_quant_plan, p, nt);
+    return plan_attention(who, a, &codes, [&](const odb_pages &q, int n, int rows, int group, int max_rows, long long max_len, long long columns, int *t, int *split,
+                                              long long *items) { paged_attn_quant_plan(q, n, rows, group, max_rows, max_len, columns, t, split, items, &p.slots); }, p, nt);
 }
 
 // what an attention call needs beside its plan: buffers, a workspace; and the launch's fields that come from them

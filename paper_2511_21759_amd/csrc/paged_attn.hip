@@ -786,9 +786,39 @@ void paged_attn_plan(const odb_pages &p, int n, int rows, int group, int max_row
     *items = *split ? *split : numbers(tile_rows);
 }
 
+// Half the bytes a key, and whole tiles of up to 64 requests are given out longest first.  nt and the shape of many rows in few tiles as above; else:
+// Many rows with a tile for every CU: whole, however ragged (whole, longest first / pieces / whole in order of the requests: four pieces of
+// prompts, 727 to 1449 rows of 2694 to 5995 positions, 304 / 321 / 392 us).  Where a last round of workgroups would hold a few tiles only,
+// these are cut, which costs a join (three of 503 to 997 rows under a window of 900, 526 tiles and 512 workgroups at once: 83 / 107 us
+// uncut; four pieces, two full rounds: 319 / 304).
+// Few rows: cuts for two workgroups a CU with 32 rows too (8 x 32 rows of 500 to 3000, 32 heads over 32: 45 us, one 53); whole where
+// the keys are up to 1536 and the pairs enough (10 x 32 rows of 454 to 1364: 24 / 31 us in pieces).
 void paged_attn_quant_plan(const odb_pages &p, int n, int rows, int group, int max_rows, long long max_len, long long columns, int *nt, int *split,
-                           long long *items) {
+                           long long *items, int *slots) {
     paged_attn_plan(p, n, rows, group, max_rows, max_len, columns, nt, split, items);
+    *slots = 0;
+    const int tile_rows = *nt == kManyRows ? many_rows(p) : 16 * *nt;
+    const long long most = (long long)max_rows * group, full = (long long)rows * group / tile_rows, numbers = (n + full) | 1;
+    const long long tiles = min((n < rows ? n : rows) + full, (long long)n * ((most + tile_rows - 1) / tile_rows)), pairs = tiles * p.n_kv_heads;
+    if (*nt == kManyRows) {
+        if (pairs < 256) return;
+        *split = 0;
+        *items = numbers;
+        const int at_once = (512 + p.n_kv_heads - 1) / p.n_kv_heads;
+        const long long over = tiles % at_once;
+        if (n <= 64 && full >= at_once && full / at_once == tiles / at_once && 2 * over <= at_once && tiles <= 4ll * at_once) {
+            *slots = *split = at_once;
+            *items = (n < rows ? n : rows) + full + at_once;                   // (of all tiles that there can be: max_rows may not hold)
+        }
+        return;
+    }
+    if (!*split) return;
+    if (*nt > 1 && n <= 64 && pairs >= 160 && pairs <= 512 && (max_len + 31) / 32 * p.head_dim <= 48 * 128) {
+        *split = 0;
+        *items = numbers;
+    } else if (*nt == 2 && p.head_dim != 256) {
+        *split = *items = (512 + p.n_kv_heads - 1) / p.n_kv_heads;
+    }
 }
 
 size_t paged_attn_workspace(const odb_pages &p, int rows, int heads, int nt, int split) {

@@ -129,12 +129,14 @@ constexpr int kPairCost = 6;
 
 // The requests' weights - row tiles, times blocks where keys are split - lie behind each other; finds the request that holds
 // item pick(total) and the item's offset inside it.  False if there is none.  Up to 64 requests every wave does it alone.
-template <int SHIFT = 5, int COST = kPairCost, class Pick>
+// LONGEST: of up to 64 requests that are given out by whole tiles, those with the most positions lie first.
+template <int SHIFT = 5, int COST = kPairCost, bool LONGEST = false, class Pick>
 __device__ __forceinline__ bool find_place(const PagedAttn &a, int tile_rows, bool need_total, Pick pick, Place &p) {
     const int lane = threadIdx.x & 63;
+    const bool by_blocks = a.split && COST >= 0;
     auto weigh = [&](const Request &q) -> long long {
         const int tiles = tiles_of(a, q, tile_rows);
-        return a.split && tiles ? (long long)tiles * (request_blocks<SHIFT>(a, q) + COST) : tiles;
+        return by_blocks && tiles ? (long long)tiles * (request_blocks<SHIFT>(a, q) + COST) : tiles;
     };
     auto scan64 = [&](long long v) -> long long {
 #pragma unroll
@@ -147,13 +149,26 @@ __device__ __forceinline__ bool find_place(const PagedAttn &a, int tile_rows, bo
     if (a.n <= 64) {
         Request q{0, 0, 0, 0};
         if (lane < a.n) q = request_of(a, lane);
-        const long long v = weigh(q), end = scan64(v);
+        long long v = weigh(q);
+        int who = lane;
+        if (LONGEST && !by_blocks && a.n > 1) {
+            // a lane's place in the order, and back: which request is at a lane's place
+            int before = 0;
+            for (int j = 0; j < a.n; j++) {
+                const int other = __builtin_amdgcn_readlane(q.len, j);
+                before += (int)(other > q.len) | ((int)(other == q.len) & (int)(j < lane));
+            }
+            who = __builtin_amdgcn_ds_permute(4 * (lane < a.n ? before : lane), lane);
+            v = __shfl((int)v, who);                                 // (tiles of one request: fewer than 2^30)
+        }
+        const long long end = scan64(v);
         p.total = uniform(__shfl(end, 63));
         const long long x = pick(p.total);
         const unsigned long long behind = __ballot(end > x);
         if (x >= p.total) return false;
-        p.r = __builtin_amdgcn_readfirstlane(__ffsll(behind) - 1);
-        p.at = x - uniform(__shfl(end - v, p.r));
+        const int at = __builtin_amdgcn_readfirstlane(__ffsll(behind) - 1);
+        p.at = x - uniform(__shfl(end - v, at));
+        p.r = __builtin_amdgcn_readlane(who, at);
         p.q.m = __builtin_amdgcn_readlane(q.m, p.r);
         p.q.len = __builtin_amdgcn_readlane(q.len, p.r);
         p.q.first = __builtin_amdgcn_readlane(q.first, p.r);
@@ -318,12 +333,16 @@ __device__ __forceinline__ void clear_odd(frag_t &v) {
 
 // Where the 16-byte piece `c` of key row `key` lies in a block of V: pieces are exchanged inside 256 bytes so that the
 // 8-byte reads of eight neighbouring keys, 32 bytes of each, fall on all 64 banks.
+// PAIRS: written by lanes that hold two pieces beside each other each, every second piece at once: those of the upper half of 256 bytes, or of
+// every second key of 128, are the other way round (eight lanes then write to all banks; a store of 1 KiB takes 13 clocks and not 16).
 template <int DH>
+__host__ __device__ constexpr int pair_turn(int key, int c) { return DH == 64 ? key & 1 : DH == 128 ? (c >> 3) & 1 : ((c >> 3) ^ (c >> 4)) & 1; }
+template <int DH, bool PAIRS = false>
 __host__ __device__ constexpr int v_piece(int key, int c) {
-    return key * (DH / 8) + (DH == 64 ? c ^ (((key >> 1) & 3) << 1) : c ^ ((key & 7) << 1));
+    return key * (DH / 8) + (c ^ (DH == 64 ? ((key >> 1) & 3) << 1 : (key & 7) << 1) ^ (PAIRS ? pair_turn<DH>(key, c) : 0));
 }
 
-template <class T, int DH, class See>
+template <class T, int DH, bool PAIRS = false, class See>
 __device__ __forceinline__ void add_odd(const unsigned char *v_block, int lane, const frag_t &pf, See see, f32x4 (&o)[DH / 16]) {
     int dl = lane;                            // (hidden from the compiler, which else keeps this part's addresses in registers)
     asm volatile("" : "+v"(dl));
@@ -339,7 +358,7 @@ __device__ __forceinline__ void add_odd(const unsigned char *v_block, int lane, 
 #pragma unroll
             for (int d = 0; d < 4; d++) {
                 const int ch = c * 16 + 4 * (dl >> 4) + d;
-                const uint32_t v = *reinterpret_cast<const u16 *>(v_block + 16 * v_piece<DH>(key, ch >> 3) + 2 * (ch & 7));
+                const uint32_t v = *reinterpret_cast<const u16 *>(v_block + 16 * v_piece<DH, PAIRS>(key, ch >> 3) + 2 * (ch & 7));
                 if ((int)seen & (int)((v & Num<T>::kExp) == Num<T>::kExp)) o[c][d] += p * Num<T>::value(v);
             }
     }
@@ -353,10 +372,10 @@ __device__ __forceinline__ frag_t v_operand_at(const unsigned char *p0, int keys
     const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p0 + keys16)));
     return frag_t{{lo.x, lo.y, hi.x, hi.y}};
 }
-template <int DH>
+template <int DH, bool PAIRS = false>
 __device__ __forceinline__ unsigned v_lane(int lane, int c) {             // bytes
     const int li = lane & 15, row = 4 * (lane >> 4) + (li >> 2), at = 2 * c + ((li >> 1) & 1);
-    return 16 * v_piece<DH>(row, at) + 8 * (li & 1);
+    return 16 * v_piece<DH, PAIRS>(row, at) + 8 * (li & 1);
 }
 template <int DH>
 __device__ __forceinline__ frag_t v_operand(const unsigned char *v_block, int lane, int c) {
@@ -433,9 +452,9 @@ struct RowsShape {
     static constexpr int NT = DH == 256 ? 1 : 2, TILE_ROWS = 64 * NT, SHIFT = DH == 256 ? 5 : 6, SK = 1 << SHIFT;
 };
 // Where piece c of a key of K lies: the 16 keys that one operand load reads fall on different banks.
-template <int DH>
+template <int DH, bool PAIRS = false>
 __host__ __device__ constexpr int k_piece(int key, int c) {
-    return key * (DH / 8) + (DH == 64 ? c ^ ((key >> 1) & 7) : c ^ (key & 15));
+    return key * (DH / 8) + (c ^ (DH == 64 ? (key >> 1) & 7 : key & 15) ^ (PAIRS ? pair_turn<DH>(key, c) : 0));
 }
 
 }  // namespace

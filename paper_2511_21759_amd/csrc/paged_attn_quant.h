@@ -10,6 +10,7 @@
 //         taken relative to a power of two beyond the largest that the row has seen (RowState), and O with them.
 //   Sums of probabilities are those of p alone, rounded to binary16 like the operands.
 #pragma once
+
 #include "paged_attn_core.h"
 
 namespace odb {
@@ -81,29 +82,35 @@ __device__ __forceinline__ void load_queries(const PagedAttn &a, const u16 *src,
 // units of log2 here), and that of V's scales: a power of two, `unit`, that none of those a row has seen exceeds.  O is in multiples of it.
 struct RowState { float at = kNone, limit = kNone, unit = 0.f, inverse = 1.f; };
 
-// What scores z of a lane's keys are multiplied by where some may be hidden, so that the product of a hidden one stays minus infinity: c is
-// nought or no number only for those that the row sees.
-__device__ __forceinline__ float seen_factor(const f32x4 &z, float c) {
-    const bool any = !(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])) == -INFINITY);
-    return any ? __builtin_elementwise_maximum(c, 0x1p-126f) : 1.0f;
+// Scores z of keys that a row may not see are minus infinity.  What these are multiplied by, and V's scales, must not make more of them: where the
+// lane's keys share a scale (EVEN) it is left out if the row sees none of them, else key by key.  A factor of nought becomes one beside it.
+template <bool EVEN>
+__device__ __forceinline__ void hide_scales(const f32x4 (&z)[2], float (&c)[2], f32x4 (&v)[2]) {
+#pragma unroll
+    for (int s = 0; s < 2; s++) {
+        if (EVEN) {
+            const bool any = !(fmaxf(fmaxf(z[s][0], z[s][1]), fmaxf(z[s][2], z[s][3])) == -INFINITY);
+            c[s] = any ? __builtin_elementwise_maximum(c[s], 0x1p-126f) : 1.0f;
+            v[s][0] = any ? v[s][0] : 0.f;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; e++) v[s][e] = z[s][e] > -INFINITY ? v[s][e] : 0.f;
+        }
+    }
 }
 
 // Probabilities of 32 keys of a row tile from their scores z (keys that are not seen: -infinity): p as the operand that is summed, p times V's
 // relative scales as that of the product.  c: what a score of the first and the second 16 keys is multiplied by; v: the keys' scales, of
 // which with EVEN only the first of each 16 counts.  References are raised, and sums and O rescaled, as in probabilities().
-template <int CT, bool EVEN, bool MASKED>
-__device__ __forceinline__ void quant_probabilities(const f32x4 (&z)[2], float c0, float c1, const f32x4 (&scale)[2], RowState &st, f32x4 &lsum, f32x4 (&o)[CT],
+template <int CT, bool EVEN>
+__device__ __forceinline__ void quant_probabilities(const f32x4 (&z)[2], const float (&f2)[2], const f32x4 (&v)[2], RowState &st, f32x4 &lsum, f32x4 (&o)[CT],
                                                     frag_t &pf, frag_t &pv) {
-    f32x4 v[2];
-    float top = fmaxf(fmaxf(fmaxf(z[0][0], z[0][1]), fmaxf(z[0][2], z[0][3])) * c0, fmaxf(fmaxf(z[1][0], z[1][1]), fmaxf(z[1][2], z[1][3])) * c1), top_v = 0.f;
+    const float c0 = f2[0], c1 = f2[1];
+    float top = fmaxf(fmaxf(fmaxf(z[0][0], z[0][1]), fmaxf(z[0][2], z[0][3])) * c0, fmaxf(fmaxf(z[1][0], z[1][1]), fmaxf(z[1][2], z[1][3])) * c1);
+    float top_v = fmaxf(v[0][0], v[1][0]);
+    if (!EVEN)
 #pragma unroll
-    for (int s = 0; s < 2; s++)
-#pragma unroll
-        for (int e = 0; e < 4; e++) {
-            v[s][e] = EVEN ? scale[s][0] : scale[s][e];
-            if (MASKED) v[s][e] = z[s][e] > -INFINITY ? v[s][e] : 0.f;         // (a scale that the row does not see may be anything)
-            if (!EVEN || MASKED || e == 0) top_v = fmaxf(top_v, v[s][e]);
-        }
+        for (int e = 1; e < 4; e++) top_v = fmaxf(top_v, fmaxf(v[0][e], v[1][e]));
     if (__any((int)(top > st.limit) | (int)(top_v > st.unit))) {
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
@@ -136,7 +143,7 @@ __device__ __forceinline__ void quant_probabilities(const f32x4 (&z)[2], float c
 #pragma unroll
         for (int e = 0; e < 4; e++) {
             p[s][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[s][e], s ? c1 : c0, -st.at));
-            w[s][e] = p[s][e] * (v[s][e] * st.inverse);
+            w[s][e] = p[s][e] * (v[s][EVEN ? 0 : e] * st.inverse);
         }
     pf = frag_t{{Num<_Float16>::pack(p[0][0], p[0][1]), Num<_Float16>::pack(p[0][2], p[0][3]), Num<_Float16>::pack(p[1][0], p[1][1]), Num<_Float16>::pack(p[1][2], p[1][3])}};
     pv = frag_t{{Num<_Float16>::pack(w[0][0], w[0][1]), Num<_Float16>::pack(w[0][2], w[0][3]), Num<_Float16>::pack(w[1][0], w[1][1]), Num<_Float16>::pack(w[1][2], w[1][3])}};
@@ -166,7 +173,7 @@ __device__ __forceinline__ void store_rounded8(const PagedAttn &a, int row, int 
 // then scalars of the wave; else every key has its own.
 template <int DH>
 struct QuantShape {
-    static constexpr int SUB = 1, KB = 32 * SUB, SHIFT = SUB == 1 ? 5 : 6, COST = kPairCost / SUB;
+    static constexpr int SUB = 1, KB = 32 * SUB, SHIFT = SUB == 1 ? 5 : 6, COST = 12;
 };
 constexpr int kLeastQuantPiece = 12;             // places, of 32 keys
 
@@ -194,7 +201,7 @@ __global__ __launch_bounds__(64 * NW, DH == 256 || NT == 4 ? 1 : 2) void quant_a
     const bool split = a.split > 0;
     auto piece_of = [&](long long total) { return max((long long)(kLeastQuantPiece / SUB), (total + a.split - 1) / max(a.split, 1)); };
     Place pl;
-    if (!find_place<SHIFT, Shape::COST>(a, TILE_ROWS, split, [&](long long total) { return split ? piece_of(total) * x : (long long)x; }, pl)) return;
+    if (!find_place<SHIFT, Shape::COST, true>(a, TILE_ROWS, split, [&](long long total) { return split ? piece_of(total) * x : (long long)x; }, pl)) return;
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, li = lane & 15;
     const int G = a.group;
@@ -316,48 +323,27 @@ __global__ __launch_bounds__(64 * NW, DH == 256 || NT == 4 ? 1 : 2) void quant_a
                             nvs[t] = ld_scalar_float(vsp, sbase[t]);
                         }
                     }
-                    // scores: of all keys at once for one row tile, which frees the registers of K
-                    f32x4 z[NT == 1 ? SUB : 1][2];
-                    frag_t kf[2][KS];
-                    auto convert_k = [&](int sub) {
+                    // scores of all keys and row tiles first, which frees the registers of K for the next block
+                    f32x4 z[SUB][NT][2];
 #pragma unroll
-                        for (int s = 0; s < 2; s++)
+                    for (int tile = 0; tile < T; tile++) {
+                        frag_t kf[KS];
 #pragma unroll
-                            for (int c = 0; c < CH; c++) {
-                                const frag_t &r = kr[2 * sub + s][c];
-                                kf[s][2 * c] = halves8<CODES>(r.w[0], r.w[1]);
-                                kf[s][2 * c + 1] = halves8<CODES>(r.w[2], r.w[3]);
-                            }
-                    };
-                    auto scores = [&](int t, f32x4 (&out)[2]) {
-#pragma unroll
-                        for (int s = 0; s < 2; s++) {
-                            out[s] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                            for (int k = 0; k < KS; k++) out[s] = mfma16(kf[s][k], q[t][k], out[s]);
+                        for (int c = 0; c < CH; c++) {
+                            kf[2 * c] = halves8<CODES>(kr[tile][c].w[0], kr[tile][c].w[1]);
+                            kf[2 * c + 1] = halves8<CODES>(kr[tile][c].w[2], kr[tile][c].w[3]);
                         }
-                    };
-                    if (NT == 1) {
 #pragma unroll
-                        for (int sub = 0; sub < SUB; sub++) {
+                        for (int t = 0; t < NT; t++) {
+                            f32x4 y = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                            for (int s = 0; s < 2; s++) {
-                                f32x4 y = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                                for (int c = 0; c < CH; c++) {
-                                    const frag_t &r = kr[2 * sub + s][c];
-                                    y = mfma16(halves8<CODES>(r.w[0], r.w[1]), q[0][2 * c], y);
-                                    y = mfma16(halves8<CODES>(r.w[2], r.w[3]), q[0][2 * c + 1], y);
-                                }
-                                z[sub][s] = y;
-                            }
-                            if (!EVEN)
-#pragma unroll
-                                for (int s = 0; s < 2; s++) z[sub][s] *= ks[2 * sub + s];
+                            for (int k = 0; k < KS; k++) y = mfma16(kf[k], q[t][k], y);
+                            if (!EVEN) y *= ks[tile];
+                            z[tile >> 1][t][tile & 1] = y;
                         }
-                        load_k(base, k_next);
-                        if (!EVEN) load_scales(ksp, sbase, ks, more);
                     }
+                    load_k(base, k_next);
+                    if (!EVEN) load_scales(ksp, sbase, ks, more);
                     bool dirty = false;
                     if (Code<CODES>::kOdd && !plain) {
                         int odd = 0;
@@ -380,14 +366,42 @@ __global__ __launch_bounds__(64 * NW, DH == 256 || NT == 4 ? 1 : 2) void quant_a
                         }
                     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
                     load_v(base, v_next);
+                    if (Code<CODES>::kOdd && __builtin_expect(dirty, 0)) {
+                        // a code that is no number makes the rows that see it no numbers, and has a zero in its place for the others
+                        int dl = lane;
+                        asm volatile("" : "+v"(dl));
+                        for (int key = 0; key < KB; key++) {
+                            int page = pg[0];
+#pragma unroll
+                            for (int t = 1; t < T; t++) page = key >> 4 == t ? pg[t] : page;
+#pragma unroll
+                            for (int t = 0; t < NT; t++) {
+                                const bool seen = sees(sight[t], key0 + key, page);
+#pragma unroll
+                                for (int c = 0; c < CT; c++)
+#pragma unroll
+                                    for (int d = 0; d < 4; d++) {
+                                        const unsigned char w = mine[(key >> 5) * 32 * DH + 16 * vq_piece<DH>(key & 31, c) + 4 * (dl >> 4) + d];
+                                        if ((int)seen & (int)((w & 0x7f) == 0x7f)) o[t][c][d] = __builtin_nanf("");
+                                    }
+                            }
+                        }
+                        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                        for (int j = 0; j < KB * DH / 1024; j++) {
+                            frag_t *at = reinterpret_cast<frag_t *>(mine + 16 * (dl + 64 * j)), v = *at;
+#pragma unroll
+                            for (int w = 0; w < 4; w++) {
+                                const uint32_t odd = ((v.w[w] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;      // the highest bit of such codes
+                                v.w[w] &= ~((odd >> 7) * 0xffu);
+                            }
+                            *at = v;
+                        }
+                        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                    }
 
 #pragma unroll
                     for (int sub = 0; sub < SUB; sub++) {
                         const int key32 = key0 + 32 * sub;
-                        if (NT > 1) {
-                            convert_k(sub);
-                            if (sub + 1 == SUB) load_k(base, k_next);
-                        }
                         f32x4 v[2];
 #pragma unroll
                         for (int s = 0; s < 2; s++) v[s] = EVEN ? f32x4{cvs[2 * sub + s], 0.f, 0.f, 0.f} : vs[2 * sub + s];
@@ -396,9 +410,7 @@ __global__ __launch_bounds__(64 * NW, DH == 256 || NT == 4 ? 1 : 2) void quant_a
                             typedef __attribute__((address_space(3))) i32x2 *lds_ptr;
                             const int r = li >> 1, key = (r & 3) + 4 * g + 4 * (r & 4);
                             const i32x2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_ptr)(mine + sub * 32 * DH + 16 * vq_piece<DH>(key, c) + 8 * (li & 1)));
-                            frag_t f = halves8<CODES>((uint32_t)w[0], (uint32_t)w[1]);
-                            if (Code<CODES>::kOdd && __builtin_expect(dirty, 0)) clear_odd<_Float16>(f);
-                            return f;
+                            return halves8<CODES>((uint32_t)w[0], (uint32_t)w[1]);
                         };
                         frag_t vt[NT > 1 ? CT : 1];                           // held for several row tiles
                         if (NT > 1)
@@ -406,44 +418,21 @@ __global__ __launch_bounds__(64 * NW, DH == 256 || NT == 4 ? 1 : 2) void quant_a
                             for (int c = 0; c < CT; c++) vt[NT > 1 ? c : 0] = v_codes(c);
 #pragma unroll
                         for (int t = 0; t < NT; t++) {
-                            f32x4 zt[2];
-                            if (NT == 1) { zt[0] = z[NT == 1 ? sub : 0][0]; zt[1] = z[NT == 1 ? sub : 0][1]; }
-                            else {
-                                scores(t, zt);
-                                if (!EVEN)
-#pragma unroll
-                                    for (int s = 0; s < 2; s++) zt[s] *= ks[2 * sub + s];
-                            }
+                            f32x4 (&zt)[2] = z[sub][t];
                             frag_t pf, pv;
-                            if (plain) {
-                                quant_probabilities<CT, EVEN, false>(zt, EVEN ? sc[t] * cks[2 * sub] : sc[t], EVEN ? sc[t] * cks[2 * sub + 1] : sc[t], v, st[t], lsum[t], o[t], pf, pv);
-                            } else {
+                            float c[2] = {EVEN ? sc[t] * cks[2 * sub] : sc[t], EVEN ? sc[t] * cks[2 * sub + 1] : sc[t]};
+                            f32x4 vt2[2] = {v[0], v[1]};
+                            if (!plain) {
                                 hide_unseen(zt, sight[t], key32, g, pg[2 * sub], pg[2 * sub + 1]);
-                                const float c0 = EVEN ? seen_factor(zt[0], sc[t] * cks[2 * sub]) : sc[t], c1 = EVEN ? seen_factor(zt[1], sc[t] * cks[2 * sub + 1]) : sc[t];
-                                quant_probabilities<CT, EVEN, true>(zt, c0, c1, v, st[t], lsum[t], o[t], pf, pv);
+                                hide_scales<EVEN>(zt, c, vt2);
                             }
-                            if (Code<CODES>::kOdd && __builtin_expect(dirty, 0)) {
-                                // a code that is no number makes the rows that see it no numbers, and has a zero in its place for the others
-                                for (int key = 0; key < 32; key++) {
-                                    const bool seen = sees(sight[t], key32 + key, key & 16 ? pg[2 * sub + 1] : pg[2 * sub]);
-#pragma unroll
-                                    for (int c = 0; c < CT; c++)
-#pragma unroll
-                                        for (int d = 0; d < 4; d++) {
-                                            const unsigned char w = mine[sub * 32 * DH + 16 * vq_piece<DH>(key, c) + 4 * g + d];
-                                            if ((int)seen & (int)((w & 0x7f) == 0x7f)) o[t][c][d] = __builtin_nanf("");
-                                        }
-                                }
-                            }
+                            quant_probabilities<CT, EVEN>(zt, c, vt2, st[t], lsum[t], o[t], pf, pv);
                             lsum[t] = mfma16(ones, pf, lsum[t]);
 #pragma unroll
                             for (int c = 0; c < CT; c++) o[t][c] = mfma16(NT > 1 ? vt[NT > 1 ? c : 0] : v_codes(c), pv, o[t][c]);
                         }
                     }
-                    if (!EVEN) {
-                        if (NT > 1) load_scales(ksp, sbase, ks, more);
-                        load_scales(vsp, sbase, vs, more);
-                    }
+                    if (!EVEN) load_scales(vsp, sbase, vs, more);
                     key0 = nkey;
 #pragma unroll
                     for (int t = 0; t < T; t++) pg[t] = npg[t];
@@ -529,6 +518,8 @@ __global__ __launch_bounds__(64 * NW, DH == 256 || NT == 4 ? 1 : 2) void quant_a
 
 // ---- many rows: the waves of a workgroup split the rows and share K and V in LDS ----------------------------------------
 
+constexpr int kMostShares = 16;
+
 // As paged_rows_kernel; codes become binary16 on their way to LDS, once for the four waves, and the keys' scales lie beside them.
 template <int CODES, int DH, bool EVEN>
 __global__ __launch_bounds__(256, 2) void quant_rows_kernel(PagedAttnQuant a) {
@@ -543,10 +534,11 @@ __global__ __launch_bounds__(256, 2) void quant_rows_kernel(PagedAttnQuant a) {
 
     const int kv = a.pages.n_kv_heads, head = (int)(blockIdx.x % (unsigned)kv), x = (int)(blockIdx.x / (unsigned)kv);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, li = lane & 15;
-    const bool split = a.split > 0;
+    const bool tail = a.slots > 0, split = a.split > 0 && !tail;
     const int cost = split ? kTileCost : 0;
     Request rq;
     int request, tiles, tile, at, left, piece = 1, total = 0;
+    int share = 0, shares = 1, cut = 0;                                          // tail: this workgroup's part of a tile, of how many, its number among the cut ones
     if (split) {
         const int32_t *plan = reinterpret_cast<const int32_t *>(a.plan);
         request = ld_scalar(plan, 4 * x);
@@ -560,7 +552,16 @@ __global__ __launch_bounds__(256, 2) void quant_rows_kernel(PagedAttnQuant a) {
         tiles = tiles_of(a, rq, Shape::TILE_ROWS);
     } else {
         Place pl;
-        if (!find_place(a, Shape::TILE_ROWS, false, [&](long long) { return (long long)x; }, pl)) return;
+        auto pick = [&](long long all) -> long long {
+            if (!tail) return x;
+            const int over = (int)(all % a.slots), full = (int)(all - over);
+            if (x < full) return x;
+            shares = over ? min(kMostShares, a.slots / over) : 1;
+            cut = x - full;
+            share = cut % shares;
+            return cut < over * shares ? full + cut / shares : all;
+        };
+        if (!find_place<5, -1, true>(a, Shape::TILE_ROWS, tail, pick, pl)) return;
         request = pl.r;
         rq = pl.q;
         tiles = tiles_of(a, rq, Shape::TILE_ROWS);
@@ -580,15 +581,25 @@ __global__ __launch_bounds__(256, 2) void quant_rows_kernel(PagedAttnQuant a) {
     typedef __attribute__((address_space(3))) unsigned char *lds_bytes;
     const unsigned lds0 = (unsigned)(uintptr_t)(lds_bytes)stages;
     auto lds_frag = [](unsigned at, int more) { return (frag_t *)((lds_bytes)(uintptr_t)at + more); };
-    const unsigned k_put = lds0 + 16 * k_piece<DH>(WK * wave + s_key, 2 * s_ch), v_put = lds0 + SK * DH * 2 + 16 * v_piece<DH>(WK * wave + s_key, 2 * s_ch);
-    const unsigned k_get = lds0 + 16 * k_piece<DH>(li, g), v_get = lds0 + SK * DH * 2 + v_lane<DH>(lane, 0);
+    auto put = [](unsigned at, int more, const frag_t &f) {                     // (as one store of 16 bytes)
+        typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+        *(__attribute__((address_space(3))) u32x4 *)((lds_bytes)(uintptr_t)at + more) = __builtin_bit_cast(u32x4, f);
+    };
+    const unsigned k_put = lds0 + 16 * k_piece<DH, true>(WK * wave + s_key, 2 * s_ch), v_put = lds0 + SK * DH * 2 + 16 * v_piece<DH, true>(WK * wave + s_key, 2 * s_ch);
+    const unsigned k_get = lds0 + 16 * k_piece<DH, true>(li, g), v_get = lds0 + SK * DH * 2 + v_lane<DH, true>(lane, 0);
     for (;;) {
         const int n_rows = rq.m * G, rho0 = (tile * 4 + wave) * 16 * NT;
         int pmin, pmax, wmin, wmax;                                             // positions of the tile's rows and of this wave's
         tile_span(rq, G, tile, Shape::TILE_ROWS, pmin, pmax);
         tile_span(rq, G, tile * 4 + wave, 16 * NT, wmin, wmax);
         const Blocks bl = blocks_of<SHIFT>(a, rq.len, pmin, pmax);
-        const int nb = max(1, bl.count), end = split ? min(nb + cost, at + left) : nb;
+        const int nb = max(1, bl.count);
+        if (tail) {
+            shares = min(shares, max(1, nb / kLeastStages));
+            if (share >= shares) return;
+            at = (int)((long long)share * nb / shares);
+        }
+        const int end = split ? min(nb + cost, at + left) : tail ? (int)((long long)(share + 1) * nb / shares) : nb;
         const int b_lo = max(0, at - cost), b_hi = min(bl.count, end - cost);
         if (end - cost > b_lo) {
             const bool whole = b_lo == 0 && end - cost == nb;
@@ -649,11 +660,11 @@ __global__ __launch_bounds__(256, 2) void quant_rows_kernel(PagedAttnQuant a) {
                         odd |= has_odd_code(vr[j]);
                     }
                     constexpr int P = KEYS * DH / 8;                            // (pieces of the keys of a load; sixteen codes become two pieces)
-                    const int k_turn = 16 * (k_piece<DH>(j * KEYS, 0) - j * P), v_turn = 16 * (v_piece<DH>(j * KEYS, 0) - j * P);
-                    *lds_frag(k_at ^ k_turn, 16 * j * P) = halves8<CODES>(kr[j].w[0], kr[j].w[1]);
-                    *lds_frag(k_at ^ (k_turn + 16), 16 * j * P) = halves8<CODES>(kr[j].w[2], kr[j].w[3]);
-                    *lds_frag(v_at ^ v_turn, 16 * j * P) = halves8<CODES>(vr[j].w[0], vr[j].w[1]);
-                    *lds_frag(v_at ^ (v_turn + 16), 16 * j * P) = halves8<CODES>(vr[j].w[2], vr[j].w[3]);
+                    const int k_turn = 16 * (k_piece<DH, true>(j * KEYS, 0) - j * P), v_turn = 16 * (v_piece<DH, true>(j * KEYS, 0) - j * P);
+                    put(k_at ^ k_turn, 16 * j * P, halves8<CODES>(kr[j].w[0], kr[j].w[1]));
+                    put(k_at ^ (k_turn ^ 16), 16 * j * P, halves8<CODES>(kr[j].w[2], kr[j].w[3]));
+                    put(v_at ^ v_turn, 16 * j * P, halves8<CODES>(vr[j].w[0], vr[j].w[1]));
+                    put(v_at ^ (v_turn ^ 16), 16 * j * P, halves8<CODES>(vr[j].w[2], vr[j].w[3]));
                 }
                 if (lane < 2 * WK) {
                     const int key = WK * wave + (lane & (WK - 1));
@@ -687,7 +698,7 @@ __global__ __launch_bounds__(256, 2) void quant_rows_kernel(PagedAttnQuant a) {
 #pragma unroll
                         for (int s = 0; s < 2; s++)
 #pragma unroll
-                            for (int k = 0; k < KS; k++) kf[s][k] = *lds_frag(k_at ^ (unsigned)(k << 6), (32 * h + 16 * s) * DH * 2);
+                            for (int k = 0; k < KS; k++) kf[s][k] = *lds_frag(k_at ^ (unsigned)(k << 6 ^ (DH > 64 ? pair_turn<DH>(0, 4 * k) << 4 : 0)), (32 * h + 16 * s) * DH * 2);
                         f32x4 ks[2], v[2];
 #pragma unroll
                         for (int s = 0; s < 2; s++) {
@@ -706,7 +717,7 @@ __global__ __launch_bounds__(256, 2) void quant_rows_kernel(PagedAttnQuant a) {
                             }
                         frag_t vt[CT];
 #pragma unroll
-                        for (int c = 0; c < CT; c++) vt[c] = v_operand_at((const unsigned char *)lds_frag(v_at ^ (unsigned)(c << 5), 32 * h * DH * 2), 16 * DH * 2);
+                        for (int c = 0; c < CT; c++) vt[c] = v_operand_at((const unsigned char *)lds_frag(v_at ^ (unsigned)(c << 5 ^ (DH > 64 ? pair_turn<DH>(0, 2 * c) << 4 : 0)), 32 * h * DH * 2), 16 * DH * 2);
                         const uint32_t fl = (uint32_t)__builtin_amdgcn_readfirstlane((int)flag_word);
                         const bool dirty = Code<CODES>::kOdd && (fl & 0x01010101u) != 0;
                         const int pg0 = -(int)(fl >> (8 * (2 * h * 16 / WK)) & 2), pg1 = -(int)(fl >> (8 * ((2 * h + 1) * 16 / WK)) & 2);
@@ -720,16 +731,15 @@ __global__ __launch_bounds__(256, 2) void quant_rows_kernel(PagedAttnQuant a) {
                             if (!EVEN)
 #pragma unroll
                                 for (int s = 0; s < 2; s++) z[t][s] *= ks[s];
-                            float c0 = EVEN ? sc[t] * ks[0][0] : sc[t], c1 = EVEN ? sc[t] * ks[1][0] : sc[t];
+                            float c[2] = {EVEN ? sc[t] * ks[0][0] : sc[t], EVEN ? sc[t] * ks[1][0] : sc[t]};
+                            f32x4 vt2[2] = {v[0], v[1]};
                             if (masked) {
                                 hide_unseen(z[t], sight[t], key32, g, pg0, pg1);
-                                if (EVEN) { c0 = seen_factor(z[t][0], c0); c1 = seen_factor(z[t][1], c1); }
-                                quant_probabilities<CT, EVEN, true>(z[t], c0, c1, v, st[t], lsum[t], o[t], pf, pv);
-                            } else {
-                                quant_probabilities<CT, EVEN, false>(z[t], c0, c1, v, st[t], lsum[t], o[t], pf, pv);
+                                hide_scales<EVEN>(z[t], c, vt2);
                             }
+                            quant_probabilities<CT, EVEN>(z[t], c, vt2, st[t], lsum[t], o[t], pf, pv);
                             if (__builtin_expect(dirty, 0))
-                                add_odd<_Float16, DH>(block, lane, pf, [&](int key) { return sees(sight[t], key32 + key, key & 16 ? pg1 : pg0); }, o[t]);
+                                add_odd<_Float16, DH, true>(block, lane, pf, [&](int key) { return sees(sight[t], key32 + key, key & 16 ? pg1 : pg0); }, o[t]);
                             lsum[t] = mfma16(ones, pf, lsum[t]);
 #pragma unroll
                             for (int c = 0; c < CT; c++) o[t][c] = mfma16(vt[c], pv, o[t][c]);
@@ -744,7 +754,7 @@ __global__ __launch_bounds__(256, 2) void quant_rows_kernel(PagedAttnQuant a) {
             // ---- results, or sums for the joining kernel
             int tid = threadIdx.x;                                                  // (hidden, as above)
             asm volatile("" : "+v"(tid));
-            const int parts = whole ? 1 : (piece * x + (min(piece, total - piece * x) - left) - at + cost + nb - 1) / piece - x + 1;
+            const int part0 = tail ? cut : x, parts = whole ? 1 : tail ? shares : (piece * x + (min(piece, total - piece * x) - left) - at + cost + nb - 1) / piece - x + 1;
 #pragma unroll
             for (int t = 0; t < NT; t++) {
                 const int in_tile = wave * 16 * NT + t * 16 + (tid & 15), rho = tile * Shape::TILE_ROWS + in_tile, eg = (tid >> 4) & 3;
@@ -752,12 +762,12 @@ __global__ __launch_bounds__(256, 2) void quant_rows_kernel(PagedAttnQuant a) {
                 const int i = rho / G, hq = head * G + (rho - i * G);
                 const float l = checked_quant_sum(st[t].at, lsum[t][0]);
                 if (!whole) {
-                    const long long place = ((2ll * x + (b_lo == 0)) * kv + head) * Shape::TILE_ROWS + in_tile;
+                    const long long place = ((2ll * part0 + (b_lo == 0)) * kv + head) * Shape::TILE_ROWS + in_tile;
 #pragma unroll
                     for (int c = 0; c < CT; c++) *reinterpret_cast<f32x4 *>(a.partial + place * DH + c * 16 + 4 * eg) = o[t][c] * st[t].unit;
                     if (eg == 0) {
                         a.ml[place] = float2{st[t].at, l};
-                        if (b_lo == 0) a.where[(size_t)(rq.row0 + i) * a.heads + hq] = int2{x, parts * kRowsPlace + in_tile};
+                        if (b_lo == 0) a.where[(size_t)(rq.row0 + i) * a.heads + hq] = int2{part0, parts * kRowsPlace + in_tile};
                     }
                     continue;
                 }
@@ -769,7 +779,7 @@ __global__ __launch_bounds__(256, 2) void quant_rows_kernel(PagedAttnQuant a) {
                                                              : uint2{Num<__bf16>::pack(y[0], y[1]), Num<__bf16>::pack(y[2], y[3])};
                     store_out4(a, rq.row0 + i, hq, DH, c * 16 + 4 * eg, w);
                 }
-                if (split && eg == 0) a.where[(size_t)(rq.row0 + i) * a.heads + hq] = int2{x, 0};
+                if (a.split && eg == 0) a.where[(size_t)(rq.row0 + i) * a.heads + hq] = int2{part0, 0};
             }
         }
         if (!split) return;
@@ -793,7 +803,7 @@ void launch_quant_dim(const PagedAttnQuant &a, int nt, hipStream_t s) {
     if (nt == kManyRows) {
         constexpr int bytes = 2 * 2 * RowsShape<DH>::SK * DH * 2;
         allow_lds<quant_rows_kernel<CODES, DH, EVEN>>(bytes);
-        if (a.split) launch_paged_plan(a, s);
+        if (a.split && !a.slots) launch_paged_plan(a, s);
         quant_rows_kernel<CODES, DH, EVEN><<<grid, 256, bytes, s>>>(a);
     } else if (nt == 1) {
         quant_attn_kernel<CODES, DH, 1, EVEN><<<grid, 256, 0, s>>>(a);
