@@ -633,7 +633,7 @@ int odb_qk_norm_rope_quant(const odb_quant_rows *rows, const odb_quant_pages *pa
  * apart.  slots dev int32 [rows] as odb_page_tables writes them; a slot outside the pool gives zeros.  code * scale in 32 bits, rounded
  * once, to an infinity beyond the type's range.  (pages->dtype is not looked at.)  Requirements: outputs aligned to 16 bytes, strides multiples of 8,
  * outputs that do not overlap.  Asynchronous on `stream`.  rows = 0 launches nothing.  Errors: ODB_E_INVALID_ARG, also where rows * n_kv_heads *
- * head_dim reaches 2^34. */
+ * head_dim reaches 2^33. */
 int odb_paged_read_quant(const odb_quant_pages *pages, const int32_t *slots, int rows, int out_dtype, void *k_out, void *v_out, long long k_row,
                          long long v_row, void *stream);
 

@@ -305,7 +305,7 @@ int odb_paged_read_quant(const odb_quant_pages *pages, const int32_t *slots, int
     if (rc) return rc;
     const int dim = any.head_dim, kv = any.n_kv_heads;
     if (rows < 0 || rows > 1 << 24) return fail(ODB_E_INVALID_ARG, "%s: rows=%d outside [0, 2^24]", who, rows);
-    if ((long long)rows * kv * dim >= 1ll << 34) return fail(ODB_E_INVALID_ARG, "%s: %d rows of %d heads are too many for one launch", who, rows, kv);
+    if ((long long)rows * kv * dim >= 1ll << 33) return fail(ODB_E_INVALID_ARG, "%s: %d rows of %d heads are too many for one launch", who, rows, kv);
     if (!slots) return fail(ODB_E_INVALID_ARG, "%s: NULL slots", who);
     if (out_dtype != ODB_F16 && out_dtype != ODB_BF16 && out_dtype != ODB_F32) return fail(ODB_E_INVALID_ARG, "%s: out_dtype=%d", who, out_dtype);
     if ((rc = check_rows(who, "k_out", k_out, k_row, kv, dim)) || (rc = check_rows(who, "v_out", v_out, v_row, kv, dim))) return rc;

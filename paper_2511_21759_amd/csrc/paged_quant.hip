@@ -77,7 +77,10 @@ long long quant_workgroups(int n, int rows, int heads, bool cu_rows, int rows_pe
 
 // Two kinds of workgroups in one launch.  The first `span_groups` take a span of positions of one request, for one head, K or V:
 // DH / 16 lanes a position with sixteen channels each, which stay in registers from the load to the codes; the largest magnitude of a group
-// goes through lanes and LDS.  The others norm and turn queries, as qk_norm_rope_kernel does.
+// goes through lanes and LDS.  The others norm and turn queries, as qk_norm_rope_kernel does, a row and group of heads a wave.
+// Bound by the memory: 11735 rows of four prompts, 48 heads of 128 in bfloat16, 267 MB, 66 us (4.0 TB/s; a copy 5.1; two rows of queries a wave 72, stored
+// past the caches 64).  Few rows are bound by loads that wait for each other - row offsets, lengths, page, scale: eleven tokens 4.8 us,
+// 6 x 32 rows of 96 heads from 32 bits 7.6.
 template <class TI, class TO, int DH, int PASSES>
 __global__ __launch_bounds__(256) void qk_norm_rope_quant_kernel(QkNormRopeQuant a, unsigned span_groups) {
     constexpr int LANES = DH / 16, PER_WAVE = 64 / LANES, PER_PASS = 4 * PER_WAVE, SPAN = PER_PASS * PASSES;
@@ -324,34 +327,57 @@ void launch_qk_norm_rope_quant(const QkNormRopeQuant &a, hipStream_t s) {
 
 // ---- values read back ------------------------------------------------------------------------------------------------
 
-// Eight channels a lane, K and V of a row beside each other in the order of the lanes: loads of 512 contiguous bytes of codes at the most,
-// stores of 1 KiB and more.
+// Sixteen bytes of values a lane, K and V of a row beside each other in the order of the lanes, of two rows whose loads are on their way
+// together; stored past the caches.  Bound by the memory: 24001 positions of 8 heads of 128, 147 MB, 22.8 us (6.4 TB/s; with ordinary stores 34, one
+// row 40), to 32 bits 39 (ordinary stores 65).  70 positions 2.6 us: a slot, then its codes.
+constexpr int kReadRows = 2;
 template <class TO>
 __global__ __launch_bounds__(256) void paged_read_quant_kernel(PagedReadQuant a, unsigned per_row) {
-    const unsigned t = blockIdx.x * 256u + threadIdx.x, row = t / per_row;
-    if (row >= (unsigned)a.rows) return;
+    constexpr int CH = 16 / sizeof(TO), WORDS = CH / 4;
+    typedef TO out_t __attribute__((ext_vector_type(CH)));
+    typedef float f32_t __attribute__((ext_vector_type(CH)));
+    const unsigned t = blockIdx.x * 256u + threadIdx.x, part = t / per_row, row0 = part * kReadRows;
+    if (row0 >= (unsigned)a.rows) return;
     const odb_pages &pg = a.pages;
-    const unsigned half = per_row >> 1, at = t - row * per_row, is_v = at >= half, e = (at - (is_v ? half : 0)) * 8, head = e / (unsigned)pg.head_dim, c = e % (unsigned)pg.head_dim;
-    const int slot = a.slots[row], page = slot >= 0 ? (int)((unsigned)slot / (unsigned)pg.page_size) : -1;
-    f32x8 x = f32x8{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (page >= 0 && page < pg.n_pages) {
-        const int in = slot - page * pg.page_size;
-        const unsigned char *src = (const unsigned char *)(is_v ? pg.v : pg.k) + (size_t)page * pg.page_stride + (size_t)head * pg.head_stride + (size_t)in * pg.pos_stride + c;
-        const float *s = (is_v ? a.scales.v : a.scales.k) + (size_t)page * a.scales.page_stride + (size_t)head * a.scales.head_stride + (in >> a.scales.group_shift);
-        const uint2 w = *reinterpret_cast<const uint2 *>(src);
-        const float scale = *s;
-        const bool int8 = a.scales.codes == ODB_INT8;
-        const f32x4 u = numbers4(int8, w.x) * scale, v = numbers4(int8, w.y) * scale;
+    const unsigned half = per_row >> 1, at = t - part * per_row, is_v = at >= half, e = (at - (is_v ? half : 0)) * CH, head = e / (unsigned)pg.head_dim, c = e % (unsigned)pg.head_dim;
+    const unsigned char *codes = (const unsigned char *)(is_v ? pg.v : pg.k) + (size_t)head * pg.head_stride + c;
+    const float *scales = (is_v ? a.scales.v : a.scales.k) + (size_t)head * a.scales.head_stride;
+    uint32_t w[kReadRows][WORDS];
+    float scale[kReadRows];
+    bool there[kReadRows];
 #pragma unroll
-        for (int i = 0; i < 4; i++) { x[i] = u[i]; x[4 + i] = v[i]; }
+    for (int i = 0; i < kReadRows; i++) {
+        const int slot = row0 + i < (unsigned)a.rows ? a.slots[row0 + i] : -1, page = slot >= 0 ? (int)((unsigned)slot / (unsigned)pg.page_size) : -1;
+        there[i] = page >= 0 && page < pg.n_pages;
+        const int in = there[i] ? slot - page * pg.page_size : 0;
+        const size_t from = there[i] ? page : 0;
+        const uint32_t *src = reinterpret_cast<const uint32_t *>(codes + from * pg.page_stride + (size_t)in * pg.pos_stride);
+#pragma unroll
+        for (int j = 0; j < WORDS; j++) w[i][j] = src[j];
+        scale[i] = scales[from * a.scales.page_stride + (in >> a.scales.group_shift)];
     }
-    store8((TO *)(is_v ? a.v : a.k) + (size_t)row * (is_v ? a.v_row : a.k_row) + e, x);
+    const bool int8 = a.scales.codes == ODB_INT8;
+    TO *out = (TO *)(is_v ? a.v : a.k) + e;
+    const long long stride = is_v ? a.v_row : a.k_row;
+#pragma unroll
+    for (int i = 0; i < kReadRows; i++) {
+        if (row0 + i >= (unsigned)a.rows) return;
+        f32_t x;
+#pragma unroll
+        for (int j = 0; j < WORDS; j++) {
+            const f32x4 u = numbers4(int8, w[i][j]) * scale[i];
+#pragma unroll
+            for (int k = 0; k < 4; k++) x[4 * j + k] = there[i] ? u[k] : 0.f;
+        }
+        out_t *dst = reinterpret_cast<out_t *>(out + (size_t)(row0 + i) * stride);
+        __builtin_nontemporal_store(__builtin_convertvector(x, out_t), dst);
+    }
 }
 
 void launch_paged_read_quant(const PagedReadQuant &a, hipStream_t s) {
     if (a.rows < 1) return;
-    const unsigned per_row = 2u * a.pages.n_kv_heads * a.pages.head_dim / 8;
-    const dim3 grid((unsigned)(((unsigned long long)a.rows * per_row + 255) / 256));
+    const unsigned per_row = 2u * a.pages.n_kv_heads * a.pages.head_dim / (a.out_dtype == ODB_F32 ? 4 : 8);
+    const dim3 grid((unsigned)((((unsigned long long)a.rows + kReadRows - 1) / kReadRows * per_row + 255) / 256));
     if (a.out_dtype == ODB_F16) paged_read_quant_kernel<_Float16><<<grid, 256, 0, s>>>(a, per_row);
     else if (a.out_dtype == ODB_BF16) paged_read_quant_kernel<__bf16><<<grid, 256, 0, s>>>(a, per_row);
     else paged_read_quant_kernel<float><<<grid, 256, 0, s>>>(a, per_row);
