@@ -191,7 +191,37 @@ def lib() -> ctypes.CDLL:
     L.odb_strerror.restype = ctypes.c_char_p
     L.odb_last_error.restype = ctypes.c_char_p
     _lib = L
+    _entries()
     return L
+
+
+_marshal = None
+_store_at = _read_at = _attention_at = _workspace_at = 0
+
+
+def _entries():
+    """Loads _marshal, which makes the calls of 8-bit pages whose tensors are as described (None from it: this file's own path goes through
+    them again, and says what is wrong), and notes the entry points' addresses for it."""
+    global _marshal, _store_at, _read_at, _attention_at, _workspace_at
+    from . import _marshal
+    _store_at, _read_at, _attention_at, _workspace_at = (ctypes.cast(f, ctypes.c_void_p).value for f in (
+        _lib.odb_qk_norm_rope_quant, _lib.odb_paged_read_quant, _lib.odb_paged_attention_quant, _lib.odb_paged_attention_quant_workspace))
+
+
+def _here(index):
+    """The current stream of device `index` if that is the current device, else None."""
+    if _lib is None:
+        lib()
+    if index < 0 or _torch.cuda.current_device() != index:
+        return None
+    return _raw_stream(index) if _raw_stream is not None else _stream()
+
+
+def _made(got):
+    """What _marshal gave: results, or an error code."""
+    if type(got) is int:
+        _check(got)
+    return got
 
 
 def _check(rc: int) -> None:
@@ -713,6 +743,12 @@ def odb_qk_norm_rope_quant(q, k, v, k_pages, v_pages, k_scale, v_scale, table, p
         dtype = out.dtype if out is not None else given
     if dtype is not torch.bfloat16 and dtype is not torch.float16:
         raise TypeError("queries become float16 or bfloat16: give dtype")
+    stream = _here(index)
+    if stream is not None:
+        got = _marshal.store(_store_at, stream, index, q, k, v, k_pages, v_pages, k_scale, v_scale, table, positions, tables, kv_len, cu_rows, first_pos,
+                             q_gain, k_gain, eps, interleaved, dtype is torch.bfloat16, out, odd)
+        if got is not None:
+            return _made(got)
     pages = _quant_pages(k_pages, v_pages, k_scale, v_scale, index, _DTYPES[dtype])
     shape = rows, heads, dim = q.shape
     kv = (rows, k_pages.shape[1], dim)
@@ -751,6 +787,11 @@ def odb_paged_read_quant(k_pages, v_pages, k_scale, v_scale, slots, dtype=None, 
     bfloat16 or float32, or `out` = (k, v)."""
     torch = _torch or _load_torch()
     index = slots.get_device()
+    stream = _here(index)
+    if stream is not None and out is None:
+        got = _marshal.read(_read_at, stream, index, k_pages, v_pages, k_scale, v_scale, slots, _DTYPES.get(dtype, -1) if dtype is not None else 0)
+        if got is not None:
+            return _made(got)
     pages = _quant_pages(k_pages, v_pages, k_scale, v_scale, index)
     if out is not None:
         dtype = out[0].dtype
@@ -786,7 +827,14 @@ def odb_paged_attention_quant(q, k_pages, v_pages, k_scale, v_scale, tables, kv_
     torch = _torch or _load_torch()
     if q.dtype is not torch.bfloat16 and q.dtype is not torch.float16:
         raise TypeError("q must be float16 or bfloat16")
-    pages = _quant_pages(k_pages, v_pages, k_scale, v_scale, q.get_device(), _DTYPES[q.dtype])
+    index = q.get_device()
+    stream = _here(index)
+    if stream is not None:
+        got = _marshal.attention(_attention_at, _workspace_at, stream, index, q, k_pages, v_pages, k_scale, v_scale, tables, kv_len, cu_rows, first_pos,
+                                 k_pages.shape[3] ** -0.5 if scale is None else scale, causal, window, sinks, max_rows, max_len, out, workspace)
+        if got is not None:
+            return _made(got)
+    pages = _quant_pages(k_pages, v_pages, k_scale, v_scale, index, _DTYPES[q.dtype])
     return _attention(odb_paged_attention_quant_workspace, lib().odb_paged_attention_quant, q, k_pages, pages, q.dtype, tables, kv_len, causal, cu_rows,
                       first_pos, scale, window, sinks, max_rows, max_len, out, workspace)
 

@@ -38,6 +38,20 @@ def _run(cmd):
     return out
 
 
+def build_marshal() -> str:
+    """_marshal: packs tensors into the C structures of calls where latency counts (csrc/marshal.cpp); host code against torch's headers."""
+    import sysconfig
+    import torch
+    from torch.utils.cpp_extension import include_paths
+    to = os.path.join(HERE, "_marshal.so")
+    flags = ["-O2", "-std=c++17", "-fPIC", "-shared", "-w", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI]
+    flags += ["-isystem" + p for p in include_paths() + [sysconfig.get_paths()["include"]]]
+    libs = ["-L" + os.path.join(os.path.dirname(torch.__file__), "lib"), "-lc10", "-ltorch_cpu", "-ltorch_python"]
+    _run([shutil.which("g++") or "c++", *flags, os.path.join(CSRC, "marshal.cpp"), "-o", to + ".tmp", *libs])
+    os.replace(to + ".tmp", to)
+    return to
+
+
 def build_library(verbose: bool = False, extra_flags=()) -> str:
     hipcc = _hipcc()
     objdir = os.path.join(HERE, "_build")
@@ -47,10 +61,12 @@ def build_library(verbose: bool = False, extra_flags=()) -> str:
     def compile_one(i):
         return _run([hipcc, *FLAGS, *extra_flags, "-c", os.path.join(CSRC, SOURCES[i]), "-o", objs[i]])
 
-    with concurrent.futures.ThreadPoolExecutor(max_workers=min(8, len(SOURCES))) as ex:
+    with concurrent.futures.ThreadPoolExecutor(max_workers=min(8, len(SOURCES) + 1)) as ex:
+        marshal = ex.submit(build_marshal)
         for out in ex.map(compile_one, range(len(SOURCES))):
             if verbose and out.strip():
                 print(out, file=sys.stderr)
+        marshal.result()
     tmp = LIB + ".tmp"
     _run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp, *objs])
     os.replace(tmp, LIB)
