@@ -27,7 +27,7 @@ SYMBOLS = (
     "odb_block_step_shared_rows", "odb_block_step_shared_logits", "odb_cache_truncate", "odb_generate",
     "odb_speculative_jump", "odb_page_tables", "odb_rope_table", "odb_qk_norm_rope", "odb_paged_attention",
     "odb_paged_attention_workspace", "odb_step_paged", "odb_qk_norm_rope_quant", "odb_paged_read_quant", "odb_paged_attention_quant",
-    "odb_paged_attention_quant_workspace",
+    "odb_paged_attention_quant_workspace", "odb_step_paged_quant",
 )
 
 KERNEL_CLASSES = ("gemm_qkv", "attention", "gemm_o", "gemm_gate_up", "gemm_down", "gemm_lm_head", "rmsnorm")
@@ -187,6 +187,7 @@ def lib() -> ctypes.CDLL:
     L.odb_paged_attention_quant.argtypes = [vp, vp, vp]
     L.odb_paged_attention_quant_workspace.argtypes = [vp, vp]
     L.odb_paged_attention_quant_workspace.restype = ctypes.c_longlong
+    L.odb_step_paged_quant.argtypes = [vp, vp, vp, ctypes.c_longlong, vp]
     L.odb_strerror.argtypes = [ci]
     L.odb_strerror.restype = ctypes.c_char_p
     L.odb_last_error.restype = ctypes.c_char_p
@@ -844,7 +845,29 @@ def odb_step_paged(model: int, tokens, k_pages, v_pages, tables, first_pos, kv_l
     """tokens int32 [n, b]; k_pages, v_pages float16 [n_layers, n_pages, n_heads, page_size, head_dim]; tables int32 [n, columns];
     first_pos, kv_len int32 [n]; positions, slots int32 [n * b]; table float32 [n_pos, head_dim / 2, 2] -> (conf f32, argmax int32,
     each [n, b - skip], unmask uint8 [n, b] or None): unmask with a threshold tau only; all None with head=False."""
-    torch = _torch or _load_torch()
+    _torch or _load_torch()
+    r, outs = _paged_rows(tokens, k_pages, v_pages, tables, first_pos, kv_len, positions, slots, table, tau, skip, head, max_len)
+    _on(tokens.get_device(), lib().odb_step_paged, model, ctypes.byref(r), _pages(k_pages[0], v_pages[0]))
+    return outs
+
+
+def odb_step_paged_quant(model: int, tokens, k_pages, v_pages, k_scale, v_scale, tables, first_pos, kv_len, positions, table, tau: Optional[float] = None,
+                         skip: int = 0, head: bool = True, max_len: int = 0):
+    """odb_step_paged over pages of 8-bit codes: k_pages, v_pages int8 or float8_e4m3fn [n_layers, n_pages, n_heads, page_size, head_dim],
+    k_scale, v_scale float32 [n_layers, n_pages, n_heads, page_size / group]."""
+    _torch or _load_torch()
+    r, outs = _paged_rows(tokens, k_pages, v_pages, tables, first_pos, kv_len, positions, None, table, tau, skip, head, max_len)
+    if k_scale.dim() != 4 or k_scale.shape != v_scale.shape or k_scale.stride() != v_scale.stride() or k_scale.shape[0] != k_pages.shape[0]:
+        raise TypeError("k_scale and v_scale must be [n_layers, n_pages, n_heads, page_size / group] with the same strides")
+    index = tokens.get_device()
+    pages = _quant_pages(k_pages[0], v_pages[0], k_scale[0], v_scale[0], index)
+    _on(index, lib().odb_step_paged_quant, model, ctypes.byref(r), pages, k_scale.stride(0))
+    return outs
+
+
+def _paged_rows(tokens, k_pages, v_pages, tables, first_pos, kv_len, positions, slots, table, tau, skip, head, max_len):
+    """An odb_paged_rows, and what it writes: (conf, argmax, unmask)."""
+    torch = _torch
     index, i32 = tokens.get_device(), torch.int32
     n, b = tokens.shape
     if k_pages.dim() != 5 or k_pages.shape != v_pages.shape or k_pages.stride() != v_pages.stride() or k_pages.get_device() != index:
@@ -861,11 +884,11 @@ def odb_step_paged(model: int, tokens, k_pages, v_pages, tables, first_pos, kv_l
         unmask = None if tau is None else tokens.new_empty((n, b), dtype=torch.uint8)
     r = odb_paged_rows(_ints("tokens", tokens, (n, b), index, i32), n, b, _ints("first_pos", first_pos, (n,), index, i32),
                        _ints("kv_len", kv_len, (n,), index, i32), _ints("tables", tables, (n, tables.shape[1]), index, i32), tables.shape[1],
-                       _ints("positions", positions, (n * b,), index, i32), _ints("slots", slots, (n * b,), index, i32), table.data_ptr(), table.shape[0],
+                       _ints("positions", positions, (n * b,), index, i32), 0 if slots is None else _ints("slots", slots, (n * b,), index, i32), table.data_ptr(),
+                       table.shape[0],
                        k_pages.stride(0), skip, max_len, 0.0 if tau is None else tau, *(None if t is None else t.data_ptr() for t in (conf, argmax, unmask)),
                        k_pages.shape[0])
-    _on(index, lib().odb_step_paged, model, ctypes.byref(r), _pages(k_pages[0], v_pages[0]))
-    return conf, argmax, unmask
+    return r, (conf, argmax, unmask)
 
 
 def odb_set_option(model: int, option: int, value: int) -> None:

@@ -1098,14 +1098,14 @@ int odb_block_step_static(odb_model *m, const odb_cache *c, const int32_t *draft
 // The stack over paged K/V: rows of requests of different lengths, dense.  QKV leaves 32-bit rows, which are turned and stored in the
 // pages in one pass (Q and K in the interleaved channel order of the projection's weights, whose scores are the same); attention
 // over the pages hands its rows to O in operand order.
-int odb_step_paged(odb_model *mh, const odb_paged_rows *args, const odb_pages *layer0, void *stream) {
-    const char *who = "step_paged";
-    if (!mh || !args || !layer0) return fail(ODB_E_INVALID_ARG, "%s: NULL argument", who);
+// `quant`: pages of 8-bit codes (layer0 is their part that both kinds have), whose scales lie scale_stride floats further with each layer.
+static int step_paged(const char *who, odb_model *mh, const odb_paged_rows *args, const odb_pages *layer0, const odb_quant_pages *quant, long long scale_stride,
+                      void *stream) {
     Model &m = mh->m;
     const odb_config &cfg = m.cfg;
     const odb_paged_rows &r = *args;
     const int d = cfg.d_model, H = cfg.n_heads, dh = cfg.head_dim, F = cfg.d_ff;
-    if (!r.tokens || !r.first_pos || !r.kv_len || !r.tables || !r.positions || !r.slots || !r.table) return fail(ODB_E_INVALID_ARG, "%s: NULL input", who);
+    if (!r.tokens || !r.first_pos || !r.kv_len || !r.tables || !r.positions || !(r.slots || quant) || !r.table) return fail(ODB_E_INVALID_ARG, "%s: NULL input", who);
     if (r.n < 1 || r.n > kMaxRequests || r.b < 1 || r.b > 65536 || (long long)r.n * r.b > 65536)
         return fail(ODB_E_INVALID_ARG, "%s: %d requests of %d rows (at most 65536 rows)", who, r.n, r.b);
     if (r.skip < 0 || r.skip >= r.b) return fail(ODB_E_INVALID_ARG, "%s: skip=%d outside [0, %d)", who, r.skip, r.b);
@@ -1115,7 +1115,9 @@ int odb_step_paged(odb_model *mh, const odb_paged_rows *args, const odb_pages *l
         return fail(ODB_E_INVALID_ARG, "%s: pages of %d heads of %d, dtype %d; the model has %d of %d in binary16", who, layer0->n_kv_heads, layer0->head_dim,
                     layer0->dtype, H, dh);
     if (r.n_layers != cfg.n_layers) return fail(ODB_E_INVALID_ARG, "%s: pools of %d layers; the model has %d", who, r.n_layers, cfg.n_layers);
-    if (cfg.n_layers > 1 && (r.layer_stride < 8 || r.layer_stride & 7)) return fail(ODB_E_INVALID_ARG, "%s: layer_stride=%lld", who, r.layer_stride);
+    const int align = quant ? 16 : 8;
+    if (cfg.n_layers > 1 && (r.layer_stride < align || r.layer_stride & (align - 1))) return fail(ODB_E_INVALID_ARG, "%s: layer_stride=%lld", who, r.layer_stride);
+    if (quant && cfg.n_layers > 1 && (scale_stride < 4 || scale_stride & 3)) return fail(ODB_E_INVALID_ARG, "%s: scale_layer_stride=%lld", who, scale_stride);
     const int rows = r.n * r.b, rows_pad = ru(rows, 16), mt = rows_pad / 16;
     const bool head = r.conf != nullptr, fused_head = r.unmask != nullptr;
 
@@ -1124,10 +1126,11 @@ int odb_step_paged(odb_model *mh, const odb_paged_rows *args, const odb_pages *l
     at.columns = r.columns; at.n = r.n; at.rows = rows; at.n_heads = H;
     at.scale = 1.0f / sqrtf((float)dh);
     at.max_rows = r.b; at.max_len = r.max_len;
-    PagedAttn pa;
+    PagedAttnQuant pa{};
     int nt;
-    int rc = plan_paged_attention(&at, layer0, true, pa, nt);
+    int rc = quant ? plan_paged_attention_quant(&at, quant, true, pa, nt) : plan_paged_attention(&at, layer0, true, pa, nt);
     if (rc) return rc;
+    if (quant && quant_workgroups(r.n, rows, H, false, r.b, *layer0, pa.scales) >= 1 << 24) return fail(ODB_E_INVALID_ARG, "%s: %d rows are too many for one launch", who, rows);
     const size_t qkv_bytes = align_up((size_t)rows_pad * 3 * d * 4, 256), at_bytes = paged_attn_workspace(*layer0, rows, H, nt, pa.split);
     if (r.n_pos < 1 || r.n_pos > 1 << 22 || (uintptr_t)r.table & 15) return fail(ODB_E_INVALID_ARG, "%s: table of %d positions, or not aligned to 16 bytes", who, r.n_pos);
 
@@ -1149,23 +1152,33 @@ int odb_step_paged(odb_model *mh, const odb_paged_rows *args, const odb_pages *l
 
     QkNormRope qk{qkv, qkv + d, qkv + 2 * (size_t)d, ODB_F32, 3ll * d, 3ll * d, 3ll * d, rows, H, nullptr, nullptr, 0.f, r.table, r.n_pos, dh, 1, r.positions,
                   r.slots, q, d, *layer0, nullptr, m.counters};
+    QkNormRopeQuant qq{qkv, qkv + d, qkv + 2 * (size_t)d, ODB_F32, 3ll * d, 3ll * d, 3ll * d, rows, H, nullptr, nullptr, 0.f, r.table, r.n_pos, dh, 1, r.positions,
+                       q, d, nullptr, r.first_pos, r.kv_len, r.tables, r.b, r.columns, r.n, pa.page_shift, *layer0, pa.scales, m.counters, kStatusSaturated, m.counters};
     pa.q = q; pa.out = ao; pa.q_row = pa.out_row = d; pa.out_mt = mt;
     pa.rows_per_request = r.b;
     pa.first = r.first_pos; pa.kv_len = r.kv_len; pa.tables = r.tables;
     pa.sc = at.scale * 1.44269504088896340736f;
     for (int l = 0; l < cfg.n_layers; l++) {
         LayerPtrs w = layer_ptrs(m, l);
-        qk.pages.k = (u16 *)layer0->k + (size_t)l * r.layer_stride;
-        qk.pages.v = (u16 *)layer0->v + (size_t)l * r.layer_stride;
-        pa.pages = qk.pages;
+        const size_t layer = (size_t)l * r.layer_stride * (quant ? 1 : 2);
+        pa.pages.k = (char *)layer0->k + layer;
+        pa.pages.v = (char *)layer0->v + layer;
+        if (quant) {
+            pa.scales.k = quant->k_scale + (size_t)l * scale_stride;
+            pa.scales.v = quant->v_scale + (size_t)l * scale_stride;
+            qq.scales = pa.scales;
+        }
+        qk.pages = qq.pages = pa.pages;
         {
             ProfScope ps(m, ODB_K_GEMM_QKV, s);
             launch_gemm_store(xa, w.qkv, GemmShape{mt, 3 * d / 16, d / 32}, ni, qkv, 1, rows_pad, rows, 3 * d, ws, s);
         }
-        launch_qk_norm_rope(qk, s);
+        if (quant) launch_qk_norm_rope_quant(qq, s);
+        else launch_qk_norm_rope(qk, s);
         {
             ProfScope ps(m, ODB_K_ATTENTION, s);
-            launch_paged_attention(pa, nt, base + pl.extra + qkv_bytes, s);
+            if (quant) launch_paged_attention_quant(pa, nt, base + pl.extra + qkv_bytes, s);
+            else launch_paged_attention(pa, nt, base + pl.extra + qkv_bytes, s);
         }
         const float *g_after_mlp = l + 1 < cfg.n_layers ? m.g1 + (size_t)(l + 1) * d : m.gf;
         {
@@ -1185,6 +1198,18 @@ int odb_step_paged(odb_model *mh, const odb_paged_rows *args, const odb_pages *l
     if (!head) return ODB_OK;
     if (fused_head) return run_head(m, base, pl, rm, 0, true, r.tokens, r.b, r.tau, r.conf, r.argmax, r.unmask, nullptr, s);
     return run_head(m, base, pl, RowMap{r.n, r.b, r.b}, r.skip, false, nullptr, 64, 0.f, r.conf, r.argmax, nullptr, nullptr, s);
+}
+
+int odb_step_paged(odb_model *mh, const odb_paged_rows *args, const odb_pages *layer0, void *stream) {
+    if (!mh || !args || !layer0) return fail(ODB_E_INVALID_ARG, "step_paged: NULL argument");
+    return step_paged("step_paged", mh, args, layer0, nullptr, 0, stream);
+}
+
+int odb_step_paged_quant(odb_model *mh, const odb_paged_rows *args, const odb_quant_pages *layer0, long long scale_layer_stride, void *stream) {
+    if (!mh || !args || !layer0) return fail(ODB_E_INVALID_ARG, "step_paged_quant: NULL argument");
+    const odb_pages codes{layer0->k, layer0->v, layer0->n_pages, layer0->page_size, layer0->n_kv_heads, layer0->head_dim, layer0->dtype,
+                          layer0->page_stride, layer0->head_stride, layer0->pos_stride};
+    return step_paged("step_paged_quant", mh, args, &codes, layer0, scale_layer_stride, stream);
 }
 
 }  // extern "C"
