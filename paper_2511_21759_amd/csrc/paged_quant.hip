@@ -75,12 +75,12 @@ long long quant_workgroups(int n, int rows, int heads, bool cu_rows, int rows_pe
     return quant_spans(n, rows, cu_rows, rows_per_request, s, p.head_dim) * 2 * p.n_kv_heads + query_workgroups(rows, heads, p.head_dim);
 }
 
-// Two kinds of workgroups in one launch.  The first `span_groups` take a span of positions of one request, for one head, K or V:
+// Two kinds of workgroups in one launch.  The last `span_groups` take a span of positions of one request, for one head, K or V:
 // DH / 16 lanes a position with sixteen channels each, which stay in registers from the load to the codes; the largest magnitude of a group
 // goes through lanes and LDS.  The others norm and turn queries, as qk_norm_rope_kernel does, a row and group of heads a wave.
-// Bound by the memory: 11735 rows of four prompts, 48 heads of 128 in bfloat16, 267 MB, 66 us (4.0 TB/s; a copy 5.1; two rows of queries a wave 72, stored
-// past the caches 64).  Few rows are bound by loads that wait for each other - row offsets, lengths, page, scale: eleven tokens 4.8 us,
-// 6 x 32 rows of 96 heads from 32 bits 7.6.
+// Bound by the memory: 11735 rows of four prompts, 48 heads of 128 in bfloat16, 267 MB, 62 us (4.3 TB/s; a copy 5.1; queries behind the spans 66, two rows of them a wave 72, stored
+// past the caches 64).  Few rows are bound by loads that wait for each other - row offsets, lengths, page, scale: eleven tokens 4.7 us,
+// 6 x 32 rows of 96 heads from 32 bits 7.0.
 template <class TI, class TO, int DH, int PASSES>
 __global__ __launch_bounds__(256) void qk_norm_rope_quant_kernel(QkNormRopeQuant a, unsigned span_groups) {
     constexpr int LANES = DH / 16, PER_WAVE = 64 / LANES, PER_PASS = 4 * PER_WAVE, SPAN = PER_PASS * PASSES;
@@ -96,9 +96,10 @@ __global__ __launch_bounds__(256) void qk_norm_rope_quant_kernel(QkNormRopeQuant
     };
     const f32x8 zeros = f32x8{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 
-    if (blockIdx.x >= span_groups) {                            // queries
+    const unsigned query_groups = gridDim.x - span_groups;
+    if (blockIdx.x < query_groups) {                            // queries
         const int waves_per_row = (a.heads + PER_WAVE - 1) / PER_WAVE;
-        const unsigned w = (blockIdx.x - span_groups) * 4u + wave;
+        const unsigned w = blockIdx.x * 4u + wave;
         const int row = (int)(w / (unsigned)waves_per_row), head = (int)(w % (unsigned)waves_per_row) * PER_WAVE + slice;
         if (row >= a.rows || head >= a.heads) return;
         const int pos = a.positions[row];
@@ -131,9 +132,10 @@ __global__ __launch_bounds__(256) void qk_norm_rope_quant_kernel(QkNormRopeQuant
     }
 
     // ---- keys or values of a span: which
-    const bool is_k = blockIdx.x & 1;
-    const int head = (int)((blockIdx.x >> 1) % (unsigned)kv);
-    int number = (int)((blockIdx.x >> 1) / (unsigned)kv), r = 0, lo, hi;
+    const unsigned item = blockIdx.x - query_groups;
+    const bool is_k = item & 1;
+    const int head = (int)((item >> 1) % (unsigned)kv);
+    int number = (int)((item >> 1) / (unsigned)kv), r = 0, lo, hi;
     constexpr int SHIFT = SPAN == 16 ? 4 : SPAN == 32 ? 5 : 6;
     static_assert(1 << SHIFT == SPAN, "span");
     if (a.cu_rows) {
