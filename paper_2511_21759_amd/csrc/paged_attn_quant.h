@@ -78,6 +78,8 @@ __device__ __forceinline__ void load_queries(const PagedAttn &a, const u16 *src,
     sc = fmaxf(ldexpf(sc, e - 8), 0x1p-126f);
 }
 
+__device__ __forceinline__ float most(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
 // What a row tile's rows carry through the keys, a row per lane and its four lanes the same: the reference of their probabilities (its limit in
 // units of log2 here), and that of V's scales: a power of two, `unit`, that none of those a row has seen exceeds.  O is in multiples of it.
 struct RowState { float at = kNone, limit = kNone, unit = 0.f, inverse = 1.f; };
@@ -106,11 +108,12 @@ template <int CT, bool EVEN>
 __device__ __forceinline__ void quant_probabilities(const f32x4 (&z)[2], const float (&f2)[2], const f32x4 (&v)[2], RowState &st, f32x4 &lsum, f32x4 (&o)[CT],
                                                     frag_t &pf, frag_t &pv) {
     const float c0 = f2[0], c1 = f2[1];
-    float top = fmaxf(fmaxf(fmaxf(z[0][0], z[0][1]), fmaxf(z[0][2], z[0][3])) * c0, fmaxf(fmaxf(z[1][0], z[1][1]), fmaxf(z[1][2], z[1][3])) * c1);
-    float top_v = fmaxf(v[0][0], v[1][0]);
+    // (maxima that hand on a NaN, which the matrix cores' results need no instruction more for; a row with one is a NaN whatever its reference)
+    float top = most(most(most(z[0][0], z[0][1]), most(z[0][2], z[0][3])) * c0, most(most(z[1][0], z[1][1]), most(z[1][2], z[1][3])) * c1);
+    float top_v = most(v[0][0], v[1][0]);
     if (!EVEN)
 #pragma unroll
-        for (int e = 1; e < 4; e++) top_v = fmaxf(top_v, fmaxf(v[0][e], v[1][e]));
+        for (int e = 1; e < 4; e++) top_v = most(top_v, most(v[0][e], v[1][e]));
     if (__any((int)(top > st.limit) | (int)(top_v > st.unit))) {
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
