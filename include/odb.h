@@ -598,7 +598,7 @@ typedef struct {
  *   a = the largest magnitude of the new values;  s = a / M (M = 127 or 448), or the scale that is there if that is larger and other
  *   positions of the group below kv_len[r] stay;  codes of the new values = value / s to the nearest code, ties to even (value * M / a
  *   in 32 bits, so that the rounding of s moves no tie);  where s grows, codes that stay are rounded anew to it, else they are left alone.
- * A group whose values are all below 2^-100, with nothing that stays, has codes and scale zero.  Positions of the group that are not
+ * A group whose values are all below 2^-100, with nothing that stays, has codes and scale zero; a scale below 2^-110 counts as zero.  Positions of the group that are not
  * below kv_len[r] are left alone.  The same call again writes the same codes and scales.
  * Of values that are not finite, infinities become the largest code of their sign and no numbers become zero; they do not count for a,
  * and *odd is set to 1 (it is never cleared).

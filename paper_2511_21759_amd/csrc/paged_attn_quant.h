@@ -171,14 +171,18 @@ __device__ __forceinline__ void store_rounded8(const PagedAttn &a, int row, int 
 
 // ---- few rows: the waves of a workgroup split the keys -----------------------------------------------------------------
 
-// As paged_attn_kernel, in blocks of KB keys, so that a wave has as many bytes on their way as with 16-bit pages.  V's codes lie in LDS as
-// they come and are transposed as they are read (eight keys of a channel per lane).  EVEN: the 16 keys of a tile share their scales, which are
-// then scalars of the wave; else every key has its own.
+// As paged_attn_kernel, with blocks of 32 keys.  V's codes lie in LDS as they come and are transposed as they are read (eight keys of a channel
+// per lane).  EVEN: the 16 keys of a tile share their scales, which are then scalars of the wave; else every key has its own.
+// Bound by HBM with single tokens (two of 1.9e5 positions, 799 MB, 125 us = 6.4 TB/s; 48 of 24 to 13524, 379 MB, 67 us = 5.7), by the latency of a
+// block's loads where pairs are few: about 1.1 us a turn of a wave (one token of 800 / 2000 positions 12.5 / 21.8 us whole), 1.7 with 32 rows.
+// Blocks of 64 keys, which have as many bytes on their way as 16-bit pages, need 194 registers and were slower nearly everywhere (48 tokens 84 / 86 us, but
+// 32 of 1000 positions 19.3 / 15.9, 10 x 32 rows 52 / 35).
+// COST: places in the list for a pair beside its blocks; they pass at twice the rate of 16-bit ones (48 tokens: 86 us with 6, 84 with 12, 86 with 20).
 template <int DH>
 struct QuantShape {
-    static constexpr int SUB = 1, KB = 32 * SUB, SHIFT = SUB == 1 ? 5 : 6, COST = 12;
+    static constexpr int SHIFT = 5, COST = 12;
 };
-constexpr int kLeastQuantPiece = 12;             // places, of 32 keys
+constexpr int kLeastQuantPiece = 12;             // places
 
 // Where the 16-byte piece c of a key lies in a wave's codes of V: the reads of 16 neighbouring lanes' keys fall on different banks.
 template <int DH>
@@ -191,7 +195,7 @@ __device__ __forceinline__ constexpr int vq_piece(int key, int c) {
 template <int CODES, int DH, int NT, bool EVEN>
 __global__ __launch_bounds__(64 * NW, DH == 256 || NT == 4 ? 1 : 2) void quant_attn_kernel(PagedAttnQuant a) {
     typedef QuantShape<DH> Shape;
-    constexpr int SUB = Shape::SUB, KB = Shape::KB, SHIFT = Shape::SHIFT, T = 2 * SUB;      // 16-key tiles of a block
+    constexpr int KB = 32, SHIFT = Shape::SHIFT, T = 2;          // keys and 16-key tiles of a block
     constexpr int CH = DH / 64, KS = DH / 32, CT = DH / 16;      // loads of a tile of K or V per lane, k-steps of S, channel tiles of O
     constexpr int KEYS = 1024 / DH;                              // keys per load of V
     constexpr int OSTRIDE = DH + 4, WAVE_LDS = 16 * OSTRIDE * 4;
@@ -202,7 +206,7 @@ __global__ __launch_bounds__(64 * NW, DH == 256 || NT == 4 ? 1 : 2) void quant_a
 
     const int kv = a.pages.n_kv_heads, head = (int)(blockIdx.x % (unsigned)kv), x = (int)(blockIdx.x / (unsigned)kv);
     const bool split = a.split > 0;
-    auto piece_of = [&](long long total) { return max((long long)(kLeastQuantPiece / SUB), (total + a.split - 1) / max(a.split, 1)); };
+    auto piece_of = [&](long long total) { return max((long long)kLeastQuantPiece, (total + a.split - 1) / max(a.split, 1)); };
     Place pl;
     if (!find_place<SHIFT, Shape::COST, true>(a, TILE_ROWS, split, [&](long long total) { return split ? piece_of(total) * x : (long long)x; }, pl)) return;
 
@@ -327,7 +331,7 @@ __global__ __launch_bounds__(64 * NW, DH == 256 || NT == 4 ? 1 : 2) void quant_a
                         }
                     }
                     // scores of all keys and row tiles first, which frees the registers of K for the next block
-                    f32x4 z[SUB][NT][2];
+                    f32x4 z[NT][2];
 #pragma unroll
                     for (int tile = 0; tile < T; tile++) {
                         frag_t kf[KS];
@@ -342,7 +346,7 @@ __global__ __launch_bounds__(64 * NW, DH == 256 || NT == 4 ? 1 : 2) void quant_a
 #pragma unroll
                             for (int k = 0; k < KS; k++) y = mfma16(kf[k], q[t][k], y);
                             if (!EVEN) y *= ks[tile];
-                            z[tile >> 1][t][tile & 1] = y;
+                            z[t][tile] = y;
                         }
                     }
                     load_k(base, k_next);
@@ -363,10 +367,7 @@ __global__ __launch_bounds__(64 * NW, DH == 256 || NT == 4 ? 1 : 2) void quant_a
 #pragma unroll
                     for (int t = 0; t < T; t++)
 #pragma unroll
-                        for (int j = 0; j < CH; j++) {
-                            const int key = 16 * (t & 1) + j * KEYS + v_key;
-                            *reinterpret_cast<frag_t *>(mine + (t >> 1) * 32 * DH + 16 * vq_piece<DH>(key, v_ch)) = vr[t][j];
-                        }
+                        for (int j = 0; j < CH; j++) *reinterpret_cast<frag_t *>(mine + 16 * vq_piece<DH>(16 * t + j * KEYS + v_key, v_ch)) = vr[t][j];
                     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
                     load_v(base, v_next);
                     if (Code<CODES>::kOdd && __builtin_expect(dirty, 0)) {
@@ -374,9 +375,7 @@ __global__ __launch_bounds__(64 * NW, DH == 256 || NT == 4 ? 1 : 2) void quant_a
                         int dl = lane;
                         asm volatile("" : "+v"(dl));
                         for (int key = 0; key < KB; key++) {
-                            int page = pg[0];
-#pragma unroll
-                            for (int t = 1; t < T; t++) page = key >> 4 == t ? pg[t] : page;
+                            const int page = key & 16 ? pg[1] : pg[0];
 #pragma unroll
                             for (int t = 0; t < NT; t++) {
                                 const bool seen = sees(sight[t], key0 + key, page);
@@ -384,7 +383,7 @@ __global__ __launch_bounds__(64 * NW, DH == 256 || NT == 4 ? 1 : 2) void quant_a
                                 for (int c = 0; c < CT; c++)
 #pragma unroll
                                     for (int d = 0; d < 4; d++) {
-                                        const unsigned char w = mine[(key >> 5) * 32 * DH + 16 * vq_piece<DH>(key & 31, c) + 4 * (dl >> 4) + d];
+                                        const unsigned char w = mine[16 * vq_piece<DH>(key, c) + 4 * (dl >> 4) + d];
                                         if ((int)seen & (int)((w & 0x7f) == 0x7f)) o[t][c][d] = __builtin_nanf("");
                                     }
                             }
@@ -402,38 +401,34 @@ __global__ __launch_bounds__(64 * NW, DH == 256 || NT == 4 ? 1 : 2) void quant_a
                         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
                     }
 
+                    f32x4 v[2];
 #pragma unroll
-                    for (int sub = 0; sub < SUB; sub++) {
-                        const int key32 = key0 + 32 * sub;
-                        f32x4 v[2];
+                    for (int s = 0; s < 2; s++) v[s] = EVEN ? f32x4{cvs[s], 0.f, 0.f, 0.f} : vs[s];
+                    auto v_codes = [&](int c) {
+                        typedef int i32x2 __attribute__((ext_vector_type(2)));
+                        typedef __attribute__((address_space(3))) i32x2 *lds_ptr;
+                        const int r = li >> 1, key = (r & 3) + 4 * g + 4 * (r & 4);
+                        const i32x2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_ptr)(mine + 16 * vq_piece<DH>(key, c) + 8 * (li & 1)));
+                        return halves8<CODES>((uint32_t)w[0], (uint32_t)w[1]);
+                    };
+                    frag_t vt[NT > 1 ? CT : 1];                           // held for several row tiles
+                    if (NT > 1)
 #pragma unroll
-                        for (int s = 0; s < 2; s++) v[s] = EVEN ? f32x4{cvs[2 * sub + s], 0.f, 0.f, 0.f} : vs[2 * sub + s];
-                        auto v_codes = [&](int c) {
-                            typedef int i32x2 __attribute__((ext_vector_type(2)));
-                            typedef __attribute__((address_space(3))) i32x2 *lds_ptr;
-                            const int r = li >> 1, key = (r & 3) + 4 * g + 4 * (r & 4);
-                            const i32x2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_ptr)(mine + sub * 32 * DH + 16 * vq_piece<DH>(key, c) + 8 * (li & 1)));
-                            return halves8<CODES>((uint32_t)w[0], (uint32_t)w[1]);
-                        };
-                        frag_t vt[NT > 1 ? CT : 1];                           // held for several row tiles
-                        if (NT > 1)
+                        for (int c = 0; c < CT; c++) vt[NT > 1 ? c : 0] = v_codes(c);
 #pragma unroll
-                            for (int c = 0; c < CT; c++) vt[NT > 1 ? c : 0] = v_codes(c);
-#pragma unroll
-                        for (int t = 0; t < NT; t++) {
-                            f32x4 (&zt)[2] = z[sub][t];
-                            frag_t pf, pv;
-                            float c[2] = {EVEN ? sc[t] * cks[2 * sub] : sc[t], EVEN ? sc[t] * cks[2 * sub + 1] : sc[t]};
-                            f32x4 vt2[2] = {v[0], v[1]};
-                            if (!plain) {
-                                hide_unseen(zt, sight[t], key32, g, pg[2 * sub], pg[2 * sub + 1]);
-                                hide_scales<EVEN>(zt, c, vt2);
-                            }
-                            quant_probabilities<CT, EVEN>(zt, c, vt2, st[t], lsum[t], o[t], pf, pv);
-                            lsum[t] = mfma16(ones, pf, lsum[t]);
-#pragma unroll
-                            for (int c = 0; c < CT; c++) o[t][c] = mfma16(NT > 1 ? vt[NT > 1 ? c : 0] : v_codes(c), pv, o[t][c]);
+                    for (int t = 0; t < NT; t++) {
+                        f32x4 (&zt)[2] = z[t];
+                        frag_t pf, pv;
+                        float c[2] = {EVEN ? sc[t] * cks[0] : sc[t], EVEN ? sc[t] * cks[1] : sc[t]};
+                        f32x4 vt2[2] = {v[0], v[1]};
+                        if (!plain) {
+                            hide_unseen(zt, sight[t], key0, g, pg[0], pg[1]);
+                            hide_scales<EVEN>(zt, c, vt2);
                         }
+                        quant_probabilities<CT, EVEN>(zt, c, vt2, st[t], lsum[t], o[t], pf, pv);
+                        lsum[t] = mfma16(ones, pf, lsum[t]);
+#pragma unroll
+                        for (int c = 0; c < CT; c++) o[t][c] = mfma16(NT > 1 ? vt[NT > 1 ? c : 0] : v_codes(c), pv, o[t][c]);
                     }
                     if (!EVEN) load_scales(vsp, sbase, vs, more);
                     key0 = nkey;
@@ -521,9 +516,13 @@ __global__ __launch_bounds__(64 * NW, DH == 256 || NT == 4 ? 1 : 2) void quant_a
 
 // ---- many rows: the waves of a workgroup split the rows and share K and V in LDS ----------------------------------------
 
-constexpr int kMostShares = 16;
+constexpr int kMostShares = 16;          // parts of a tile that is cut
 
-// As paged_rows_kernel; codes become binary16 on their way to LDS, once for the four waves, and the keys' scales lie beside them.
+// As paged_rows_kernel; codes become binary16 on their way to LDS, once for the four waves, and the keys' scales lie beside them.  A lane converts sixteen
+// codes to two pieces beside each other and stores every second piece at once, which the swizzle is made for (PAIRS in k_piece and v_piece).
+// Bound by vector and matrix instructions together: 74 of the one and 17 of the other for a row tile and 32 keys, 38 more than with 16-bit pages:
+// 8 products and 4 conversions for p times V's scale, 8 conversions of codes, what the two references ask for.  Four requests of 4096 rows at 8192 positions, 32
+// heads over 8 of 128: 2.64 ms with E4M3 codes and scales of 64 positions (834 TFLOP/s), 2.83 with INT8 codes and a scale a position (777), 16-bit pages 2.33.
 template <int CODES, int DH, bool EVEN>
 __global__ __launch_bounds__(256, 2) void quant_rows_kernel(PagedAttnQuant a) {
     typedef RowsShape<DH> Shape;
