@@ -80,11 +80,12 @@ __device__ __forceinline__ Blocks blocks_of(const PagedAttn &a, int len, int pmi
     }
     Blocks b;
     constexpr int M = (1 << SHIFT) - 1;
-    const int last = hi > lo ? (hi + M) >> SHIFT : 0;
+    int last = hi > lo ? (hi + M) >> SHIFT : 0;
     b.from = hi > lo ? lo >> SHIFT : 0;
     const int stay = min(a.window ? a.sinks : 0, a.causal ? min(len, pmax + 1) : len);
     b.head = stay > 0 ? (stay + M) >> SHIFT : 0;
     if (last > b.from) {
+        last = max(last, b.head);                                // (positions that stay may reach beyond the window)
         b.head = min(b.head, b.from);
         b.count = b.head + last - b.from;
     } else {

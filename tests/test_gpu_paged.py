@@ -318,6 +318,17 @@ def test_many_rows_whose_keys_are_split_over_workgroups(cache, dim, heads, kv, c
     assert (out[280:] == 3.0).all()
 
 
+@pytest.mark.parametrize("cache,dim", [("f16", 64), ("bf16", 128), ("f16", 256)])
+@pytest.mark.parametrize("window,sinks", [(1, 50), (3, 700), (40, 45), (64, 2000)])
+def test_positions_that_stay_visible_beyond_the_window(cache, dim, window, sinks):
+    """... which, where rows see what lies behind them, are not the first of what a row sees: single tokens, few rows, keys split over workgroups, many
+    rows, pieces of them."""
+    for heads, kv, rows, lens, first, columns in ((4, 2, [1, 1, 5], [300, 40, 1000], [2, 39, 100], 1), (6, 2, [5, 1, 33], [40, 17, 2300], [0, 3, 9], 300),
+                                                  (40, 40, [220, 130, 3], [220, 1000, 60], [0, 200, 1], 1), (16, 16, [150, 129], [3500, 9000], [7, 400], 1)):
+        rq = Requests(dim + window + sum(rows), rows, lens, heads, kv, dim, cache, 16, extra_columns=columns)
+        rq.check(rq.run(first=first, causal=False, window=window, sinks=sinks), first=first, window=window, sinks=sinks, oracle=plain.attention_many)
+
+
 @pytest.mark.parametrize("cache,dim,heads,kv,rows,lens", [
     ("f16", 64, 32, 32, [66, 100, 1, 0, 70, 99, 80, 65, 91], [900, 101, 1, 40, 70, 0, 333, 640, 257]),                     # whole tiles
     ("bf16", 128, 96, 32, [23, 33, 1, 42, 30, 24, 29, 1, 36], [900, 101, 1, 40, 70, 0, 333, 640, 257]),

@@ -161,6 +161,17 @@ def test_many_rows_whose_keys_are_split_over_workgroups(dtype, dim, heads, kv, k
     assert (out[280:] == 3.0).all()
 
 
+@pytest.mark.parametrize("dtype,dim,kind,group", [("f16", 64, "int8", 16), ("bf16", 128, "e4m3", 1), ("f16", 256, "e4m3", 16)])
+@pytest.mark.parametrize("window,sinks", [(1, 50), (3, 700), (40, 45), (64, 2000)])
+def test_positions_that_stay_visible_beyond_the_window(dtype, dim, kind, group, window, sinks):
+    """... which, where rows see what lies behind them, are not the first of what a row sees: single tokens, few rows, keys split over workgroups, many
+    rows, pieces of them."""
+    for heads, kv, rows, lens, first, columns in ((4, 2, [1, 1, 5], [300, 40, 1000], [2, 39, 100], 1), (6, 2, [5, 1, 33], [40, 17, 2300], [0, 3, 9], 300),
+                                                  (40, 40, [220, 130, 3], [220, 1000, 60], [0, 200, 1], 1), (16, 16, [150, 129], [3500, 9000], [7, 400], 1)):
+        rq = Requests(dim + window + sum(rows), rows, lens, heads, kv, dim, dtype, kind, group, 16, extra_columns=columns)
+        rq.check(rq.run(first=first, causal=False, window=window, sinks=sinks), first=first, window=window, sinks=sinks, oracle=plain.attention_many)
+
+
 @pytest.mark.parametrize("kind,group", KINDS)
 @pytest.mark.parametrize("causal,window,sinks", [(False, 0, 0), (True, 0, 0), (True, 9, 2), (False, 9, 2)])
 def test_rows_at_given_positions(kind, group, causal, window, sinks):
