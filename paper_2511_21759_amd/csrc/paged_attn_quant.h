@@ -129,7 +129,9 @@ __device__ __forceinline__ void quant_probabilities(const f32x4 (&z)[2], const f
         float f = __builtin_amdgcn_exp2f(st.at - up);
         lsum *= f;
         if (top_v > st.unit) {
-            const int e = __builtin_amdgcn_frexp_expf(fminf(top_v, 0x1p125f)) + 1;            // (some room above: scales differ)
+            // (some room above: scales differ.  From 2^-124 to 2^127, so that the unit and its inverse are both numbers for subnormal scales too: an
+            // inverse of infinity times the unit of nought that a row begins with would be no number)
+            const int e = __builtin_amdgcn_frexp_expf(fminf(fmaxf(top_v, 0x1p-126f), 0x1p125f)) + 1;
             st.inverse = ldexpf(1.0f, -e);
             f *= st.unit * st.inverse;
             st.unit = ldexpf(1.0f, e);

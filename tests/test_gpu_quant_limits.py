@@ -1,0 +1,35 @@
+"""Attention over pages of 8-bit codes at the ends of what scales and queries can be, on every way that sizes lead to.  Tolerances are those of
+test_gpu_quant_attention.py."""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import paged_plain as plain                                          # noqa: E402
+from test_gpu_quant_attention import KINDS, Requests                 # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+# heads, K/V heads, rows, lengths, further columns of the tables: single tokens, few rows, keys split over workgroups, many rows, pieces of them
+WAYS = [(8, 2, [1, 1, 1], [100, 33, 700], 1), (6, 2, [5, 33], [90, 333], 1), (8, 2, [1, 1], [5000, 900], 3), (6, 2, [9, 40], [2300, 601], 300),
+        (64, 64, [260, 131], [301, 131], 1), (16, 16, [150, 129], [3500, 9000], 1)]
+
+
+@pytest.mark.parametrize("heads,kv,rows,lens,columns", WAYS)
+@pytest.mark.parametrize("dtype,dim", [("f16", 64), ("bf16", 128), ("bf16", 256)])
+@pytest.mark.parametrize("kind,group", KINDS)
+def test_scales_of_v_below_the_smallest_normal_number(kind, group, dtype, dim, heads, kv, rows, lens, columns):
+    """The first scales of V that a row sees are subnormal: whatever follows, and where nothing does, results are numbers.  (The unit of probabilities times
+    scales is then 2^-124: a key's part of a row is off by 2^-157 of its code, below the last place of any result.)"""
+    rq = Requests(dim + sum(rows) + group, rows, lens, heads, kv, dim, dtype, kind, group, 32, extra_columns=columns)
+    v_scale = rq.scales[1]
+    for r, first in enumerate((2.0 ** -140, 2.0 ** -149, 2.0 ** -130)[:len(rows)]):
+        pages = rq.tables[r, :-(-lens[r] // 32)]
+        v_scale[pages[0]] = first
+        if len(pages) > 2:
+            v_scale[pages[1]] = 1.5 * 2.0 ** -127
+            v_scale[pages[2]] = 0.0
+    first = [0] * len(rows) if rows[0] == 260 else None                     # (rows that see nothing else)
+    rq.check(rq.run(causal=True, first=first), causal=True, first=first, oracle=plain.attention_many)
+    for r in range(len(rows)):
+        v_scale[rq.tables[r, :-(-lens[r] // 32)]] = 2.0 ** -130
+    rq.check(rq.run(causal=False), causal=False, oracle=plain.attention_many)
