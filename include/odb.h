@@ -641,7 +641,7 @@ int odb_paged_read_quant(const odb_quant_pages *pages, const int32_t *slots, int
  * Queries meet the codes in binary16, which holds every code (bfloat16 queries as multiples of a power of two of their row's largest, within
  * 2^-33 of it), probabilities times V's scales are rounded to binary16; scores and sums are 32-bit.  A position adds to a row to within 2^-31 of
  * the largest value that V's scales in its sight can stand for (a scale of 2^-126 at least), beside the relative roundings.  V's scales that are
- * visible have to be below 2^127, K's times scale * log2(e) finite in 32 bits.  The largest score that a row sees, times
+ * visible have to be below 2^127, K's below 2^64 and times scale * log2(e) finite in 32 bits.  The largest score that a row sees, times
  * scale * log2(e), has to stay below 2^27 in magnitude (the results of a row where it does not are no numbers). */
 int odb_paged_attention_quant(const odb_attention *a, const odb_quant_pages *pages, void *stream);
 long long odb_paged_attention_quant_workspace(const odb_attention *a, const odb_quant_pages *pages);

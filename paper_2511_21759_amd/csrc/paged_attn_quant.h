@@ -54,7 +54,8 @@ constexpr float kQuantBeyond = 1 << 27;          // scores times their scales ar
 __device__ __forceinline__ float checked_quant_sum(float at, float sum) { return fabsf(at) >= kQuantBeyond && at != kNone ? __builtin_bit_cast(float, -1) : sum; }
 
 // Queries of a lane's row in operand order, binary16, and the factor of its scores.  bfloat16 has another range: the row is taken as
-// multiples of 2^(e - 8), 2^e beyond its largest magnitude, in which its own eight bits are kept down to 2^-22 of that.
+// multiples of 2^(e - 9), 2^e beyond its largest magnitude, which is 2^8 or more in them: its own eight bits are kept down to 2^-23 of 2^e, and
+// below, half of binary16's smallest number, 2^-25, is within 2^-33 of the largest.
 // PAIRS: the channels of two k-steps are those of 64 in the order in which a lane loads codes, sixteen at once.
 template <int DH, bool PAIRS>
 __device__ __forceinline__ void load_queries(const PagedAttn &a, const u16 *src, int g, frag_t (&q)[DH / 32], float &sc) {
@@ -74,8 +75,8 @@ __device__ __forceinline__ void load_queries(const PagedAttn &a, const u16 *src,
     for (int k = 0; k < DH / 32; k++)
 #pragma unroll
         for (int w = 0; w < 4; w++)
-            q[k].w[w] = Num<_Float16>::pack(ldexpf(bf2f((u16)q[k].w[w]), 8 - e), ldexpf(bf2f((u16)(q[k].w[w] >> 16)), 8 - e));
-    sc = fmaxf(ldexpf(sc, e - 8), 0x1p-126f);
+            q[k].w[w] = Num<_Float16>::pack(ldexpf(bf2f((u16)q[k].w[w]), 9 - e), ldexpf(bf2f((u16)(q[k].w[w] >> 16)), 9 - e));
+    sc = fmaxf(ldexpf(sc, e - 9), 0x1p-126f);
 }
 
 __device__ __forceinline__ float most(float a, float b) { return __builtin_elementwise_maximum(a, b); }

@@ -5,7 +5,8 @@ import pytest
 torch = pytest.importorskip("torch")
 
 import paged_plain as plain                                          # noqa: E402
-from test_gpu_quant_attention import KINDS, Requests                 # noqa: E402
+import quant_plain as quant                                          # noqa: E402
+from test_gpu_quant_attention import F, KINDS, U16, Requests         # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -33,3 +34,26 @@ def test_scales_of_v_below_the_smallest_normal_number(kind, group, dtype, dim, h
     for r in range(len(rows)):
         v_scale[rq.tables[r, :-(-lens[r] // 32)]] = 2.0 ** -130
     rq.check(rq.run(causal=False), causal=False, oracle=plain.attention_many)
+
+
+@pytest.mark.parametrize("heads,kv,rows,lens,columns", WAYS)
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("kind,group", KINDS)
+def test_small_channels_of_bfloat16_queries(kind, group, dim, heads, kv, rows, lens, columns):
+    """bfloat16 queries are kept within 2^-33 of their row's largest: multiples of 2^-32 beside a channel of 1.5, which alone meet codes that are not zero, are
+    whole multiples of binary16's smallest number then, and come through exactly."""
+    rq = Requests(dim + sum(rows) + group, rows, lens, heads, kv, dim, "bf16", kind, group, 32, extra_columns=columns)
+    odd = torch.randint(-4, 4, rq.q.shape, generator=rq.g) * 2 + 1
+    rq.q = (odd * 2.0 ** -32).bfloat16()
+    rq.q[..., 0] = 1.5
+    rq.codes[0].view(torch.int8)[..., 0] = 0
+    rq.scales[0] = torch.where(rq.scales[0].isnan(), rq.scales[0], 2.0 ** 26 / quant.MOST[kind])
+    scale = 2.0 ** 4 * dim ** -0.5
+    got, (k, v), u = rq.run(causal=True, scale=scale).cpu().double(), rq.values(), 2.0 ** -8
+    want, size, big = plain.attention_many(rq.q.double(), k, v, rq.tables, lens, rows, None, scale, True, 0, 0)
+    assert 0.5 < big.max() < 2.0 ** 6                                       # (scores that tell whether the channels were there)
+    n = max(lens)
+    # as Requests.check, whose part for what queries lose is nought here
+    off = U16 + (dim + 6) * F * big[..., None] + 10 * F + n * F / 4 + n * 2.0 ** -33
+    bound = 2 * off * size * (1 + 4 * off) + n * 2.0 ** -31 * v[v.isfinite()].abs().max() + u * want.abs() * (1 + u) + torch.finfo(torch.bfloat16).tiny
+    assert ((got - want).abs() <= bound).all(), ((got - want).abs() / bound).max().item()
