@@ -4,6 +4,10 @@ Every function has the name of the C entry point it calls.  Device buffers are
 torch CUDA tensors (PyTorch-ROCm is the device allocator and stream provider);
 all arithmetic happens inside libodb.so.  There is no fallback: if the library
 has not been built, or a call fails, an exception is raised.
+
+Three calls of 8-bit pages, whose latency counts, are packed and made by
+_marshal (csrc/marshal.cpp), an extension of this Python and torch that is
+loaded with the first of them; the others need libodb.so alone.
 """
 from __future__ import annotations
 
@@ -192,29 +196,31 @@ def lib() -> ctypes.CDLL:
     L.odb_strerror.restype = ctypes.c_char_p
     L.odb_last_error.restype = ctypes.c_char_p
     _lib = L
-    _entries()
     return L
 
 
-_marshal = None
-_store_at = _read_at = _attention_at = _workspace_at = 0
+_calls = None           # (library, _marshal, addresses of the library's store, read, attention and workspace)
 
 
 def _entries():
     """Loads _marshal, which makes the calls of 8-bit pages whose tensors are as described (None from it: this file's own path goes through
-    them again, and says what is wrong), and notes the entry points' addresses for it."""
-    global _marshal, _store_at, _read_at, _attention_at, _workspace_at
-    from . import _marshal
-    _store_at, _read_at, _attention_at, _workspace_at = (ctypes.cast(f, ctypes.c_void_p).value for f in (
-        _lib.odb_qk_norm_rope_quant, _lib.odb_paged_read_quant, _lib.odb_paged_attention_quant, _lib.odb_paged_attention_quant_workspace))
+    them again, and says what is wrong), and notes the entry points' addresses for it.  Published as a whole: other threads may look."""
+    global _calls
+    L = lib()
+    try:
+        from . import _marshal
+    except ImportError as e:
+        raise OdbError("_marshal.so cannot be loaded (%s): build it with `python -m paper_2511_21759_amd.build`" % e) from None
+    _calls = (L, _marshal, *(ctypes.cast(f, ctypes.c_void_p).value for f in (
+        L.odb_qk_norm_rope_quant, L.odb_paged_read_quant, L.odb_paged_attention_quant, L.odb_paged_attention_quant_workspace)))
 
 
 def _here(index):
-    """The current stream of device `index` if that is the current device, else None."""
-    if _lib is None:
-        lib()
+    """The current stream of device `index` if that is the current device, and _calls are those of the open library; else None."""
     if index < 0 or _torch.cuda.current_device() != index:
         return None
+    if _calls is None or _calls[0] is not _lib:
+        _entries()
     return _raw_stream(index) if _raw_stream is not None else _stream()
 
 
@@ -746,7 +752,8 @@ def odb_qk_norm_rope_quant(q, k, v, k_pages, v_pages, k_scale, v_scale, table, p
         raise TypeError("queries become float16 or bfloat16: give dtype")
     stream = _here(index)
     if stream is not None:
-        got = _marshal.store(_store_at, stream, index, q, k, v, k_pages, v_pages, k_scale, v_scale, table, positions, tables, kv_len, cu_rows, first_pos,
+        calls = _calls
+        got = calls[1].store(calls[2], stream, index, q, k, v, k_pages, v_pages, k_scale, v_scale, table, positions, tables, kv_len, cu_rows, first_pos,
                              q_gain, k_gain, eps, interleaved, dtype is torch.bfloat16, out, odd)
         if got is not None:
             return _made(got)
@@ -790,7 +797,8 @@ def odb_paged_read_quant(k_pages, v_pages, k_scale, v_scale, slots, dtype=None, 
     index = slots.get_device()
     stream = _here(index)
     if stream is not None and out is None:
-        got = _marshal.read(_read_at, stream, index, k_pages, v_pages, k_scale, v_scale, slots, _DTYPES.get(dtype, -1) if dtype is not None else 0)
+        calls = _calls
+        got = calls[1].read(calls[3], stream, index, k_pages, v_pages, k_scale, v_scale, slots, _DTYPES.get(dtype, -1) if dtype is not None else 0)
         if got is not None:
             return _made(got)
     pages = _quant_pages(k_pages, v_pages, k_scale, v_scale, index)
@@ -831,7 +839,8 @@ def odb_paged_attention_quant(q, k_pages, v_pages, k_scale, v_scale, tables, kv_
     index = q.get_device()
     stream = _here(index)
     if stream is not None:
-        got = _marshal.attention(_attention_at, _workspace_at, stream, index, q, k_pages, v_pages, k_scale, v_scale, tables, kv_len, cu_rows, first_pos,
+        calls = _calls
+        got = calls[1].attention(calls[4], calls[5], stream, index, q, k_pages, v_pages, k_scale, v_scale, tables, kv_len, cu_rows, first_pos,
                                  k_pages.shape[3] ** -0.5 if scale is None else scale, causal, window, sinks, max_rows, max_len, out, workspace)
         if got is not None:
             return _made(got)
