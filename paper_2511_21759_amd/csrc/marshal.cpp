@@ -81,6 +81,13 @@ bool pages_of(Args &x, int i, int dtype, odb_quant_pages &p) {
 
 Tensor empty_like(const Tensor &q, at::IntArrayRef shape, at::ScalarType type) { return at::empty(shape, q.options().dtype(type).requires_grad(false)); }
 
+// Other threads of Python run while memory is found and the call is made, which may wait for room in a queue.  (Tensors that are arguments stay: the
+// caller holds them.)
+struct Unlocked {
+    PyThreadState *state = PyEval_SaveThread();
+    ~Unlocked() { PyEval_RestoreThread(state); }
+};
+
 // the results, or the entry's error code
 template <class F>
 PyObject *finish(int rc, F results) { return rc ? PyLong_FromLong(rc) : results(); }
@@ -115,18 +122,24 @@ PyObject *store(PyObject *, PyObject *const *a, Py_ssize_t n) try {
     r.odd = (int32_t *)x.ints(odd, 1);
     if (out) r.q_out_row = x.rows(out, type, rows, heads, dim);
     if (!x.good) Py_RETURN_NONE;
-    Tensor made;
-    if (!out) {
-        made = empty_like(*q, {rows, heads, dim}, type);
-        r.q_out_row = heads * dim;
-        out = &made;
-    }
-    r.q = q->data_ptr(); r.k = k->data_ptr(); r.v = v->data_ptr(); r.q_out = out->data_ptr();
+    r.q = q->data_ptr(); r.k = k->data_ptr(); r.v = v->data_ptr();
     r.in_dtype = code_of(given); r.rows = (int)rows; r.n_heads = (int)heads;
     r.q_gain = qg ? (const float *)qg->data_ptr() : nullptr; r.k_gain = kg ? (const float *)kg->data_ptr() : nullptr;
     r.table = (const float *)table->data_ptr(); r.n_pos = (int)table->size(0); r.rot_dim = 2 * (int)table->size(1); r.interleaved = x.truth(19);
     r.columns = (int)columns; r.n = (int)reqs;
-    return finish(((store_entry)entry)(&r, &p, (void *)stream), [&] {
+    Tensor made;
+    int rc;
+    {
+        Unlocked other_threads;
+        if (!out) {
+            made = empty_like(*q, {rows, heads, dim}, type);
+            r.q_out_row = heads * dim;
+            out = &made;
+        }
+        r.q_out = out->data_ptr();
+        rc = ((store_entry)entry)(&r, &p, (void *)stream);
+    }
+    return finish(rc, [&] {
         if (made.defined()) return THPVariable_Wrap(made);
         Py_INCREF(a[21]);
         return a[21];
@@ -150,8 +163,15 @@ PyObject *read(PyObject *, PyObject *const *a, Py_ssize_t n) try {
     if (!x.good || rows < 1 || rows > INT_MAX) Py_RETURN_NONE;
     const at::ScalarType type = dtype == ODB_F16 ? at::kHalf : dtype == ODB_BF16 ? at::kBFloat16 : at::kFloat;
     const int64_t row = (int64_t)p.n_kv_heads * p.head_dim;
-    const Tensor k = empty_like(*slots, {rows, p.n_kv_heads, p.head_dim}, type), v = empty_like(*slots, {rows, p.n_kv_heads, p.head_dim}, type);
-    return finish(((read_entry)entry)(&p, at, (int)rows, dtype, k.data_ptr(), v.data_ptr(), row, row, (void *)stream), [&]() -> PyObject * {
+    Tensor k, v;
+    int rc;
+    {
+        Unlocked other_threads;
+        k = empty_like(*slots, {rows, p.n_kv_heads, p.head_dim}, type);
+        v = empty_like(*slots, {rows, p.n_kv_heads, p.head_dim}, type);
+        rc = ((read_entry)entry)(&p, at, (int)rows, dtype, k.data_ptr(), v.data_ptr(), row, row, (void *)stream);
+    }
+    return finish(rc, [&]() -> PyObject * {
         PyObject *pair = PyTuple_New(2);
         if (!pair) return nullptr;
         PyTuple_SET_ITEM(pair, 0, THPVariable_Wrap(k));
@@ -187,23 +207,29 @@ PyObject *attention(PyObject *, PyObject *const *a, Py_ssize_t n) try {
     if (work && (work->scalar_type() != at::kByte || work->get_device() != x.device || !work->is_contiguous())) Py_RETURN_NONE;
     if (!x.good) Py_RETURN_NONE;
     r.columns = (int)columns; r.n = (int)reqs; r.rows = (int)rows; r.n_heads = (int)heads;
-    Tensor made, room;
-    if (!out) {
-        made = empty_like(*q, {rows, heads, dim}, type);
-        out = &made;
-    }
-    r.q = q->data_ptr(); r.out = out->data_ptr();
+    r.q = q->data_ptr();
     const long long need = ((workspace_entry)space)(&r, &p);
     if (need < 0) return PyLong_FromLongLong(need);
-    if (need > 0) {
-        if (!work) {
-            room = empty_like(*q, {need}, at::kByte);
-            work = &room;
+    Tensor made, room;
+    int rc;
+    {
+        Unlocked other_threads;
+        if (!out) {
+            made = empty_like(*q, {rows, heads, dim}, type);
+            out = &made;
         }
-        r.workspace = work->data_ptr();
-        r.workspace_bytes = (size_t)work->numel();
+        r.out = out->data_ptr();
+        if (need > 0) {
+            if (!work) {
+                room = empty_like(*q, {need}, at::kByte);
+                work = &room;
+            }
+            r.workspace = work->data_ptr();
+            r.workspace_bytes = (size_t)work->numel();
+        }
+        rc = ((attention_entry)entry)(&r, &p, (void *)stream);
     }
-    return finish(((attention_entry)entry)(&r, &p, (void *)stream), [&] {
+    return finish(rc, [&] {
         if (made.defined()) return THPVariable_Wrap(made);
         Py_INCREF(a[19]);
         return a[19];
