@@ -40,7 +40,11 @@ struct Args {
         if (x == -1.0 && PyErr_Occurred()) { PyErr_Clear(); good = false; }
         return x;
     }
-    bool truth(int i) { return PyObject_IsTrue(a[i]) == 1; }
+    bool truth(int i) {
+        const int x = PyObject_IsTrue(a[i]);
+        if (x < 0) { PyErr_Clear(); good = false; }
+        return x == 1;
+    }
     const int32_t *ints(const Tensor *t, int64_t n, int64_t m = -1) {
         if (!t) return nullptr;
         if (t->scalar_type() != at::kInt || t->get_device() != device || !t->is_contiguous() || t->dim() != (m < 0 ? 1 : 2) || t->size(0) != n || (m >= 0 && t->size(1) != m))
@@ -114,6 +118,7 @@ PyObject *store(PyObject *, PyObject *const *a, Py_ssize_t n) try {
     r.k_row = x.rows(k, given, rows, p.n_kv_heads, dim);
     r.v_row = x.rows(v, given, rows, p.n_kv_heads, dim);
     r.eps = (float)x.real(18);
+    r.interleaved = x.truth(19);
     r.positions = x.ints(positions, rows);
     r.cu_rows = x.ints(cu, reqs + 1);
     r.first_pos = x.ints(first, reqs);
@@ -125,7 +130,7 @@ PyObject *store(PyObject *, PyObject *const *a, Py_ssize_t n) try {
     r.q = q->data_ptr(); r.k = k->data_ptr(); r.v = v->data_ptr();
     r.in_dtype = code_of(given); r.rows = (int)rows; r.n_heads = (int)heads;
     r.q_gain = qg ? (const float *)qg->data_ptr() : nullptr; r.k_gain = kg ? (const float *)kg->data_ptr() : nullptr;
-    r.table = (const float *)table->data_ptr(); r.n_pos = (int)table->size(0); r.rot_dim = 2 * (int)table->size(1); r.interleaved = x.truth(19);
+    r.table = (const float *)table->data_ptr(); r.n_pos = (int)table->size(0); r.rot_dim = 2 * (int)table->size(1);
     r.columns = (int)columns; r.n = (int)reqs;
     Tensor made;
     int rc;

@@ -123,3 +123,24 @@ def test_other_threads_run_while_an_entry_point_waits(stub, name):
     assert not isinstance(got, int), "the entry point waited in vain"
     shapes = [tuple(t.shape) for t in (got if isinstance(got, tuple) else (got,))]
     assert shapes == {"store": [(3, 4, 64)], "attend": [(3, 4, 64)], "read": [(3, 2, 64)] * 2}[name]
+
+
+def test_what_has_no_truth_value_is_left_to_the_bindings_own_path(stub):
+    """... which names the error: no call is made, and no exception is left behind."""
+    call, none = Call(stub), torch.zeros(2)
+    for name in ("store", "attend"):
+        stub.set(1)
+        assert getattr(call, name)(none) is None and not stub.inside()
+        assert getattr(call, name)(torch.ones(1)) is not None and stub.inside()
+
+
+@pytest.mark.gpu
+def test_what_has_no_truth_value_is_refused():
+    i32, none = torch.int32, torch.zeros(2)
+    pools = [torch.zeros(5, 2, 32, 64, dtype=torch.int8, device="cuda") for _ in range(2)] + [torch.zeros(5, 2, 2, device="cuda") for _ in range(2)]
+    q = torch.zeros(2, 4, 64, dtype=torch.float16, device="cuda")
+    requests = torch.zeros(2, 4, dtype=i32, device="cuda"), torch.ones(2, dtype=i32, device="cuda")
+    with pytest.raises(RuntimeError, match="ambiguous"):
+        B.odb_paged_attention_quant(q, *pools, *requests, causal=none)
+    with pytest.raises(RuntimeError, match="ambiguous"):
+        B.odb_qk_norm_rope_quant(q, q[:, :2], q[:, 2:], *pools, B.odb_rope_table(64, 64, 10000.0), torch.zeros(2, dtype=i32, device="cuda"), *requests, interleaved=none)
