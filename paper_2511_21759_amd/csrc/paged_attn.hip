@@ -789,8 +789,9 @@ void paged_attn_plan(const odb_pages &p, int n, int rows, int group, int max_row
 // Half the bytes a key, and whole tiles of up to 64 requests are given out longest first.  nt and the shape of many rows in few tiles as above; else:
 // Many rows with a tile for every CU: whole, however ragged (whole, longest first / pieces / whole in order of the requests: four pieces of
 // prompts, 727 to 1449 rows of 2694 to 5995 positions, 304 / 321 / 392 us).  Where a last round of workgroups would hold a few tiles only,
-// these are cut, which costs a join (three of 503 to 997 rows under a window of 900, 526 tiles and 512 workgroups at once: 83 / 107 us
-// uncut; four pieces, two full rounds: 319 / 304).
+// these are cut, which costs a join and its workspace (three of 503 to 997 rows under a window of 900, 526 tiles and 512 workgroups at once: 83 / 107 us
+// uncut; four pieces, two full rounds: 319 / 304).  Full rounds have nothing to cut (2048 rows of as many positions 79 us, 86 with the join; 4096 203,
+// 218; 8192 688, 716).
 // Few rows: cuts for two workgroups a CU with 32 rows too (8 x 32 rows of 500 to 3000, 32 heads over 32: 45 us, one 53); whole where
 // the keys are up to 1536 and the pairs enough (10 x 32 rows of 454 to 1364: 24 / 31 us in pieces).
 void paged_attn_quant_plan(const odb_pages &p, int n, int rows, int group, int max_rows, long long max_len, long long columns, int *nt, int *split,
@@ -806,7 +807,7 @@ void paged_attn_quant_plan(const odb_pages &p, int n, int rows, int group, int m
         *items = numbers;
         const int at_once = (512 + p.n_kv_heads - 1) / p.n_kv_heads;
         const long long over = tiles % at_once;
-        if (n <= 64 && full >= at_once && full / at_once == tiles / at_once && 2 * over <= at_once && tiles <= 4ll * at_once) {
+        if (n <= 64 && full >= at_once && full / at_once == tiles / at_once && over > 0 && 2 * over <= at_once && tiles <= 4ll * at_once) {
             *slots = *split = at_once;
             *items = (n < rows ? n : rows) + full + at_once;                   // (of all tiles that there can be: max_rows may not hold)
         }
