@@ -1,0 +1,146 @@
+"""Attention over 8-bit pages where the row tiles of a last round are cut and joined, against 64 bits.  Which tiles are cut, and in how many parts, is worked out
+here once more, so that a call that cuts none fails."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2511_21759_amd import binding as B                        # noqa: E402
+from test_gpu_quant_attention import Requests, ints                  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+
+def up(x, y):
+    return -(-x // y)
+
+
+def stages(keys, length, pmin, pmax, causal, window, sinks):
+    """Stages of `keys` keys that rows at positions pmin .. pmax see together."""
+    seen = set()
+    for s in range(up(length, keys)):
+        a, b = s * keys, min(s * keys + keys, length) - 1                # first and last position of the stage
+        if causal and a > pmax:
+            continue
+        if not window or (b > pmin - window and a < pmax + window) or a < sinks:
+            seen.add(s)
+    return max(1, len(seen))
+
+
+def parts_of_cut_tiles(rows, lens, first, group, kv, dim, causal, window, sinks):
+    """Parts of each tile of the last round, none if it is not cut: longest request first, its last rows first, 512 / kv tiles at a time."""
+    tile_rows, keys = (64, 32) if dim == 256 else (128, 64)
+    at_once, full, n = up(512, kv), sum(rows) * group // tile_rows, len(rows)
+    most = min(min(n, sum(rows)) + full, n * up(max(rows) * group, tile_rows))           # (what the host knows)
+    if not (full >= at_once and full // at_once == most // at_once and 0 < 2 * (most % at_once) <= at_once and most <= 4 * at_once and most * kv >= 256):
+        return []
+    tiles = []
+    for r in sorted(range(n), key=lambda r: (-lens[r], r)):
+        for t in reversed(range(up(rows[r] * group, tile_rows))):
+            lo, hi = first[r] + t * tile_rows // group, first[r] + min(((t + 1) * tile_rows - 1) // group, rows[r] - 1)
+            tiles.append(stages(keys, lens[r], lo, hi, causal, window, sinks))
+    over = len(tiles) % at_once
+    return [min(16, at_once // over, max(1, s // 4)) for s in tiles[len(tiles) - over:]] if over else []
+
+
+def oracle(q, k_pages, v_pages, tables, kv_len, rows, first, scale, causal, window, sinks):
+    """As plain.attention_many, where pages may be missing too."""
+    n_pages, _, page, dim = k_pages.shape
+    group = q.shape[1] // k_pages.shape[1]
+    out, size, big = torch.zeros_like(q), torch.zeros_like(q), torch.zeros(q.shape[:2], dtype=torch.float64)
+    row = 0
+    for r, m in enumerate(rows):
+        length = kv_len[r]
+        if m == 0 or length <= 0:
+            row += m
+            continue
+        p, key = (first[r] + torch.arange(m))[:, None], torch.arange(length)[None, :]
+        ids = torch.tensor(tables[r, :up(length, page)].astype(np.int64))
+        there = (ids >= 0) & (ids < n_pages)
+        seen = there.repeat_interleave(page)[:length].expand(m, length).clone()
+        if causal:
+            seen &= key <= p
+        if window:
+            seen &= ((p - key).abs() < window) | (key < sinks)
+        for h in range(q.shape[1]):
+            k, v = (torch.where(there[:, None, None], x[ids.clamp(0, n_pages - 1), h // group], 0.0).reshape(-1, dim)[:length] for x in (k_pages, v_pages))
+            x = q[row:row + m, h]
+            z = torch.softmax((x @ k.t() * scale).masked_fill(~seen, float("-inf")), -1).nan_to_num(0.0)
+            out[row:row + m, h], size[row:row + m, h] = z @ v, z @ v.abs()
+            big[row:row + m, h] = (x.abs() @ k.abs().t()).masked_fill(~seen, 0.0).amax(-1) * scale
+        row += m
+    return out, size, big
+
+
+# 64 heads over 64, so that eight tiles of 128 rows run at once (heads of 256: of 64 rows, of requests half as long).  The last two tiles are those of one request;
+# of two, one in parts and one whole; one request's first rows in many parts; beside a request without rows.
+SHAPES = {"two": ([600, 300, 200], [1500, 1100, 900]), "one": ([300, 100, 700], [1100, 300, 1500]), "alone": ([1100], [1900]), "empty": ([560, 0, 540], [900, 90, 980])}
+
+
+def make(shape, dtype, dim, kind, group, heads=64, kv=64, page=64):
+    rows, lens = SHAPES[shape]
+    if dim == 256:
+        rows, lens = [x // 2 for x in rows], [x // 2 for x in lens]
+    rq = Requests(dim + sum(rows), rows, lens, heads, kv, dim, dtype, kind, group, page)
+    return rq, rows, lens, [length - m for m, length in zip(rows, lens)]
+
+
+@pytest.mark.parametrize("shape", ["two", "one", "alone", "empty"])
+@pytest.mark.parametrize("dtype,dim,kind,group", [("f16", 64, "int8", 1), ("bf16", 128, "e4m3", 16), ("f16", 128, "e4m3", 1), ("bf16", 256, "int8", 64), ("f16", 256, "e4m3", 1),
+                                                  ("bf16", 64, "e4m3", 64)])
+@pytest.mark.parametrize("causal,window,sinks", [(False, 0, 0), (True, 0, 0), (True, 700, 70), (False, 400, 3)])
+def test_cut_tiles(shape, dtype, dim, kind, group, causal, window, sinks):
+    rq, rows, lens, first = make(shape, dtype, dim, kind, group)
+    parts = parts_of_cut_tiles(rows, lens, first, 1, 64, dim, causal, window, sinks)
+    assert max(parts) > 1 and (shape != "one" or min(parts) == 1), parts
+    out = torch.full((sum(rows) + 5, 64, dim), 3.0, dtype=rq.q.dtype, device="cuda")     # rows that belong to no request stay
+    q = torch.cat([rq.q, rq.q[:5]]).cuda()
+    args = [t.cuda() for t in rq.codes + rq.scales] + [ints(rq.tables), ints(rq.lens)]
+    B.odb_paged_attention_quant(q, *args, causal=causal, window=window, sinks=sinks, cu_rows=ints(np.r_[0, np.cumsum(rows)]), max_rows=max(rows), out=out)
+    rq.check(out[:-5], first=first, causal=causal, window=window, sinks=sinks, oracle=oracle)
+    assert (out[-5:] == 3.0).all()
+
+
+@pytest.mark.parametrize("dtype,dim,kind,group", [("f16", 64, "int8", 16), ("bf16", 128, "e4m3", 1), ("f16", 256, "e4m3", 32)])
+def test_cut_tiles_with_missing_pages(dtype, dim, kind, group):
+    """... among them all of one part's, and all that a tile sees."""
+    rq, rows, lens, first = make("two", dtype, dim, kind, group, page=32)
+    assert max(parts_of_cut_tiles(rows, lens, first, 1, 64, dim, False, 0, 0)) == 3
+    whole = rq.tables.copy()
+    rq.tables[2, :up(lens[2], 32) // 3 + 1] = -1
+    rq.tables[0, 5:9], rq.tables[1, 3] = rq.codes[0].shape[0], 2 ** 31 - 1
+    rq.check(rq.run(causal=False, max_rows=max(rows)), first=first, oracle=oracle)
+    rq.tables = whole
+    rq.tables[2] = -1
+    got = rq.run(causal=False, max_rows=max(rows))
+    rq.check(got, first=first, oracle=oracle)
+    assert (got[sum(rows[:2]):] == 0).all()
+
+
+@pytest.mark.parametrize("dim,group", [(64, 1), (128, 16), (256, 1)])
+def test_codes_that_are_no_numbers_in_cut_tiles(dim, group):
+    """A code of V that is no number, seen by some rows of a cut tile: these have no number in its channel, the others and the other channels stay as they were."""
+    rq, rows, lens, first = make("alone", "f16", dim, "e4m3", group)
+    assert max(parts_of_cut_tiles(rows, lens, first, 1, 64, dim, True, 0, 0)) > 1
+    clean = rq.run(causal=True, max_rows=max(rows)).cpu()
+    for key in (0, 130, first[0] + 20):                                     # in the first part, in another, and between the rows of the tile
+        sees = max(0, key - first[0])
+        where, keep = (int(rq.tables[0, key // 64]), slice(None), key % 64, 5), rq.codes[1].clone()
+        rq.codes[1].view(torch.int8)[where] = 0x7f
+        got = rq.run(causal=True, max_rows=max(rows)).cpu()
+        assert torch.isnan(got[sees:, :, 5]).all() and torch.equal(got[:sees], clean[:sees])
+        assert torch.equal(got[:, :, :5], clean[:, :, :5]) and torch.equal(got[:, :, 6:], clean[:, :, 6:])
+        rq.codes[1] = keep
+
+
+def test_cut_tiles_of_shared_heads():
+    """32 heads over 8, as a model has them, the same from call to call."""
+    rows, lens, first = [700, 2400, 1100], [3000, 3600, 2900], [2300, 1200, 1800]
+    assert max(parts_of_cut_tiles(rows, lens, first, 4, 8, 128, True, 0, 0)) > 1
+    rq = Requests(1, rows, lens, 32, 8, 128, "bf16", "e4m3", 64, 64)
+    out = rq.run(causal=True, max_rows=max(rows))
+    for _ in range(3):
+        assert torch.equal(out, rq.run(causal=True, max_rows=max(rows)))
+    # (64 bits for one head of each K/V head: all of them take a minute)
+    rq.q = rq.q[:, ::4]
+    rq.check(out[:, ::4].contiguous(), first=first, causal=True, oracle=oracle)
