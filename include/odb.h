@@ -648,8 +648,9 @@ long long odb_paged_attention_quant_workspace(const odb_attention *a, const odb_
 
 /* odb_step_paged over such pages (dtype ODB_F16): K and V of the rows are stored as odb_qk_norm_rope_quant stores them, at first_pos[r] + i, where that is
  * below kv_len[r] and the row's position is in the table of angles; slots is not looked at.  The codes of the next layers lie rows->layer_stride
- * bytes further each (a multiple of 16), the scales scale_layer_stride floats (a multiple of 4).  Queries beyond the binary16 range, and K or
- * V that are not finite, are reported by odb_model_status.  Else as odb_step_paged. */
+ * bytes further each (a multiple of 16), the scales scale_layer_stride floats (a multiple of 4).  Queries beyond the binary16 range, K or
+ * V that are not finite, and answers of the attention beyond the binary16 range, are reported by odb_model_status (K and V beyond it that are finite
+ * are stored as they are).  Else as odb_step_paged. */
 int odb_step_paged_quant(odb_model *m, const odb_paged_rows *rows, const odb_quant_pages *layer0, long long scale_layer_stride, void *stream);
 
 /* Copies cached K (kv = 0, post-RoPE, logical channel order) or V (kv = 1) of
