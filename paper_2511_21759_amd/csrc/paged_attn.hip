@@ -786,12 +786,14 @@ void paged_attn_plan(const odb_pages &p, int n, int rows, int group, int max_row
     *items = *split ? *split : numbers(tile_rows);
 }
 
-// Half the bytes a key, and whole tiles of up to 64 requests are given out longest first.  nt and the shape of many rows in few tiles as above; else:
-// Many rows with a tile for every CU: whole, however ragged (whole, longest first / pieces / whole in order of the requests: four pieces of
-// prompts, 727 to 1449 rows of 2694 to 5995 positions, 304 / 321 / 392 us).  Where a last round of workgroups would hold a few tiles only,
-// these are cut, which costs a join and its workspace (three of 503 to 997 rows under a window of 900, 526 tiles and 512 workgroups at once: 83 / 107 us
-// uncut; four pieces, two full rounds: 319 / 304).  Full rounds have nothing to cut (2048 rows of as many positions 79 us, 86 with the join; 4096 203,
-// 218; 8192 688, 716).
+// Half the bytes a key, and whole tiles of up to 64 requests are given out longest first.  nt, and many rows whole or in pieces, as above (whole longest first /
+// pieces, us, 32 heads over 8 of 128 where nothing else is said: four pieces of prompts, 727 to 1449 rows of 2694 to 5995 positions, 304 / 321, in order of the
+// requests 392; 32 x 24 rows of 300 to 5000 158 / 63, 100 x 24 212 / 157, 64 x 24 of 1000 to 8000 256 / 170, of 5000 each 219 / 229; 40 x 40 of 300 to 8000 250 /
+// 131, 60 x 48 of 1000 to 6000 225 / 253; 2 x 1500 of 5000 to 9000 262 / 193, 3 x 900 338 / 351; 64 heads over 8 of 64, 32 x 12 of 300 to 5000 115 / 50; 16 over 2 of
+// 256, 130 x 8 190 / 84).
+// Where a last round of whole tiles' workgroups would hold a few only, these are cut, which costs a join and its workspace (three of 503 to 997 rows under a
+// window of 900, 526 tiles and 512 workgroups at once: 83 / 107 us uncut; four pieces, two full rounds: 319 / 304).  Full rounds have nothing to cut (2048 rows of as
+// many positions 79 us, 86 with the join; 4096 203, 218; 8192 688, 716).
 // Few rows: cuts for two workgroups a CU with 32 rows too (8 x 32 rows of 500 to 3000, 32 heads over 32: 45 us, one 53); whole where
 // the keys are up to 1536 and the pairs enough (10 x 32 rows of 454 to 1364: 24 / 31 us in pieces).
 void paged_attn_quant_plan(const odb_pages &p, int n, int rows, int group, int max_rows, long long max_len, long long columns, int *nt, int *split,
@@ -802,9 +804,7 @@ void paged_attn_quant_plan(const odb_pages &p, int n, int rows, int group, int m
     const long long most = (long long)max_rows * group, full = (long long)rows * group / tile_rows, numbers = (n + full) | 1;
     const long long tiles = min((n < rows ? n : rows) + full, (long long)n * ((most + tile_rows - 1) / tile_rows)), pairs = tiles * p.n_kv_heads;
     if (*nt == kManyRows) {
-        if (pairs < 256) return;
-        *split = 0;
-        *items = numbers;
+        if (*split || pairs < 256) return;
         const int at_once = (512 + p.n_kv_heads - 1) / p.n_kv_heads;
         const long long over = tiles % at_once;
         if (n <= 64 && full >= at_once && full / at_once == tiles / at_once && over > 0 && 2 * over <= at_once && tiles <= 4ll * at_once) {

@@ -144,3 +144,17 @@ def test_cut_tiles_of_shared_heads():
     # (64 bits for one head of each K/V head: all of them take a minute)
     rq.q = rq.q[:, ::4]
     rq.check(out[:, ::4].contiguous(), first=first, causal=True, oracle=oracle)
+
+
+@pytest.mark.parametrize("dtype,dim,kind,group", [("f16", 64, "int8", 1), ("bf16", 128, "e4m3", 16), ("bf16", 256, "int8", 16)])
+@pytest.mark.parametrize("n,causal,window,sinks", [(40, True, 0, 0), (70, False, 0, 0), (70, True, 5000, 3)])
+def test_many_ragged_requests_in_pieces(n, causal, window, sinks, dtype, dim, kind, group):
+    """A tile of each request and a tile for every CU, lengths from nothing to 4300: pieces of all tiles' stages."""
+    rng = np.random.default_rng(n + dim)
+    rows = [int(x) for x in rng.choice([0, 1, 20, 24, 24, 24, 24], n)]
+    lens = [int(m + rng.integers(0, 500)) for m in rows]
+    lens[3], lens[n - 2], rows[3] = 4300, 2900, 24
+    lens[5] = 0
+    rq = Requests(n + dim, rows, lens, 32, 8, dim, dtype, kind, group, 32)
+    first = [max(0, length - m) for m, length in zip(rows, lens)]
+    rq.check(rq.run(first=first, causal=causal, window=window, sinks=sinks, max_rows=24), first=first, causal=causal, window=window, sinks=sinks, oracle=oracle)

@@ -20,10 +20,17 @@ def workspace(lib, rows, max_rows, n, heads=32, kv=8, dim=128, length=8192):    
 @pytest.mark.parametrize("rows,max_rows,n", [(2048, 2048, 1), (4096, 4096, 1), (6144, 6144, 1), (8192, 8192, 1), (2048, 1024, 2), (4096, 1024, 4)])
 def test_rounds_that_are_full_have_nothing_to_cut(lib, rows, max_rows, n):          # noqa: F811
     """64 tiles of 128 rows and heads run at once (512 workgroups, 8 K/V heads): whole rounds of them need no sums of parts, no join and no room for either."""
-    assert workspace(lib, rows, max_rows, n) == 0
+    assert workspace(lib, rows, max_rows, n, length=4032) == 0        # (two requests of longer keys go in pieces)
 
 
 @pytest.mark.parametrize("rows,max_rows,n", [(2080, 2080, 1), (3000, 3000, 1), (4100, 4100, 1), (4200, 2400, 3)])
 def test_tiles_of_a_last_round_that_holds_a_few_are_cut(lib, rows, max_rows, n):    # noqa: F811
     # parts of 64 places, heads of K/V, rows of a tile: sums and (reference, sum), twice; then where each row's parts are
     assert workspace(lib, rows, max_rows, n) >= 2 * 64 * 8 * 128 * (128 * 4 + 8) + rows * 32 * 8
+
+
+@pytest.mark.parametrize("rows,max_rows,n,heads,kv,dim", [(768, 24, 32, 32, 8, 128), (2400, 24, 100, 32, 8, 128), (384, 12, 32, 64, 8, 64),
+                                                          (1040, 8, 130, 16, 2, 256)])
+def test_ragged_requests_of_long_keys_go_in_pieces(lib, rows, max_rows, n, heads, kv, dim):       # noqa: F811
+    """Requests with a tile or two each, whose lengths may differ: whole tiles would all wait for the longest.  In pieces as over 16-bit pages."""
+    assert workspace(lib, rows, max_rows, n, heads, kv, dim, 9024) > 0
