@@ -794,8 +794,9 @@ void paged_attn_plan(const odb_pages &p, int n, int rows, int group, int max_row
 // Where a last round of whole tiles' workgroups would hold a few only, these are cut, which costs a join and its workspace (three of 503 to 997 rows under a
 // window of 900, 526 tiles and 512 workgroups at once: 83 / 107 us uncut; four pieces, two full rounds: 319 / 304).  Full rounds have nothing to cut (2048 rows of as
 // many positions 79 us, 86 with the join; 4096 203, 218; 8192 688, 716).
-// Few rows: cuts for two workgroups a CU with 32 rows too (8 x 32 rows of 500 to 3000, 32 heads over 32: 45 us, one 53); whole where
-// the keys are up to 1536 and the pairs enough (10 x 32 rows of 454 to 1364: 24 / 31 us in pieces).
+// Few rows: cuts for two workgroups a CU with 32 rows too (8 x 32 rows of 500 to 3000, 32 heads over 32: 45 us, one 53); whole where the pairs are enough and
+// the keys up to 1536, up to 768 with heads of 256 (whole / pieces, 32 heads over 32: 10 x 32 rows of 454 to 1364 24 / 31, of 900 to 1500 28 / 34, 14 x 32 of
+// 1490 to 1500 41 / 53, 8 x 48 of 1400 to 1500 38 / 40; longer ones, 64 heads over 8 of 64, 20 x 4 rows of 300 to 3000 31 / 20, 40 x 4 of 1000 to 3000 34 / 32).
 void paged_attn_quant_plan(const odb_pages &p, int n, int rows, int group, int max_rows, long long max_len, long long columns, int *nt, int *split,
                            long long *items, int *slots) {
     paged_attn_plan(p, n, rows, group, max_rows, max_len, columns, nt, split, items);
@@ -814,7 +815,7 @@ void paged_attn_quant_plan(const odb_pages &p, int n, int rows, int group, int m
         return;
     }
     if (!*split) return;
-    if (*nt > 1 && n <= 64 && pairs >= 160 && pairs <= 512 && (max_len + 31) / 32 * p.head_dim <= 48 * 128) {
+    if (*nt > 1 && n <= 64 && pairs >= 160 && pairs <= 512 && (max_len + 31) / 32 * max(p.head_dim, 128) <= 48 * 128) {
         *split = 0;
         *items = numbers;
     } else if (*nt == 2 && p.head_dim != 256) {

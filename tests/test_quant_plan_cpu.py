@@ -34,3 +34,9 @@ def test_tiles_of_a_last_round_that_holds_a_few_are_cut(lib, rows, max_rows, n):
 def test_ragged_requests_of_long_keys_go_in_pieces(lib, rows, max_rows, n, heads, kv, dim):       # noqa: F811
     """Requests with a tile or two each, whose lengths may differ: whole tiles would all wait for the longest.  In pieces as over 16-bit pages."""
     assert workspace(lib, rows, max_rows, n, heads, kv, dim, 9024) > 0
+
+
+@pytest.mark.parametrize("heads,kv,dim,rows,n,longest,whole", [(32, 32, 128, 320, 10, 1536, True), (32, 32, 128, 320, 10, 1600, False), (64, 8, 64, 80, 20, 1536, True),
+                                                               (64, 8, 64, 80, 20, 3008, False), (16, 16, 256, 320, 10, 768, True), (16, 16, 256, 320, 10, 832, False)])
+def test_few_rows_are_whole_up_to_1536_keys(lib, heads, kv, dim, rows, n, longest, whole):      # noqa: F811
+    assert (workspace(lib, rows, rows // n, n, heads, kv, dim, longest) == 0) == whole
