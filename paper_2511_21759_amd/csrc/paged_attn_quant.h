@@ -525,7 +525,7 @@ constexpr int kMostShares = 16;          // parts of a tile that is cut
 // codes to two pieces beside each other and stores every second piece at once, which the swizzle is made for (PAIRS in k_piece and v_piece).
 // Bound by vector and matrix instructions together: 74 of the one and 17 of the other for a row tile and 32 keys, 38 more than with 16-bit pages:
 // 8 products and 4 conversions for p times V's scale, 8 conversions of codes, what the two references ask for.  Four requests of 4096 rows at 8192 positions, 32
-// heads over 8 of 128: 2.64 ms with E4M3 codes and scales of 64 positions (834 TFLOP/s), 2.83 with INT8 codes and a scale a position (777), 16-bit pages 2.33.
+// heads over 8 of 128: 2.63 ms with E4M3 codes and scales of 64 positions (836 TFLOP/s), 2.79 with INT8 codes and a scale a position (788), 16-bit pages 2.30.
 template <int CODES, int DH, bool EVEN>
 __global__ __launch_bounds__(256, 2) void quant_rows_kernel(PagedAttnQuant a) {
     typedef RowsShape<DH> Shape;
