@@ -600,8 +600,8 @@ typedef struct {
  *   in 32 bits, so that the rounding of s moves no tie);  where s grows, codes that stay are rounded anew to it, else they are left alone.
  * A group whose values are all below 2^-100, with nothing that stays, has codes and scale zero; a scale below 2^-110 counts as zero.  Positions of the group that are not
  * below kv_len[r] are left alone.  The same call again writes the same codes and scales.
- * Of values that are not finite, infinities become the largest code of their sign and no numbers become zero; they do not count for a,
- * and *odd is set to 1 (it is never cleared).
+ * Of values that are not finite, infinities become the largest code of their sign (zero where nothing else gives the group a scale) and no numbers
+ * become zero; they do not count for a, and *odd is set to 1 (it is never cleared).
  *   q, k, v, in_dtype, rows, n_heads, strides, gains, eps, table, n_pos, rot_dim, interleaved, q_out   as for odb_qk_norm_rope; in_dtype is
  *               ODB_F32 or the pages' dtype, which q_out has
  *   positions   dev int32 [rows]: of the angles.  A position outside [0, n_pos) marks a padding row: its queries become zero, nothing is stored
